@@ -13,6 +13,11 @@
  *   spec_accept        acceptance-rejection with residual resampling and the bonus
  *                      token (Section 2.1).
  *
+ * Around them, what a paged cache needs: spec_append_kv writes the step's keys and values
+ * (rotated by their positions) before the attention, spec_compact_kv tidies up after
+ * acceptance; spec_append_kv_quant, spec_verify_attn_quant and spec_compact_kv_quant are
+ * the same three over a cache of 8-bit values.
+ *
  * Conventions common to every entry point
  *   - Pointers are DEVICE pointers unless the comment says "host".
  *   - The caller owns every buffer (inputs, outputs, workspace).  The library
@@ -359,6 +364,125 @@ int32_t spec_compact_kv(
     const int32_t* q_offsets,    /* [B+1] prefix sums of n[b]                          */
     const int32_t* parent,       /* [total_q] or NULL = linear chains                  */
     const int32_t* stop_node,    /* [B] last accepted node, -1 = none                  */
+    int32_t* new_len,            /* optional [B]                                       */
+    void* stream);
+
+/* ------------------------------------------------------------------------------
+ * spec_append_kv
+ *
+ * Writes the keys and values of new tokens into the paged bf16 cache, rotated by their
+ * positions on the way, and rotates their queries: the call before spec_verify_attn.
+ * Token i of request b (row q_offsets[b] + i of q, k, v) goes to logical slot
+ * ctx_len[b] + i, for every KV head; prompts (any length, parent == NULL) and drafts
+ * alike.  Values are copied, queries rotated into q_out (contiguous, as spec_verify_attn
+ * takes them).  Rotation (rotary position embedding): the first rotary_dim dimensions of
+ * a head are pairs (x1, x2), dimension i with i + rotary_dim / 2, or 2 i with 2 i + 1
+ * (interleaved != 0); with a = position * inv_freq[i] (64-bit arithmetic)
+ *   x1' = s (x1 cos a - x2 sin a),   x2' = s (x2 cos a + x1 sin a),
+ * s = rotary_scale; results are rounded once.  The position is positions[row] if given,
+ * else ctx_len[b] + depth, depth = i (parent == NULL) or the number of ancestors of node
+ * i: after spec_compact_kv the accepted path is rotated as a linear context is.
+ * Slots whose page is outside [0, num_pages), or behind max_pages_per_req pages, receive
+ * nothing (their queries are rotated all the same); rows from q_offsets[B] on, and slots
+ * no token goes to, are left as they are.  The pages that receive tokens belong to one
+ * request only.  A draft tree has at most 128 nodes (max_q_per_req with parent).
+ * q_out == q is allowed where q_stride is num_q_heads * head_dim; else outputs must not
+ * overlap inputs.  q, k, v, q_out and the pools are 16-byte aligned, the strides
+ * multiples of 8 elements (SPEC_ERR_SHAPE otherwise).  No workspace.
+ * ---------------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch;             /* B >= 0                                              */
+  int32_t num_q_heads;       /* Hq                                                  */
+  int32_t num_kv_heads;      /* Hkv; Hq + 2 Hkv at most 8192                        */
+  int32_t head_dim;          /* D: 64 or 128                                        */
+  int32_t page_size;         /* tokens per cache page: 16                           */
+  int32_t total_q;           /* rows of q, k, v; q_offsets[B] at most               */
+  int32_t max_q_per_req;     /* upper bound of the new tokens of a request          */
+  int32_t max_pages_per_req; /* row stride of block_table                           */
+  int32_t num_pages;         /* pages of the pools                                  */
+  int32_t rotary_dim;        /* 0 (no rotation) .. D, a multiple of 16              */
+  int32_t interleaved;       /* pairs: 0 = (i, i + rotary_dim / 2), 1 = (2 i, 2 i + 1) */
+  float rotary_scale;        /* s; 0 selects 1                                      */
+} spec_append_desc;
+
+int32_t spec_append_kv(
+    const spec_append_desc* desc, /* host                                             */
+    const void* q, int64_t q_stride, /* [total_q] rows of [Hq, D] bf16, q_stride elements
+                                    apart; NULL (with q_out NULL) = keys and values only */
+    const void* k, int64_t k_stride, /* ... [Hkv, D]                                  */
+    const void* v, int64_t v_stride, /* ... [Hkv, D]                                  */
+    const float* inv_freq,       /* [rotary_dim / 2]; may be NULL when rotary_dim is 0 */
+    const int32_t* positions,    /* optional [total_q] rotation positions              */
+    void* k_pool,                /* [num_pages, Hkv, page_size, D] bf16, modified      */
+    void* v_pool,                /* [num_pages, Hkv, page_size, D] bf16, modified      */
+    const int32_t* block_table,  /* [B, max_pages_per_req]                             */
+    const int32_t* ctx_len,      /* [B] tokens before the new ones                     */
+    const int32_t* q_offsets,    /* [B+1]                                              */
+    const int32_t* parent,       /* [total_q] or NULL, as for spec_verify_attn         */
+    void* q_out,                 /* [total_q, Hq, D] bf16                              */
+    void* stream);
+
+/* ------------------------------------------------------------------------------
+ * The 8-bit cache: spec_append_kv_quant, spec_verify_attn_quant, spec_compact_kv_quant
+ *
+ * Half the bytes of the bf16 cache, which bound the attention.  An entry is an e4m3 code
+ * (1-4-3 bits, largest value 448, NaN but no infinity) times the scale of its page and KV
+ * head; keys and values have scales of their own.  Scales are powers of two, 2^-100 to
+ * 2^119, written by these calls:
+ *   k_pool  [num_pages, Hkv, D / 16, page_size, 16] bytes: dimension 16 c + i of token t
+ *           at [c, t, i];     k_scale [num_pages, Hkv] fp32
+ *   v_pool  [num_pages, Hkv, D, page_size] bytes: [dimension, token];  v_scale likewise.
+ *
+ * spec_append_kv_quant is spec_append_kv into it (same descriptor and arguments; keys are
+ * rotated in fp32 and rounded once, to 8 bits).  Per page and head the scale becomes the
+ * least one that holds the largest new entry, at least the page's own where tokens
+ * 0 .. ctx_len[b] - 1 lie in it; where that is larger than the page's own, those are
+ * rewritten for it (exactly, but for codes that become subnormal).  Infinities are stored
+ * as +-448 times the scale, which only finite entries set; NaN stays NaN.
+ *
+ * spec_verify_attn_quant is spec_verify_attn over it: same descriptor, masks and results
+ * (at most 128 nodes per request, one for plain decoding; at most 1024 query heads per
+ * KV head).  Positions whose page is
+ * outside [0, num_pages), or behind max_pages_per_req pages, count as not there; a row
+ * that sees no position at all gives zeros and lse = -infinity.  Slots behind the last
+ * draft are read but take no part, whatever they hold; an entry of a draft that is NaN
+ * reaches the rows that see that draft only.  Entries of v below 2^-39 of the largest
+ * scale of v in the context may lose precision.  out is exact to about 2^-12 (fp32: 2^-20)
+ * of its row's size before it is rounded.  The workspace need not be cleared.
+ *
+ * spec_compact_kv_quant is spec_compact_kv over it.  A page that entries move to gets the
+ * largest of its own scale, if it holds tokens 0 .. ctx_len[b] - 1, and of the scales of
+ * the pages that they come from.  Entries whose page (of origin or of destination) is
+ * outside the pool stay where they are.  At most 128 nodes per request.
+ * ---------------------------------------------------------------------------- */
+int32_t spec_append_kv_quant(
+    const spec_append_desc* desc, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+    const void* v, int64_t v_stride, const float* inv_freq, const int32_t* positions,
+    void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
+    const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent, void* q_out, void* stream);
+
+/* Bytes of workspace spec_verify_attn_quant uses for this descriptor (host call; the token
+ * hint does not matter). */
+size_t spec_verify_attn_quant_workspace_size(const spec_attn_desc* desc);
+
+int32_t spec_verify_attn_quant(
+    const spec_attn_desc* desc,  /* host                                              */
+    int32_t num_pages,           /* pages of the pools                                 */
+    const void* q,               /* [total_q, Hq, D] bf16                             */
+    const void* k_pool, const void* v_pool, const float* k_scale, const float* v_scale,
+    const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent,
+    void* out,                   /* [total_q, Hq, D] of out_dtype                     */
+    float* lse,                  /* optional [total_q, Hq]                             */
+    void* workspace, size_t workspace_bytes, void* stream);
+/* q, the pools, out and workspace must be 16-byte aligned (SPEC_ERR_SHAPE otherwise). */
+
+/* One-line description of the kernel and the cut spec_verify_attn_quant takes (host). */
+int32_t spec_describe_attn_quant_plan(const spec_attn_desc* desc, char* buf, size_t buf_bytes);
+
+int32_t spec_compact_kv_quant(
+    int32_t B, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t max_pages_per_req, int32_t num_pages,
+    void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
+    const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent, const int32_t* stop_node,
     int32_t* new_len,            /* optional [B]                                       */
     void* stream);
 

@@ -28,6 +28,8 @@ EXPORTS = [
     "spec_routing_scores", "spec_adaptive_speculation", "spec_compact_kv",
     "spec_row_stats_size", "spec_lm_head_workspace_size", "spec_lm_head", "spec_accept_prestats",
     "spec_describe_lm_head_plan",
+    "spec_append_kv", "spec_append_kv_quant", "spec_verify_attn_quant_workspace_size", "spec_verify_attn_quant",
+    "spec_describe_attn_quant_plan", "spec_compact_kv_quant",
     "spec_strerror", "spec_abi_version",
 ]
 
@@ -38,6 +40,15 @@ class SpecAttnDesc(ctypes.Structure):
         ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("total_q", ctypes.c_int32),
         ("max_q_per_req", ctypes.c_int32), ("max_pages_per_req", ctypes.c_int32),
         ("total_kv_tokens_hint", ctypes.c_int64), ("scale", ctypes.c_float), ("out_dtype", ctypes.c_int32),
+    ]
+
+
+class SpecAppendDesc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("total_q", ctypes.c_int32),
+        ("max_q_per_req", ctypes.c_int32), ("max_pages_per_req", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("rotary_scale", ctypes.c_float),
     ]
 
 
@@ -115,6 +126,20 @@ def lib() -> ctypes.CDLL:
         L.spec_describe_lm_head_plan.argtypes = [i32] * 3 + [ctypes.c_char_p, sz]
         L.spec_lm_head.restype = i32
         L.spec_lm_head.argtypes = [i32, i32, i32, vp, vp, f32, vp, vp, vp, sz, vp]
+        i64 = ctypes.c_int64
+        rows = [ctypes.POINTER(SpecAppendDesc), vp, i64, vp, i64, vp, i64]
+        L.spec_append_kv.restype = i32
+        L.spec_append_kv.argtypes = rows + [vp] * 10
+        L.spec_append_kv_quant.restype = i32
+        L.spec_append_kv_quant.argtypes = rows + [vp] * 12
+        L.spec_verify_attn_quant_workspace_size.restype = sz
+        L.spec_verify_attn_quant_workspace_size.argtypes = [ctypes.POINTER(SpecAttnDesc)]
+        L.spec_verify_attn_quant.restype = i32
+        L.spec_verify_attn_quant.argtypes = [ctypes.POINTER(SpecAttnDesc), i32] + [vp] * 12 + [sz, vp]
+        L.spec_describe_attn_quant_plan.restype = i32
+        L.spec_describe_attn_quant_plan.argtypes = [ctypes.POINTER(SpecAttnDesc), ctypes.c_char_p, sz]
+        L.spec_compact_kv_quant.restype = i32
+        L.spec_compact_kv_quant.argtypes = [i32] * 6 + [vp] * 11
         _lib = L
     return _lib
 
@@ -378,3 +403,116 @@ def spec_compact_kv(k_pool, v_pool, block_table, ctx_len, q_offsets, parent, sto
                                _ptr(new_len), _stream(stream))
     if rc != SPEC_OK:
         raise SpecError("spec_compact_kv", rc)
+
+
+# ---- keys and values into the cache, and the 8-bit cache ----
+def make_append_desc(batch, num_q_heads, num_kv_heads, head_dim, total_q, max_q_per_req, max_pages_per_req, num_pages,
+                     rotary_dim=0, interleaved=False, rotary_scale=0.0, page_size=16) -> SpecAppendDesc:
+    return SpecAppendDesc(batch, num_q_heads, num_kv_heads, head_dim, page_size, total_q, max_q_per_req, max_pages_per_req,
+                          num_pages, rotary_dim, int(interleaved), rotary_scale)
+
+
+def _typed(t, dtype, what):
+    """The pointer of a contiguous tensor of that type (None: NULL); another type would be read as this one's bits."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} expected, not {t.dtype}")
+    return _ptr(t)
+
+
+def _rows(t, heads, head_dim, rows, what):
+    """(pointer, elements between tokens) of a [tokens, heads, head_dim] bf16 tensor whose tokens may lie apart."""
+    import torch
+    if t is None:
+        return None, 0
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{what}: torch.bfloat16 expected, not {t.dtype}")
+    if tuple(t.shape) != (rows, heads, head_dim) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+        raise ValueError(f"{what}: [{rows}, {heads}, {head_dim}] with contiguous heads expected")
+    return t.data_ptr(), t.stride(0) if rows > 1 else heads * head_dim
+
+
+def _quant_pools(k_pool, v_pool, k_scale, v_scale):
+    """Pointers of an 8-bit cache: k_pool [num_pages, Hkv, D / 16, 16, 16] and v_pool [num_pages, Hkv, D, 16] of torch.float8_e4m3fn
+    or torch.uint8, scales [num_pages, Hkv] float32."""
+    import torch
+    if k_pool.element_size() != 1 or v_pool.element_size() != 1:
+        raise TypeError("the pools of the 8-bit cache have one byte per entry")
+    pages, heads, dim, page = v_pool.shape
+    if tuple(k_pool.shape) != (pages, heads, dim // 16, page, 16) or tuple(k_scale.shape) != (pages, heads) or k_scale.shape != v_scale.shape:
+        raise ValueError("k_pool [num_pages, Hkv, D / 16, 16, 16], v_pool [num_pages, Hkv, D, 16] and scales [num_pages, Hkv] expected")
+    return (_ptr(k_pool), _ptr(v_pool), _typed(k_scale, torch.float32, "k_scale"), _typed(v_scale, torch.float32, "v_scale"))
+
+
+def _append(fn, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream):
+    import torch
+    D, i32 = desc.head_dim, torch.int32
+    qp, qs = _rows(q, desc.num_q_heads, D, desc.total_q, "q")
+    kp, ks = _rows(k, desc.num_kv_heads, D, desc.total_q, "k")
+    vp, vs = _rows(v, desc.num_kv_heads, D, desc.total_q, "v")
+    rc = getattr(lib(), fn)(ctypes.byref(desc), qp, qs, kp, ks, vp, vs, _typed(inv_freq, torch.float32, "inv_freq"),
+                            _typed(positions, i32, "positions"), *pools, _typed(block_table, i32, "block_table"),
+                            _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"), _typed(parent, i32, "parent"),
+                            _typed(q_out, torch.bfloat16, "q_out"), _stream(stream))
+    if rc != SPEC_OK:
+        raise SpecError(fn, rc)
+
+
+def spec_append_kv(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, block_table, ctx_len, q_offsets, parent, q_out,
+                   positions=None, stream=None) -> None:
+    """Device tensors: q [total_q, Hq, D], k and v [total_q, Hkv, D] bf16 (tokens may lie apart, as slices of one projection do),
+    inv_freq [rotary_dim / 2] float32, pools [num_pages, Hkv, 16, D] bf16 (modified), the rest int32; q_out [total_q, Hq, D] bf16."""
+    import torch
+    pools = (_typed(k_pool, torch.bfloat16, "k_pool"), _typed(v_pool, torch.bfloat16, "v_pool"))
+    _append("spec_append_kv", desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream)
+
+
+def spec_append_kv_quant(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets,
+                         parent, q_out, positions=None, stream=None) -> None:
+    """spec_append_kv into an 8-bit cache (pools and scales modified)."""
+    _append("spec_append_kv_quant", desc, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale), block_table, ctx_len,
+            q_offsets, parent, q_out, positions, stream)
+
+
+def spec_verify_attn_quant_workspace_size(desc: SpecAttnDesc) -> int:
+    return int(lib().spec_verify_attn_quant_workspace_size(ctypes.byref(desc)))
+
+
+def spec_verify_attn_quant(desc: SpecAttnDesc, q, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, out,
+                           lse=None, workspace=None, stream=None) -> None:
+    """spec_verify_attn over an 8-bit cache; workspace uint8 of at least spec_verify_attn_quant_workspace_size(desc) bytes."""
+    import torch
+    i32 = torch.int32
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib().spec_verify_attn_quant(ctypes.byref(desc), k_pool.shape[0], _typed(q, torch.bfloat16, "q"),
+                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale), _typed(block_table, i32, "block_table"),
+                                      _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
+                                      _typed(parent, i32, "parent"),
+                                      _typed(out, torch.float32 if desc.out_dtype == SPEC_F32 else torch.bfloat16, "out"),
+                                      _typed(lse, torch.float32, "lse"), _ptr(workspace), ws_bytes, _stream(stream))
+    if rc != SPEC_OK:
+        raise SpecError("spec_verify_attn_quant", rc)
+
+
+def spec_describe_attn_quant_plan(desc: SpecAttnDesc) -> str:
+    buf = ctypes.create_string_buffer(256)
+    rc = lib().spec_describe_attn_quant_plan(ctypes.byref(desc), buf, 256)
+    if rc != SPEC_OK:
+        raise SpecError("spec_describe_attn_quant_plan", rc)
+    return buf.value.decode()
+
+
+def spec_compact_kv_quant(k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, stop_node, new_len=None,
+                          stream=None) -> None:
+    """spec_compact_kv over an 8-bit cache (pools and scales modified in place); the rest int32 device tensors."""
+    import torch
+    i32 = torch.int32
+    pages, heads, dim, page = v_pool.shape
+    rc = lib().spec_compact_kv_quant(ctx_len.shape[0], heads, dim, page, block_table.shape[1], pages,
+                                     *_quant_pools(k_pool, v_pool, k_scale, v_scale), _typed(block_table, i32, "block_table"),
+                                     _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
+                                     _typed(parent, i32, "parent"), _typed(stop_node, i32, "stop_node"),
+                                     _typed(new_len, i32, "new_len"), _stream(stream))
+    if rc != SPEC_OK:
+        raise SpecError("spec_compact_kv_quant", rc)

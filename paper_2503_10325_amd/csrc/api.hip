@@ -40,6 +40,9 @@ const char* spec_strerror(int32_t status) {
 
 int32_t spec_abi_version(void) { return 3; }
 
+// Query heads per KV head that the 8-bit attention takes: rows per KV head are a grid dimension.
+constexpr int kQuantMaxGroup = 1024;
+
 static int check_attn_desc(const spec_attn_desc* d) {
   if (!d) return SPEC_ERR_NULL;
   if (d->batch < 0 || d->total_q < 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 ||
@@ -387,6 +390,122 @@ int32_t spec_compact_kv(int32_t B, int32_t num_kv_heads, int32_t head_dim, int32
   a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets; a.parent = parent;
   a.stop_node = stop_node; a.new_len = new_len;
   launch_compact_kv(a, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+static int32_t append_entry(bool quant, const spec_append_desc* d, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, const float* inv_freq, const int32_t* positions, void* k_pool,
+                            void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table, const int32_t* ctx_len,
+                            const int32_t* q_offsets, const int32_t* parent, void* q_out, void* stream) {
+  if (!d) return SPEC_ERR_NULL;
+  if (d->batch < 0 || d->total_q < 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->max_q_per_req < 0 ||
+      d->max_pages_per_req < 0 || d->num_pages < 0)
+    return SPEC_ERR_SHAPE;
+  if (d->num_q_heads % d->num_kv_heads != 0) return SPEC_ERR_SHAPE;
+  if (d->rotary_dim < 0 || d->rotary_dim > d->head_dim || !(d->rotary_scale >= 0.f)) return SPEC_ERR_SHAPE;
+  if ((d->head_dim != 64 && d->head_dim != 128) || d->page_size != 16 || d->rotary_dim % 16 != 0) return SPEC_ERR_UNSUPPORTED;
+  if (d->interleaved != 0 && d->interleaved != 1) return SPEC_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->num_q_heads) + 2 * static_cast<int64_t>(d->num_kv_heads) > 8192) return SPEC_ERR_UNSUPPORTED;
+  if (parent && d->max_q_per_req > 128) return SPEC_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->total_q) / 16 + 2 * static_cast<int64_t>(d->batch) > (1 << 23)) return SPEC_ERR_UNSUPPORTED;
+  if (d->batch == 0 || d->total_q == 0) return SPEC_OK;
+  if (!k || !v || !k_pool || !v_pool || !block_table || !ctx_len || !q_offsets) return SPEC_ERR_NULL;
+  if ((q == nullptr) != (q_out == nullptr)) return SPEC_ERR_NULL;
+  if (d->rotary_dim > 0 && !inv_freq) return SPEC_ERR_NULL;
+  if (quant && (!k_scale || !v_scale)) return SPEC_ERR_NULL;
+  if (d->max_pages_per_req == 0 || d->num_pages == 0 || d->max_q_per_req == 0) return SPEC_ERR_SHAPE;
+  const int64_t q_row = static_cast<int64_t>(d->num_q_heads) * d->head_dim, kv_row = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
+  if ((q && (q_stride < q_row || q_stride % 8)) || k_stride < kv_row || k_stride % 8 || v_stride < kv_row || v_stride % 8) return SPEC_ERR_SHAPE;
+  if (q && q == q_out && q_stride != q_row) return SPEC_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(q_out) |
+       reinterpret_cast<uintptr_t>(k_pool) | reinterpret_cast<uintptr_t>(v_pool)) & 15u)
+    return SPEC_ERR_SHAPE;
+  AppendArgs a{};
+  a.B = d->batch; a.Hq = d->num_q_heads; a.Hkv = d->num_kv_heads; a.D = d->head_dim; a.total_q = d->total_q;
+  a.max_pages = d->max_pages_per_req; a.num_pages = d->num_pages; a.rotary = d->rotary_dim; a.interleaved = d->interleaved;
+  a.rotary_scale = d->rotary_scale == 0.f ? 1.f : d->rotary_scale;
+  a.q = q; a.k = k; a.v = v; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.inv_freq = inv_freq; a.positions = positions; a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;
+  a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets; a.parent = parent; a.q_out = q_out;
+  launch_append(a, quant, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+int32_t spec_append_kv(const spec_append_desc* desc, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const float* inv_freq, const int32_t* positions, void* k_pool, void* v_pool,
+                       const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent,
+                       void* q_out, void* stream) {
+  return append_entry(false, desc, q, q_stride, k, k_stride, v, v_stride, inv_freq, positions, k_pool, v_pool, nullptr, nullptr, block_table,
+                      ctx_len, q_offsets, parent, q_out, stream);
+}
+
+int32_t spec_append_kv_quant(const spec_append_desc* desc, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, const float* inv_freq, const int32_t* positions, void* k_pool,
+                             void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table, const int32_t* ctx_len,
+                             const int32_t* q_offsets, const int32_t* parent, void* q_out, void* stream) {
+  return append_entry(true, desc, q, q_stride, k, k_stride, v, v_stride, inv_freq, positions, k_pool, v_pool, k_scale, v_scale, block_table,
+                      ctx_len, q_offsets, parent, q_out, stream);
+}
+
+size_t spec_verify_attn_quant_workspace_size(const spec_attn_desc* desc) {
+  if (check_attn_desc(desc) != SPEC_OK || desc->num_q_heads / desc->num_kv_heads > kQuantMaxGroup) return 0;
+  const AttnArgs a = attn_args_from(desc);
+  return quant_attn_workspace_bytes(a, make_quant_attn_plan(a));
+}
+
+int32_t spec_verify_attn_quant(const spec_attn_desc* desc, int32_t num_pages, const void* q, const void* k_pool, const void* v_pool,
+                               const float* k_scale, const float* v_scale, const int32_t* block_table, const int32_t* ctx_len,
+                               const int32_t* q_offsets, const int32_t* parent, void* out, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  const int rc = check_attn_desc(desc);
+  if (rc != SPEC_OK) return rc;
+  if (num_pages < 0) return SPEC_ERR_SHAPE;
+  if (desc->num_q_heads / desc->num_kv_heads > kQuantMaxGroup) return SPEC_ERR_UNSUPPORTED;
+  if (desc->batch == 0 || desc->total_q == 0) return SPEC_OK;
+  if (!q || !k_pool || !v_pool || !k_scale || !v_scale || !block_table || !ctx_len || !q_offsets || !out) return SPEC_ERR_NULL;
+  if (num_pages == 0) return SPEC_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_pool) | reinterpret_cast<uintptr_t>(v_pool) |
+       reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15u)
+    return SPEC_ERR_SHAPE;
+  AttnArgs a = attn_args_from(desc);
+  if (a.scale == 0.f) a.scale = 1.0f / sqrtf(static_cast<float>(a.D));
+  const QuantAttnPlan plan = make_quant_attn_plan(a);
+  const size_t need = quant_attn_workspace_bytes(a, plan);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SPEC_ERR_WORKSPACE;
+  a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.block_table = block_table; a.ctx_len = ctx_len;
+  a.q_offsets = q_offsets; a.parent = parent; a.out = out; a.lse = lse; a.workspace = workspace;
+  launch_attn_quant(a, k_scale, v_scale, num_pages, plan, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+int32_t spec_describe_attn_quant_plan(const spec_attn_desc* desc, char* buf, size_t buf_bytes) {
+  const int rc = check_attn_desc(desc);
+  if (rc != SPEC_OK) return rc;
+  if (!buf || buf_bytes == 0) return SPEC_ERR_NULL;
+  const AttnArgs a = attn_args_from(desc);
+  if (desc->num_q_heads / desc->num_kv_heads > kQuantMaxGroup) return SPEC_ERR_UNSUPPORTED;
+  const QuantAttnPlan p = make_quant_attn_plan(a);
+  snprintf(buf, buf_bytes, "attn_quant_kernel<%d, %d>: %d query rows per workgroup, %d group(s) of them, %d range(s) of the tokens per KV head",
+           a.D, p.wave_blocks, 16 * p.blocks, p.groups, p.ranges);
+  return SPEC_OK;
+}
+
+int32_t spec_compact_kv_quant(int32_t B, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t max_pages_per_req,
+                              int32_t num_pages, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                              const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent,
+                              const int32_t* stop_node, int32_t* new_len, void* stream) {
+  if (B < 0 || num_kv_heads <= 0 || max_pages_per_req < 0 || num_pages < 0) return SPEC_ERR_SHAPE;
+  if ((head_dim != 64 && head_dim != 128) || page_size != 16) return SPEC_ERR_UNSUPPORTED;
+  if (B > 65535 || num_kv_heads > 65535) return SPEC_ERR_UNSUPPORTED;
+  if (B == 0) return SPEC_OK;
+  if (!k_pool || !v_pool || !k_scale || !v_scale || !block_table || !ctx_len || !q_offsets || !stop_node) return SPEC_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(k_pool) | reinterpret_cast<uintptr_t>(v_pool)) & 15u) return SPEC_ERR_SHAPE;
+  QuantCompactArgs a{};
+  a.B = B; a.Hkv = num_kv_heads; a.D = head_dim; a.max_pages = max_pages_per_req; a.num_pages = num_pages;
+  a.k_pool = static_cast<unsigned char*>(k_pool); a.v_pool = static_cast<unsigned char*>(v_pool);
+  a.k_scale = k_scale; a.v_scale = v_scale; a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets;
+  a.parent = parent; a.stop_node = stop_node; a.new_len = new_len;
+  launch_compact_kv_quant(a, static_cast<hipStream_t>(stream));
   return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
 }
 

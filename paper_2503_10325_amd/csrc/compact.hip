@@ -9,6 +9,7 @@
 // everything is read.  Pure data movement: at most 128 rows of 2*D bytes per tensor, latency-bound.
 #include "common.h"
 #include "kernels.h"
+#include "quant.h"
 
 namespace specv {
 
@@ -77,6 +78,152 @@ void launch_compact_kv(const CompactArgs& a, hipStream_t stream) {
   if (a.B <= 0 || a.Hkv <= 0) return;
   hipLaunchKernelGGL(compact_kv_kernel, dim3(a.B, a.Hkv), dim3(kCompactThreads), 0, stream, a.Hkv, a.D, a.max_pages,
                      a.k_pool, a.v_pool, a.block_table, a.ctx_len, a.q_offsets, a.parent, a.stop_node, a.new_len);
+}
+
+// ----------------------------------------------------------------------------------
+// The same for the 8-bit cache (quant.h), whose pages have a scale each: a written page takes the largest of its own scale, if it
+// holds committed tokens, and of those of the pages that its new entries come from; entries that move to, or stay under, a larger
+// scale are rewritten for it (exactly, but for those that become subnormal).
+//
+// One workgroup per (request, KV head).  A job is 16 bytes of a written page: one token's chunk of 16 dimensions of K, one dimension's
+// 16 slots of V.  All jobs are read and worked out, a barrier, then all are written.  Latency-bound: offsets -> page ids -> scales and
+// entries -> store.
+// ----------------------------------------------------------------------------------
+constexpr int kQuantPathPages = kCompactMaxNodes / kQuantPage + 1;       // pages that 128 consecutive slots touch
+
+template <int D>
+__global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
+    int Hkv, int max_pages, int num_pages, unsigned char* __restrict__ k_pool, unsigned char* __restrict__ v_pool,
+    float* __restrict__ k_scale, float* __restrict__ v_scale, const int32_t* __restrict__ block_table,
+    const int32_t* __restrict__ ctx_len, const int32_t* __restrict__ q_offsets, const int32_t* __restrict__ parent,
+    const int32_t* __restrict__ stop_node, int32_t* __restrict__ new_len) {
+  constexpr int kRounds = (kQuantPathPages * D + kCompactThreads - 1) / kCompactThreads;    // D jobs of 16 bytes per page and tensor
+  const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+  __shared__ int sh_parent[kCompactMaxNodes], sh_path[kCompactMaxNodes];      // path: leaf -> root
+  __shared__ int sh_depth;
+  __shared__ int sh_page[kCompactMaxNodes], sh_slot[kCompactMaxNodes];        // where entry d comes from; page -1: it is not moved
+  __shared__ float sh_scale[2][kCompactMaxNodes];                            // its scale, then its ratio to the new one
+  __shared__ int sh_to[kQuantPathPages];                                     // written pages (-1: none)
+  __shared__ float sh_old[2][kQuantPathPages], sh_new[2][kQuantPathPages];
+  const int o = q_offsets[b];
+  int n = q_offsets[b + 1] - o;
+  n = n < 0 ? 0 : (n > kCompactMaxNodes ? kCompactMaxNodes : n);
+  const int ctx = ctx_len[b], stop = stop_node[b];
+  if (ctx < 0) return;
+  if (parent == nullptr) {                                                   // linear drafts lie where they belong
+    if (tid == 0 && h == 0 && new_len) new_len[b] = ctx + (stop >= 0 && stop < n ? stop + 1 : 0);
+    return;
+  }
+  if (tid < n) sh_parent[tid] = parent[o + tid];
+  __syncthreads();
+  if (tid == 0) {
+    int depth = 0;
+    for (int a = stop; a >= 0 && a < n && depth < kCompactMaxNodes;) {
+      sh_path[depth++] = a;
+      const int p = sh_parent[a];
+      a = p < a ? p : -1;                                                    // a malformed parent entry ends the path
+    }
+    sh_depth = depth;
+    if (h == 0 && new_len) new_len[b] = ctx + depth;
+  }
+  __syncthreads();
+  const int depth = sh_depth;
+  if (depth == 0) return;
+  const int32_t* bt = block_table + static_cast<int64_t>(b) * max_pages;
+  auto page_of = [&](int lp) {
+    const int id = lp < max_pages ? bt[lp] : -1;
+    return id >= 0 && id < num_pages ? id : -1;
+  };
+  const int lp0 = ctx / kQuantPage, pages = (ctx + depth - 1) / kQuantPage - lp0 + 1, held = ctx % kQuantPage;
+  if (tid < depth) {
+    const int pos = ctx + sh_path[depth - 1 - tid], id = page_of(pos / kQuantPage);
+    sh_page[tid] = id;
+    sh_slot[tid] = pos % kQuantPage;
+    sh_scale[0][tid] = id < 0 ? 0.f : k_scale[static_cast<int64_t>(id) * Hkv + h];
+    sh_scale[1][tid] = id < 0 ? 0.f : v_scale[static_cast<int64_t>(id) * Hkv + h];
+  }
+  __syncthreads();
+  if (tid < 2 * pages) {
+    const int j = tid >> 1, which = tid & 1, id = page_of(lp0 + j);
+    const float own = id < 0 ? 0.f : (which ? v_scale : k_scale)[static_cast<int64_t>(id) * Hkv + h];
+    float m = j == 0 && held > 0 ? own : 0.f;
+    for (int t = 0; t < kQuantPage; ++t) {
+      const int d = (lp0 + j) * kQuantPage + t - ctx;
+      if (d >= 0 && d < depth) m = fmaxf(m, sh_scale[which][d]);
+    }
+    sh_old[which][j] = own;
+    sh_new[which][j] = m > 0.f ? m : own;                                   // (no entry reaches it)
+    if (which == 0) sh_to[j] = id;
+  }
+  __syncthreads();
+  if (tid < depth) {
+    const int j = (ctx + tid) / kQuantPage - lp0;
+    sh_scale[0][tid] *= inverse_scale(sh_new[0][j]);
+    sh_scale[1][tid] *= inverse_scale(sh_new[1][j]);
+  }
+  __syncthreads();
+
+  auto at = [&](int page, int byte) { return (static_cast<int64_t>(page) * Hkv + h) * (kQuantPage * D) + byte; };
+  raw4 kw[kRounds], vw[kRounds];
+  bool k_set[kRounds], v_set[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int it = r * kCompactThreads + tid, j = it / D, in = it % D;
+    k_set[r] = v_set[r] = false;
+    if (j >= pages || sh_to[j] < 0) continue;
+    {
+      const int chunk = in / kQuantPage, t = in % kQuantPage, d = (lp0 + j) * kQuantPage + t - ctx;
+      int page = -1, slot = t;
+      float ratio = 1.f;
+      if (d >= 0 && d < depth) {
+        page = sh_page[d]; slot = sh_slot[d]; ratio = sh_scale[0][d];
+      } else if (d < 0 && sh_new[0][j] > sh_old[0][j]) {
+        page = sh_to[j]; ratio = sh_old[0][j] * inverse_scale(sh_new[0][j]);
+      }
+      if (page >= 0) {
+        kw[r] = *reinterpret_cast<const raw4*>(k_pool + at(page, chunk * 256 + slot * 16));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) kw[r][w] = rescale_e4m3(kw[r][w], ratio);
+        k_set[r] = true;
+      }
+    }
+    {
+      vw[r] = *reinterpret_cast<const raw4*>(v_pool + at(sh_to[j], in * kQuantPage));
+      const int d0 = (lp0 + j) * kQuantPage - ctx;                          // entry that slot 0 takes
+      if (j == 0 && sh_new[1][0] > sh_old[1][0]) {
+        const float ratio = sh_old[1][0] * inverse_scale(sh_new[1][0]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t mine = slot_mask(4 * w, 0, held);
+          vw[r][w] = (rescale_e4m3(vw[r][w], ratio) & mine) | (vw[r][w] & ~mine);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kQuantPage; ++t) {
+        const int d = d0 + t;
+        if (d < 0 || d >= depth || sh_page[d] < 0) continue;
+        const uint32_t byte = rescale_e4m3(v_pool[at(sh_page[d], in * kQuantPage + sh_slot[d])], sh_scale[1][d]) & 0xffu;
+        vw[r][t >> 2] = (vw[r][t >> 2] & ~(0xffu << (8 * (t & 3)))) | (byte << (8 * (t & 3)));
+      }
+      v_set[r] = true;
+    }
+  }
+  __syncthreads();                                                           // everything that is read has been
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int it = r * kCompactThreads + tid, j = it / D, in = it % D;
+    if (k_set[r]) *reinterpret_cast<raw4*>(k_pool + at(sh_to[j], in * 16)) = kw[r];
+    if (v_set[r]) *reinterpret_cast<raw4*>(v_pool + at(sh_to[j], in * 16)) = vw[r];
+  }
+  if (tid < 2 * pages && sh_to[tid >> 1] >= 0)
+    (tid & 1 ? v_scale : k_scale)[static_cast<int64_t>(sh_to[tid >> 1]) * Hkv + h] = sh_new[tid & 1][tid >> 1];
+}
+
+void launch_compact_kv_quant(const QuantCompactArgs& a, hipStream_t stream) {
+  if (a.B <= 0 || a.Hkv <= 0) return;
+  auto kernel = a.D == 128 ? compact_kv_quant_kernel<128> : compact_kv_quant_kernel<64>;
+  hipLaunchKernelGGL(kernel, dim3(a.B, a.Hkv), dim3(kCompactThreads), 0, stream, a.Hkv, a.max_pages, a.num_pages, a.k_pool, a.v_pool,
+                     a.k_scale, a.v_scale, a.block_table, a.ctx_len, a.q_offsets, a.parent, a.stop_node, a.new_len);
 }
 
 }  // namespace specv

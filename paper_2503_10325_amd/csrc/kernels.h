@@ -134,6 +134,42 @@ struct CompactArgs {
   int32_t* new_len;
 };
 void launch_compact_kv(const CompactArgs& a, hipStream_t stream);
+struct QuantCompactArgs {
+  int B, Hkv, D, max_pages, num_pages;
+  unsigned char* k_pool;
+  unsigned char* v_pool;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* block_table;
+  const int32_t* ctx_len;
+  const int32_t* q_offsets;
+  const int32_t* parent;
+  const int32_t* stop_node;
+  int32_t* new_len;
+};
+void launch_compact_kv_quant(const QuantCompactArgs& a, hipStream_t stream);
+
+// ---- append.hip -------------------------------------------------------------------
+struct AppendArgs {
+  int B, Hq, Hkv, D, total_q, max_pages, num_pages, rotary, interleaved;
+  float rotary_scale;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride;
+  const float* inv_freq;
+  const int32_t* positions;
+  void* k_pool;
+  void* v_pool;
+  float* k_scale;              // 8-bit cache only
+  float* v_scale;
+  const int32_t* block_table;
+  const int32_t* ctx_len;
+  const int32_t* q_offsets;
+  const int32_t* parent;
+  void* q_out;
+};
+void launch_append(const AppendArgs& a, bool quant, hipStream_t stream);
 
 // ---- fuse.hip ---------------------------------------------------------------------
 struct FuseArgs {
@@ -192,6 +228,20 @@ AttnPlan make_attn_plan(const AttnArgs& a, bool small_workspace = false);
 size_t attn_workspace_bytes(const AttnArgs& a, const AttnPlan& plan);
 const char* attn_plan_name(const AttnPlan& plan);
 int launch_attn(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);   // 0 or a negative spec_status
+
+// ---- attn_quant.hip ---------------------------------------------------------------
+// A pure function of the descriptor, as AttnPlan.
+struct QuantAttnPlan {
+  int blocks;         // 16-row blocks of query rows a workgroup takes (1 .. 8)
+  int groups;         // ... groups of so many blocks that cover a request's rows
+  int wave_blocks;    // most of them a wave multiplies a unit with: 1 or 2
+  int ranges;         // workgroups per KV head and group: equal ranges of the batch's tokens
+  int least_units;    // ... of at least so many 64-token units
+};
+QuantAttnPlan make_quant_attn_plan(const AttnArgs& a);
+size_t quant_attn_workspace_bytes(const AttnArgs& a, const QuantAttnPlan& plan);
+void launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_scale, int num_pages, const QuantAttnPlan& plan,
+                       hipStream_t stream);
 
 // Vector (16-byte) accesses need 16-byte aligned base pointers; the launchers pick the scalar
 // variants of their kernels when a caller's pointer is not.
