@@ -30,10 +30,13 @@ typedef _Float16 qf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kQaThreads = 256;
 constexpr int kQaWaves = 4;
-constexpr int kUnit = 64;                     // tokens a wave takes at a time
+constexpr int kUnit = 32;                     // tokens a wave takes at a time
 constexpr int kQaMaxNodes = 128;
-constexpr int kQaBlocks = 8;                  // most 16-row blocks of a workgroup
-constexpr int kWeightBias = 14;               // weights are fed as fp16(2^14 p), at most 16384: they stay normal down to p = 2^-28
+constexpr float kNoScore = -3.0e38f;          // the reference before the first position: finite, so that -infinity stays ahead of nothing
+constexpr int kQaWaveBlocks = 3;              // most 16-row blocks that a wave multiplies a unit with: what 256 registers hold
+constexpr int kQaBlocks = kQaWaves * kQaWaveBlocks;      // ... of a workgroup
+constexpr int kWeightBias = 6;                // weights are fed as fp16(2^6 p): normal down to p = 2^-20, and
+constexpr float kSlack = 8.f;                 // the reference of a row's softmax follows its maximum when that is 2^8 ahead: below 2^14 then
 constexpr float kLeastV = 3.0517578125e-5f;   // 2^-15: what V may be scaled by and still be exact in fp16
 
 struct QuantAttnParams {
@@ -97,6 +100,10 @@ __device__ __forceinline__ int range_of(int64_t u, int64_t units, int used) {
 }
 
 
+// __any as the compiler knows it to be uniform: a branch on it stays a scalar one (around the other kind it keeps a second copy of every
+// register that the branch changes).
+__device__ __forceinline__ bool any_lane(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0ull; }
+
 // max and sum over the four lane groups: the same bits in lanes n, 16 + n, 32 + n and 48 + n.
 __device__ __forceinline__ float groups_max(float x) {
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -140,16 +147,16 @@ __device__ __forceinline__ uint32_t spread4(uint32_t bits) {
   return ((bits & 1u) * 0xffu) | ((bits >> 1 & 1u) * 0xff00u) | ((bits >> 2 & 1u) * 0xff0000u) | ((bits >> 3 & 1u) * 0xff000000u);
 }
 
-template <int D>
+template <int D, int MAXB>
 struct QuantAttnShared {
   static constexpr int kStride = D + 4;                        // floats; padded row of the merge
   unsigned long long anc[kQaMaxNodes][2];
   int parent[kQaMaxNodes];
   int nans;                                                    // a draft's value is NaN
-  float m[kQaWaves][64], l[kQaWaves][64];
+  float m[kQaWaves][16 * MAXB], l[kQaWaves][16 * MAXB];
   union {
     __align__(16) float o[kQaWaves][16][kStride];              // the merge, when the queries are done with
-    __align__(16) raw4 q[kQaBlocks * 2 * (D / 64)][kWave];     // query operands: [block, step][lane]
+    __align__(16) raw4 q[kQaWaves * MAXB * 2 * (D / 64)][kWave];     // query operands: [block, step][lane]
   };
 };
 
@@ -162,8 +169,8 @@ struct QuantPiece {
 
 // Dimensions d0 .. d0 + 3 of a row's result are NaN where a value is that the row sees, among the units that reach the drafts (of the others
 // every row sees every token, and the products are NaN by themselves).
-template <int D>
-__device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const QuantAttnShared<D>& S, const QuantPiece& J, int row, int d0, float4& o) {
+template <int D, typename Shared>
+__device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const Shared& S, const QuantPiece& J, int row, int d0, float4& o) {
   const int node = (J.row_base + row) / P.G;
   const int end = min(J.t1 * kUnit, J.ctx + J.n);
   for (int tok = max(J.t0 * kUnit, J.ctx & ~(kUnit - 1)); tok < end; ++tok) {
@@ -183,8 +190,8 @@ __device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const Qu
 // SANITIZE: NaN among the drafts' values are taken out of the products (where a row does not see a draft its weight is zero, and zero times
 // NaN would be NaN) and put back into the results of the rows that see them.  Without, a piece that meets one writes nothing and
 // says so in S.nans.
-template <int D, int NB, int TERMS, bool SANITIZE>
-__device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnShared<D>& S, const QuantPiece& J) {
+template <int D, int NB, int TERMS, bool SANITIZE, typename Shared>
+__device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S, const QuantPiece& J) {
   constexpr int kH = D / 64;                                   // K: 16-byte chunks of a lane per token
   constexpr int kDT = D / 16;                                  // 16-dimension tiles of the output
   const int tid = threadIdx.x, lane = tid & 63;
@@ -222,21 +229,20 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
     __syncthreads();
   }
 
-  int node[NB];
-#pragma unroll
-  for (int qi = 0; qi < NB; ++qi) node[qi] = (J.row_base + min(16 * (kind * NB + qi) + rn, J.rows - 1)) / P.G;
+  auto node_of = [&](int qi) __attribute__((always_inline)) { return (J.row_base + min(16 * (kind * NB + qi) + rn, J.rows - 1)) / P.G; };
   const int64_t page_bytes = static_cast<int64_t>(P.Hkv) * kQuantPage * D;
-  const unsigned char* k_lane = P.k_pool + static_cast<int64_t>(J.kvh) * kQuantPage * D + g * 256 + (rn & 3) * 16;
-  const unsigned char* v_lane = P.v_pool + static_cast<int64_t>(J.kvh) * kQuantPage * D + rn * 16;
+  const unsigned char* k_lane = P.k_pool + static_cast<int64_t>(J.kvh) * kQuantPage * D + g * 256 + (8 * ((rn >> 2) & 1) + (rn & 3)) * 16;
+  const unsigned char* v_lane = P.v_pool + static_cast<int64_t>(J.kvh) * kQuantPage * D + rn * 16 + 8 * (g & 1);
   const int32_t* bt = P.block_table + static_cast<int64_t>(J.b) * P.max_pages;
   const int last_page = min((L - 1) / kQuantPage, P.max_pages - 1);
 
-  int id_k, id_v;                                               // of the tile whose loads go out next; lane: page rn / 4 of K, page g of V
+  int id_k, id_v;                                               // of the unit whose loads go out next; lane: page rn / 8 of K, page g / 2 of V
   auto fetch_ids = [&](int t) __attribute__((always_inline)) {
-    id_k = bt[min(4 * t + (rn >> 2), last_page)];
-    id_v = bt[min(4 * t + g, last_page)];
+    id_k = bt[min(2 * t + (rn >> 3), last_page)];
+    id_v = bt[min(2 * t + (g >> 1), last_page)];
   };
-  raw4 kr[kH][4], vr[kDT];
+  raw4 kr[kH][2];
+  uint2 vr[kDT];
   float ks, vs;
   bool page_ok;
   // a page that is none of the pool's holds nothing: its tokens are masked, what is read instead is page 0
@@ -246,25 +252,26 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
 #pragma unroll
     for (int h = 0; h < kH; ++h)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) kr[h][t] = *reinterpret_cast<const raw4*>(at + 1024 * h + 64 * t);
+      for (int st = 0; st < 2; ++st) kr[h][st] = *reinterpret_cast<const raw4*>(at + 1024 * h + 64 * st);
   };
   auto issue_v = [&](int t) __attribute__((always_inline)) {
     const bool ok = usable(id_v);
     const int id = ok ? id_v : 0;
     const unsigned char* at = v_lane + id * page_bytes;
 #pragma unroll
-    for (int d = 0; d < kDT; ++d) vr[d] = *reinterpret_cast<const raw4*>(at + 256 * d);
+    for (int d = 0; d < kDT; ++d) vr[d] = *reinterpret_cast<const uint2*>(at + 256 * d);
     ks = P.k_scale[static_cast<int64_t>(id) * P.Hkv + J.kvh];
     vs = P.v_scale[static_cast<int64_t>(id) * P.Hkv + J.kvh];
-    page_ok = ok && 4 * t + g < P.max_pages;
+    page_ok = ok && 2 * t + (g >> 1) < P.max_pages;
   };
 
-  float m_run[NB], l_run[NB], v_ref = __uint_as_float(static_cast<uint32_t>(kLeastScaleExp + 127) << 23);
+  // ref: what a row's weights are relative to, in log2 units; sum: of this lane's tokens; v_ref: what the results are relative to
+  float ref[NB], sum[NB], v_ref = __uint_as_float(static_cast<uint32_t>(kLeastScaleExp + 127) << 23);
   qf32x4 oacc[NB][kDT];
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
-    m_run[qi] = -INFINITY;
-    l_run[qi] = 0.f;
+    ref[qi] = kNoScore;
+    sum[qi] = 0.f;
 #pragma unroll
     for (int d = 0; d < kDT; ++d) oacc[qi][d] = qf32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -273,129 +280,132 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
   auto unit = [&](int t, int next, auto more_tag) __attribute__((always_inline)) {
     constexpr bool MORE = decltype(more_tag)::value;
     // ---- scores ----
-    qf32x4 s[NB][4];
-#pragma unroll
-    for (int qi = 0; qi < NB; ++qi)
-#pragma unroll
-      for (int st = 0; st < 4; ++st) s[qi][st] = qf32x4{0.f, 0.f, 0.f, 0.f};
+    qf32x4 s[NB][2];
 #pragma unroll
     for (int h = 0; h < kH; ++h)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        qbf16x8 q[NB];
+        const qbf16x8 a0 = operand_bf16(kr[h][0][2 * e], kr[h][0][2 * e + 1]), a1 = operand_bf16(kr[h][1][2 * e], kr[h][1][2 * e + 1]);
 #pragma unroll
-        for (int qi = 0; qi < NB; ++qi) q[qi] = __builtin_bit_cast(qbf16x8, S.q[(kind * NB + qi) * 2 * kH + 2 * h + e][lane]);
-#pragma unroll
-        for (int st = 0; st < 4; ++st) {
-          const qbf16x8 a = operand_bf16(kr[h][st][2 * e], kr[h][st][2 * e + 1]);
-#pragma unroll
-          for (int qi = 0; qi < NB; ++qi) s[qi][st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[qi], s[qi][st], 0, 0, 0);
+        for (int qi = 0; qi < NB; ++qi) {
+          const qbf16x8 q = __builtin_bit_cast(qbf16x8, S.q[(kind * NB + qi) * 2 * kH + 2 * h + e][lane]);
+          const qf32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          s[qi][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, q, h + e == 0 ? zero : s[qi][0], 0, 0, 0);
+          s[qi][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, q, h + e == 0 ? zero : s[qi][1], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     const bool ok = page_ok;
-    const float factor = ks * P.c;
-    // V is fed relative to the largest scale so far (v_ref), down to 2^-15 of it by itself, exactly; what a page's scale is smaller still
-    // goes into its weights, whose fp16 has room for it.
-    const float v_new = fmaxf(v_ref, groups_max(ok ? vs : 0.f));
-    const float ratio = vs * inverse_scale(v_new), v_by = fmaxf(ratio, kLeastV), p_by = ratio * inverse_scale(v_by);
-    const float grow = v_ref * inverse_scale(v_new);
-    const float shift = static_cast<float>(kWeightBias) + static_cast<float>(static_cast<int>(__float_as_uint(p_by) >> 23) - 127);
-    const float unshift = inverse_scale(p_by);
-    v_ref = v_new;
+    const float factor = ks * P.c, v_own = ok ? vs : 0.f;
     if constexpr (MORE) issue_k();
 
-    // ---- mask: only where the unit reaches the drafts, or a page is none ----
-    const int past = t * kUnit + 16 * g - J.ctx;                // page g starts that far behind the context
-    const bool drafts = (t + 1) * kUnit > J.ctx, masked = __any(!ok) || drafts;
+    // ---- masks: only where the unit reaches the drafts, or a page is none ----
+    const int past = t * kUnit + 16 * (g >> 1) - J.ctx;         // the lane's page starts that far behind the context
+    const bool drafts = (t + 1) * kUnit > J.ctx, masked = any_lane(!ok) || drafts;
     if (masked) {
 #pragma unroll
       for (int qi = 0; qi < NB; ++qi) {
-        uint32_t seen = page_mask(0ull, 0ull, past);
-        if (past > -16) seen = page_mask(S.anc[node[qi]][0], S.anc[node[qi]][1], past);
-        seen = ok ? seen : 0u;
+        uint32_t seen = 0xffffu;
+        if (past > -16) {
+          const int node = node_of(qi);
+          seen = page_mask(S.anc[node][0], S.anc[node][1], past);
+        }
+        seen = ok ? seen >> (8 * (g & 1)) : 0u;
 #pragma unroll
-        for (int st = 0; st < 4; ++st)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[qi][st][i] = (seen >> (4 * st + i)) & 1u ? s[qi][st][i] : -INFINITY;
-        __builtin_amdgcn_sched_barrier(0);
       }
     }
 
-    // ---- online softmax; 2^shift times the weights, as TERMS fp16 terms ----
-    raw4 hi[NB][2], lo[TERMS == 2 ? NB : 1][2];
+    // ---- a row's reference follows its maximum where that has come far ahead, and the scale of V likewise ----
+    float top[NB];
+    bool ahead = v_own > v_ref;
 #pragma unroll
     for (int qi = 0; qi < NB; ++qi) {
-      float top = -INFINITY;
+      top[qi] = fmaxf(fmaxf(fmaxf(s[qi][0][0], s[qi][0][1]), fmaxf(s[qi][0][2], s[qi][0][3])),
+                      fmaxf(fmaxf(s[qi][1][0], s[qi][1][1]), fmaxf(s[qi][1][2], s[qi][1][3]))) * factor;    // factor > 0
+      ahead |= top[qi] > ref[qi] + kSlack;
+    }
+    if (any_lane(ahead)) {
+      const float v_new = fmaxf(v_ref, groups_max(v_own)), v_by = v_ref * inverse_scale(v_new);
+      v_ref = v_new;
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[qi][st][i]);
-      top = groups_max(top * factor);                           // factor > 0: the maximum commutes with it
-      const float m_new = fmaxf(m_run[qi], top);
-      const float m_safe = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = fast_exp2(m_run[qi] - m_safe), by = alpha * grow;
-      if (__any(by != 1.f)) {
+      for (int qi = 0; qi < NB; ++qi) {
+        const float now = fmaxf(ref[qi], groups_max(top[qi]));
+        const float by = fast_exp2(ref[qi] - now);
+        ref[qi] = now;
+        sum[qi] *= by;
+        const float all = by * v_by;
 #pragma unroll
         for (int d = 0; d < kDT; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) oacc[qi][d][i] *= by;
+          for (int i = 0; i < 4; ++i) oacc[qi][d][i] *= all;
       }
-      const float sub = m_safe - shift;
-      float sum = 0.f;
+    }
+
+    // ---- 2^shift times the weights, as TERMS fp16 terms ----
+    // V is fed relative to v_ref, down to 2^-15 of it by itself, exactly; what a page's scale is smaller still goes into its weights, whose
+    // fp16 has room for it.
+    asm volatile("" : "+v"(v_ref));      // (its inverse worked out on both sides of the branch makes it one with an else part, whose copies cost the
+                                         // registers of all results a second time)
+    const float ratio = vs * inverse_scale(v_ref), v_by = fmaxf(ratio, kLeastV), p_by = ratio * inverse_scale(v_by);
+    const float shift = static_cast<float>(static_cast<int>(__float_as_uint(p_by) >> 23) - 127 + kWeightBias);
+    const float unshift = inverse_scale(p_by);
+    raw4 hi[NB], lo[TERMS == 2 ? NB : 1];
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+    for (int qi = 0; qi < NB; ++qi) {
+      const float sub = ref[qi] - shift;
+      float z = 0.f;
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const float p0 = fast_exp2(fmaf(s[qi][st][2 * i], factor, -sub)), p1 = fast_exp2(fmaf(s[qi][st][2 * i + 1], factor, -sub));
-          sum += p0 + p1;
+          z += p0 + p1;
           const qf16x2 h = {static_cast<_Float16>(p0), static_cast<_Float16>(p1)};
-          hi[qi][st >> 1][2 * (st & 1) + i] = __builtin_bit_cast(uint32_t, h);
+          hi[qi][2 * st + i] = __builtin_bit_cast(uint32_t, h);
           if constexpr (TERMS == 2) {
             const qf16x2 r = {static_cast<_Float16>(p0 - static_cast<float>(h[0])), static_cast<_Float16>(p1 - static_cast<float>(h[1]))};
-            lo[qi][st >> 1][2 * (st & 1) + i] = __builtin_bit_cast(uint32_t, r);
+            lo[qi][2 * st + i] = __builtin_bit_cast(uint32_t, r);
           }
         }
-      l_run[qi] = l_run[qi] * alpha + sum * unshift;
-      m_run[qi] = m_new;
-      __builtin_amdgcn_sched_barrier(0);
+      sum[qi] = fmaf(z, unshift, sum[qi]);
     }
 
     // ---- O^T += V^T P^T ----
     // Slots behind the last token, and pages that are none, hold anything: a weight of zero times NaN would be NaN.
-    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+    uint32_t keep[2] = {~0u, ~0u};
     if (masked) {
-      const int valid = ok ? min(max(L - t * kUnit - 16 * g, 0), 16) : 0;
+      const int valid = ok ? min(max(L - t * kUnit - 8 * g, 0), 8) : 0;
       uint32_t nans = 0u;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < 2; ++w) {
         keep[w] = spread4(((1u << valid) - 1u) >> (4 * w));
         if constexpr (!SANITIZE) {
 #pragma unroll
-          for (int d = 0; d < kDT; ++d) nans |= nan_bytes(vr[d][w] & keep[w]);
+          for (int d = 0; d < kDT; ++d) nans |= nan_bytes((w ? vr[d].y : vr[d].x) & keep[w]);
         }
       }
-      if (!SANITIZE && drafts && __any(nans != 0u) && lane == 0) S.nans = 1;
+      if (!SANITIZE && drafts && any_lane(nans != 0u) && lane == 0) S.nans = 1;
     }
 #pragma unroll
     for (int d = 0; d < kDT; ++d) {
-      raw4 v;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        v[w] = vr[d][w] & keep[w];
-        if constexpr (SANITIZE) v[w] = drafts ? v[w] & ~((nan_bytes(v[w]) >> 7) * 0xffu) : v[w];
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const qf16x8 a = operand_f16(v[2 * u], v[2 * u + 1], v_by);
-#pragma unroll
-        for (int qi = 0; qi < NB; ++qi) {
-          oacc[qi][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, __builtin_bit_cast(qf16x8, hi[qi][u]), oacc[qi][d], 0, 0, 0);
-          if constexpr (TERMS == 2)
-            oacc[qi][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, __builtin_bit_cast(qf16x8, lo[qi][u]), oacc[qi][d], 0, 0, 0);
+      uint32_t x = vr[d].x & keep[0], y = vr[d].y & keep[1];
+      if constexpr (SANITIZE) {
+        if (drafts) {
+          x &= ~((nan_bytes(x) >> 7) * 0xffu);
+          y &= ~((nan_bytes(y) >> 7) * 0xffu);
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
+      const qf16x8 a = operand_f16(x, y, v_by);
+#pragma unroll
+      for (int qi = 0; qi < NB; ++qi) {
+        oacc[qi][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, __builtin_bit_cast(qf16x8, hi[qi]), oacc[qi][d], 0, 0, 0);
+        if constexpr (TERMS == 2)
+          oacc[qi][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, __builtin_bit_cast(qf16x8, lo[qi]), oacc[qi][d], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (MORE) {
       issue_v(next);
@@ -426,10 +436,11 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
   // ---- merge the waves that share rows, one block of each wave at a time ----
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
-    l_run[qi] = groups_sum(l_run[qi]) * (1.f / (1 << kWeightBias));
+    sum[qi] = groups_sum(sum[qi]) * (1.f / (1 << kWeightBias));
+    if (sum[qi] == 0.f) ref[qi] = -INFINITY;                    // nothing seen
     if (lane < 16) {
-      S.m[wave][16 * qi + lane] = m_run[qi];
-      S.l[wave][16 * qi + lane] = l_run[qi];
+      S.m[wave][16 * qi + lane] = ref[qi];
+      S.l[wave][16 * qi + lane] = sum[qi];
     }
   }
   if constexpr (!SANITIZE) {
@@ -443,7 +454,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
     __syncthreads();
     float top = -INFINITY;
     for (int s = 0; s < slices; ++s) top = fmaxf(top, S.m[kind + kinds * s][16 * qi + rn]);
-    const float f = m_run[qi] == -INFINITY ? 0.f : fast_exp2(m_run[qi] - top - static_cast<float>(kWeightBias)) * v_ref;
+    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - top - static_cast<float>(kWeightBias)) * v_ref;
 #pragma unroll
     for (int d = 0; d < kDT; ++d)
       *reinterpret_cast<float4*>(&S.o[wave][rn][16 * d + 4 * g]) =
@@ -460,11 +471,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
       for (int s = 0; s < slices; ++s) {
         const int w = k + kinds * s;
         const float mw = S.m[w][16 * qi + r];
-        if (mw == -INFINITY) {
-          Z += S.l[w][16 * qi + r];                             // 0, or NaN where every score is
-        } else {
-          Z += S.l[w][16 * qi + r] * fast_exp2(mw - M);
-        }
+        if (mw != -INFINITY) Z += S.l[w][16 * qi + r] * fast_exp2(mw - M);
         const float4 x = *reinterpret_cast<const float4*>(&S.o[w][r][4 * d4]);
         o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
       }
@@ -492,8 +499,8 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, QuantAttnS
 
 // MAXB: most 16-row blocks a wave multiplies a unit with; TERMS: fp16 terms of a weight.
 template <int D, int MAXB, int TERMS>
-__global__ __launch_bounds__(kQaThreads, MAXB == 1 ? 2 : 1) void attn_quant_kernel(QuantAttnParams P) {
-  __shared__ QuantAttnShared<D> S;
+__global__ __launch_bounds__(kQaThreads, 2) void attn_quant_kernel(QuantAttnParams P) {
+  __shared__ QuantAttnShared<D, MAXB> S;
   const int lane = threadIdx.x & 63;
   const int range = blockIdx.x;
   QuantPiece J;
@@ -539,6 +546,9 @@ __global__ __launch_bounds__(kQaThreads, MAXB == 1 ? 2 : 1) void attn_quant_kern
     const int kinds = blocks <= MAXB ? 1 : (blocks <= 2 * MAXB ? 2 : 4);
     const int per_wave = (blocks + kinds - 1) / kinds;
     [&] {
+      if constexpr (MAXB >= 3) {
+        if (per_wave == 3) return quant_piece<D, 3, TERMS, false>(P, S, J);
+      }
       if constexpr (MAXB >= 2) {
         if (per_wave == 2) return quant_piece<D, 2, TERMS, false>(P, S, J);
       }
@@ -591,7 +601,7 @@ __global__ __launch_bounds__(256) void attn_quant_combine_kernel(QuantAttnParams
     const float2 ml = P.ws_ml[part(s)];
     const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - M);
     const float4 x = *reinterpret_cast<const float4*>(P.ws_o + part(s) * D + 4 * d4);
-    Z += ml.x == -INFINITY ? ml.y : ml.y * f;
+    Z += ml.y * f;
     o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
   }
   const int64_t at_row = static_cast<int64_t>(first + row / P.G) * P.Hq + kvh * P.G + row % P.G;
@@ -612,13 +622,13 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   QuantAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.Hq / a.Hkv);
   const int blocks = static_cast<int>(std::max<int64_t>(1, (rows + 15) / 16));
-  p.blocks = std::min(blocks, kQaBlocks);                       // four waves of two blocks each
-  p.groups = (blocks + p.blocks - 1) / p.blocks;
-  p.wave_blocks = p.blocks <= 1 ? 1 : 2;
+  p.groups = (blocks + kQaBlocks - 1) / kQaBlocks;
+  p.blocks = (blocks + p.groups - 1) / p.groups;
+  p.wave_blocks = std::min(p.blocks, kQaWaveBlocks);
   const int64_t pairs = static_cast<int64_t>(a.Hkv) * p.groups;
   const int64_t target = 512;
   p.ranges = static_cast<int>(std::max<int64_t>(1, target / pairs));
-  p.least_units = 4;
+  p.least_units = 8;
   return p;
 }
 
@@ -632,7 +642,7 @@ size_t quant_attn_workspace_bytes(const AttnArgs& a, const QuantAttnPlan& p) {
 template <int D, int TERMS>
 static void launch_quant(const QuantAttnParams& P, const AttnArgs& a, const QuantAttnPlan& p, hipStream_t stream) {
   const dim3 grid(p.ranges, a.Hkv, p.groups);
-  auto kernel = p.wave_blocks == 1 ? attn_quant_kernel<D, 1, TERMS> : attn_quant_kernel<D, 2, TERMS>;
+  auto kernel = p.wave_blocks == 1 ? attn_quant_kernel<D, 1, TERMS> : (p.wave_blocks == 2 ? attn_quant_kernel<D, 2, TERMS> : attn_quant_kernel<D, kQaWaveBlocks, TERMS>);
   hipLaunchKernelGGL(kernel, grid, dim3(kQaThreads), 0, stream, P);
   if (p.ranges > 1) {
     const int rows = a.max_q * (a.Hq / a.Hkv), per = 256 / (D / 4);
