@@ -474,7 +474,7 @@ int32_t spec_verify_attn_quant(const spec_attn_desc* desc, int32_t num_pages, co
   if (need > 0 && (!workspace || workspace_bytes < need)) return SPEC_ERR_WORKSPACE;
   a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.block_table = block_table; a.ctx_len = ctx_len;
   a.q_offsets = q_offsets; a.parent = parent; a.out = out; a.lse = lse; a.workspace = workspace;
-  launch_attn_quant(a, k_scale, v_scale, num_pages, plan, static_cast<hipStream_t>(stream));
+  if (launch_attn_quant(a, k_scale, v_scale, num_pages, plan, static_cast<hipStream_t>(stream)) != 0) return SPEC_ERR_LAUNCH;
   return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
 }
 
@@ -485,8 +485,8 @@ int32_t spec_describe_attn_quant_plan(const spec_attn_desc* desc, char* buf, siz
   const AttnArgs a = attn_args_from(desc);
   if (desc->num_q_heads / desc->num_kv_heads > kQuantMaxGroup) return SPEC_ERR_UNSUPPORTED;
   const QuantAttnPlan p = make_quant_attn_plan(a);
-  snprintf(buf, buf_bytes, "attn_quant_kernel<%d, %d>: %d query rows per workgroup, %d group(s) of them, %d range(s) of the tokens per KV head",
-           a.D, p.wave_blocks, 16 * p.blocks, p.groups, p.ranges);
+  snprintf(buf, buf_bytes, "attn_quant_kernel<%d, %d, %d>: %d query rows at a time, %d group(s) of them, %d range(s) of the tokens per KV head",
+           a.D, a.out_dtype == SPEC_F32 ? 2 : 1, p.waves, p.rows, p.groups, p.ranges);
   return SPEC_OK;
 }
 

@@ -1,19 +1,22 @@
 // Verify-attention over the 8-bit paged cache (quant.h): the draft queries of each request attend over its committed context and
 // their draft ancestors, keys and values read as e4m3 with a scale per (page, KV head).
 //
-// A wave takes 64 tokens (4 pages) at a time, straight from memory into registers: pages are laid out so that a lane's 16 bytes
-// are matrix operands as they lie, and no LDS, transposition or barrier stands between memory and the matrix cores.
-//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, tokens as M.  Row 4 g + i of sub-tile t is token 4 t + i of page g, so that lane group
-//                 g (lanes 16 g .. 16 g + 15, one query row each) ends up with all 16 tokens of page g: its scale is one register, and
-//   O^T = V^T P^T takes those 16 weights as its operand without any exchange between lanes.
+// A wave takes units of 32 tokens (2 pages), straight from memory into a ring of its own in LDS (K two units deep, V one: both go on to
+// registers at once): no barrier stands between memory and the matrix cores, and the bytes in flight cost no registers.  Pages are laid
+// out so that a lane's 16 (K) or 8 (V) bytes are matrix operands as they lie, without transposition.
+//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, tokens as M.  Row 4 g + i of sub-tile t is token 8 (g % 2) + 4 t + i of page g / 2, so that
+//                 lane group g (lanes 16 g .. 16 g + 15, one query row each) ends up with 8 tokens of one page: its scale is one register, and
+//   O^T = V^T P^T takes those 8 weights as its operand without any exchange between lanes.
 // e4m3 is exact in bf16 and fp16.  K's scale rides on the softmax factor; V is fed in fp16, its page's scale on the conversion, relative to the
 // largest scale so far.  A weight is one fp16 term (2^-12 off, a sixteenth of the rounding of a bf16 result), or two for fp32 results.
 //
-// Work: per KV head (and group of query rows) the 64-token units of all requests lie end to end and are cut into equal ranges,
-// one per workgroup, whatever the lengths; every workgroup works out from ctx_len and q_offsets which requests its range
-// meets.  A range that ends inside a request leaves an unnormalised partial result, attn_quant_combine_kernel merges them.  The waves
-// of a workgroup take units in turn and merge through LDS.
+// Work: a request's query rows of a KV head are taken in groups of up to 64 (a wave multiplies each unit with up to four 16-row blocks).
+// Per KV head the units of all requests and groups lie end to end and are cut into ranges of equal cost, one per workgroup, whatever the
+// lengths; every workgroup works out from ctx_len and q_offsets which pieces its range holds.  A range that ends inside a request
+// leaves an unnormalised partial result; the workgroup that finishes the last piece merges them, in their order.  The four or
+// eight waves of a workgroup take units in turn and merge through LDS.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "common.h"
@@ -28,16 +31,16 @@ typedef __bf16 qbf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 qf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 qf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kQaThreads = 256;
-constexpr int kQaWaves = 4;
 constexpr int kUnit = 32;                     // tokens a wave takes at a time
 constexpr int kQaMaxNodes = 128;
+constexpr int kMergeRoom = 2048;              // (piece, row) pairs whose statistics a merge holds at a time
 constexpr float kNoScore = -3.0e38f;          // the reference before the first position: finite, so that -infinity stays ahead of nothing
-constexpr int kQaWaveBlocks = 3;              // most 16-row blocks that a wave multiplies a unit with: what 256 registers hold
-constexpr int kQaBlocks = kQaWaves * kQaWaveBlocks;      // ... of a workgroup
+constexpr int kQaBlocks = 4;                  // most 16-row blocks that a wave multiplies a unit with: what 256 registers hold (a
+constexpr int most_blocks(int D, int terms) { return D == 128 && terms == 2 ? 3 : kQaBlocks; }      // second term's operands are too many)
 constexpr int kWeightBias = 6;                // weights are fed as fp16(2^6 p): normal down to p = 2^-20, and
 constexpr float kSlack = 8.f;                 // the reference of a row's softmax follows its maximum when that is 2^8 ahead: below 2^14 then
 constexpr float kLeastV = 3.0517578125e-5f;   // 2^-15: what V may be scaled by and still be exact in fp16
+static __device__ const float kNoScale[1] = {0.f};      // read in place of the scale of a page that is none
 
 struct QuantAttnParams {
   const uint16_t* q;
@@ -51,12 +54,14 @@ struct QuantAttnParams {
   const int32_t* parent;
   void* out;
   float* lse;
-  float* ws_o;        // [KV heads * groups][ranges][2][rows][D] unnormalised partial results
+  float* ws_o;        // [KV heads][ranges][2][rows][D] unnormalised partial results
   float2* ws_ml;      // ... [rows] (maximum in log2 units, sum)
-  int B, Hq, Hkv, G, total_q, max_pages, num_pages;
-  int ranges;         // per KV head and group of rows, at most
-  int least_units;    // ... a range has at least this many units where there are enough
-  int blocks;         // 16-row blocks of a group of rows
+  int B, Hq, Hkv, G, total_q, max_q, max_pages, num_pages;
+  unsigned long long* arrived;      // [KV heads][groups][B] messages: how many pieces of a request's rows are done
+  unsigned long long tag;
+  int ranges;         // per KV head, at most
+  int groups;         // of query rows, at most
+  int rows;           // of a group, at most
   float c;            // scale * log2(e)
   int out_f32;
 };
@@ -70,35 +75,84 @@ __device__ __forceinline__ int wave_scan_i32(int x, int lane) {
   return x;
 }
 
-// The units of all requests, 64 requests at a time: lane i holds request 64 k + i.
-struct Requests {
-  int ctx, first, n, units, upto;               // of this lane's request; upto: units up to its end, within these 64
-  int sum;                                      // units of these 64
+// A request's 16-row blocks in groups of at most `most`, alike.
+struct RowGroups {
+  int groups, per;
 };
-__device__ __forceinline__ Requests load_requests(const QuantAttnParams& P, int k, int lane) {
+__device__ __forceinline__ RowGroups group_rows(int rows, int most) {
+  const int blocks = (rows + 15) >> 4;
+  RowGroups r;
+  r.groups = (blocks + most - 1) / most;
+  r.per = (blocks + r.groups - 1) / max(r.groups, 1);
+  return r;
+}
+// What a unit costs its workgroup by the 16-row blocks it is multiplied with, and what a group of rows costs besides: its start and its end.
+__device__ __forceinline__ int unit_cost(int blocks) { return 24 + 4 * blocks; }
+constexpr int kStartCost = 128;
+constexpr int kWholeCost = 776;               // a group of at most this cost (24 units of few rows) is not cut: its merge would take longer
+constexpr int kLeastRange = 256;              // ranges cost at least this, or as much as the average group
+
+// The requests, 64 at a time: lane i holds request 64 k + i.
+struct Requests {
+  int ctx, first, n, units, groups, per;        // of this lane's request
+  int upto;                                     // cost up to its end, within these 64
+  int sum, count;                               // cost of these 64, and their groups
+};
+__device__ __forceinline__ Requests load_requests(const QuantAttnParams& P, int k, int most, int lane) {
   Requests r;
   const int b = 64 * k + lane;
   r.ctx = r.first = r.n = 0;
   if (b < P.B) {
     r.ctx = max(P.ctx_len[b], 0);
     r.first = P.q_offsets[b];
-    r.n = max(min(min(P.q_offsets[b + 1], P.total_q) - r.first, kQaMaxNodes), 0);
+    r.n = max(min(min(P.q_offsets[b + 1], P.total_q) - r.first, P.max_q), 0);
   }
   r.units = r.n > 0 ? static_cast<int>((static_cast<unsigned>(r.ctx) + r.n + kUnit - 1) / kUnit) : 0;
-  r.upto = wave_scan_i32(r.units, lane);
+  const RowGroups g = group_rows(r.n * P.G, most);
+  r.groups = g.groups;
+  r.per = g.per;
+  r.upto = wave_scan_i32(r.groups * (kStartCost + r.units * unit_cost(r.per)), lane);
   r.sum = __builtin_amdgcn_readlane(r.upto, 63);
+  r.count = __builtin_amdgcn_readlane(wave_scan_i32(r.groups, lane), 63);
   return r;
 }
-// Ranges that are used: range s holds the units [s U / ranges, (s + 1) U / ranges).
-__device__ __forceinline__ int used_ranges(const QuantAttnParams& P, int64_t units) {
-  const int64_t want = units / P.least_units;
-  return static_cast<int>(want < 1 ? 1 : (want < P.ranges ? want : P.ranges));
-}
-// The range that unit u is in.
-__device__ __forceinline__ int range_of(int64_t u, int64_t units, int used) {
-  return static_cast<int>(((u + 1) * used + units - 1) / units) - 1;
-}
 
+// The cost of the batch in `used` ranges of equal cost (one more in the first `more`): range s starts at s * each + min(s, more).
+struct Cut {
+  int used, each, more;
+};
+__device__ __forceinline__ Cut cut_ranges(const QuantAttnParams& P, int total, int count) {
+  Cut c;
+  c.used = min(max(max(total / kLeastRange, count), 1), P.ranges);
+  c.each = total / c.used;
+  c.more = total - c.each * c.used;
+  return c;
+}
+__device__ __forceinline__ int range_start(const Cut& c, int s) { return s * c.each + min(s, c.more); }
+__device__ __forceinline__ int range_of(const Cut& c, int at) {
+  const int wide = c.more * (c.each + 1);
+  return at < wide ? at / (c.each + 1) : c.more + (at - wide) / c.each;
+}
+// A group of a request's rows that starts at `start` has its units there if it is not cut, else unit 0 there and unit k at start + kStartCost + k * cost; a
+// unit belongs to the range that its place is in.  Ranges cost more than any unit, so those behind the second unit's hold one each.
+struct Place {
+  int start, units, cost;
+};
+__device__ __forceinline__ bool is_whole(const Place& p) { return kStartCost + p.units * p.cost <= kWholeCost; }
+__device__ __forceinline__ int first_unit(const Place& p, int at) {           // at or behind `at`
+  return at <= p.start ? 0 : (is_whole(p) ? p.units : max(1, (at - p.start - kStartCost + p.cost - 1) / p.cost));
+}
+// The pieces of a group that is cut: piece 0 in range `first`, the others in `rest` and those behind it.
+struct Pieces {
+  int first, rest, count;
+};
+__device__ __forceinline__ Pieces pieces_of(const Cut& c, const Place& p) {
+  Pieces r;
+  r.first = range_of(c, p.start);
+  r.rest = max(range_of(c, p.start + kStartCost + p.cost), r.first + 1);
+  r.count = 1 + max(range_of(c, p.start + kStartCost + (p.units - 1) * p.cost) - r.rest + 1, 0);
+  return r;
+}
 
 // __any as the compiler knows it to be uniform: a branch on it stays a scalar one (around the other kind it keeps a second copy of every
 // register that the branch changes).
@@ -132,6 +186,14 @@ __device__ __forceinline__ qf16x8 operand_f16(uint32_t lo, uint32_t hi, float sc
   return __builtin_bit_cast(qf16x8, w);
 }
 
+__device__ __forceinline__ __attribute__((address_space(3))) raw4* lds_raw4(unsigned at) { return (__attribute__((address_space(3))) raw4*)at; }
+typedef uint32_t raw2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ __attribute__((address_space(3))) raw2* lds_raw2(unsigned at) { return (__attribute__((address_space(3))) raw2*)at; }
+__device__ __forceinline__ __attribute__((address_space(3))) float* lds_f32(unsigned at) { return (__attribute__((address_space(3))) float*)at; }
+// At most N loads of this wave on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
 // Which of the 16 tokens of a page a node sees, the page starting `past` tokens behind the context (negative: before its end).
 __device__ __forceinline__ uint32_t page_mask(unsigned long long lo, unsigned long long hi, int past) {
   if (past <= -16) return 0xffffu;
@@ -147,31 +209,55 @@ __device__ __forceinline__ uint32_t spread4(uint32_t bits) {
   return ((bits & 1u) * 0xffu) | ((bits >> 1 & 1u) * 0xff00u) | ((bits >> 2 & 1u) * 0xff0000u) | ((bits >> 3 & 1u) * 0xff000000u);
 }
 
-template <int D, int MAXB>
+template <int D_, int NW>
 struct QuantAttnShared {
+  static constexpr int D = D_, kWaves = NW, kThreads = NW * kWave;
   static constexpr int kStride = D + 4;                        // floats; padded row of the merge
+  static constexpr int kPageBytes = kQuantPage * D;            // of K, or V, of a head
+  static constexpr int kHalf = 2 * kPageBytes;                 // a unit's K, or V
+  union {
+    __align__(1024) unsigned char ring[NW][3][kHalf];          // K, K, V
+    __align__(16) float o[NW][16][kStride];                    // the merge of the waves, when the units are done with
+    struct {
+      float m[kMergeRoom], l[kMergeRoom];
+    } merge;                                                   // ... of the pieces
+  };
+  __align__(16) raw4 q[kQaBlocks * 2 * (D / 64)][kWave];       // query operands: [block, step][lane]
+  float scales[NW][kWave];                                     // of a unit's pages: lane i: page i / 2 % 2, K or V i % 2
   unsigned long long anc[kQaMaxNodes][2];
   int parent[kQaMaxNodes];
   int nans;                                                    // a draft's value is NaN
-  float m[kQaWaves][16 * MAXB], l[kQaWaves][16 * MAXB];
-  union {
-    __align__(16) float o[kQaWaves][16][kStride];              // the merge, when the queries are done with
-    __align__(16) raw4 q[kQaWaves * MAXB * 2 * (D / 64)][kWave];     // query operands: [block, step][lane]
-  };
+  int last;                                                    // this workgroup finished its request's last piece
+  int64_t row[16 * kQaBlocks];                                 // of q and out, of the piece's query rows
+  int node[16 * kQaBlocks];
+  float top[16 * kQaBlocks], sum[16 * kQaBlocks];              // a row's statistics
+  float m[NW][16 * kQaBlocks], l[NW][16 * kQaBlocks];
 };
 
-// One piece of a request: units [t0, t1) of it, for the query rows [row_base, row_base + rows) of a KV head, NB 16-row blocks per wave.
+// One piece of a request: units [t0, t1) of it, for the query rows [row_base, row_base + rows) of a KV head.
 struct QuantPiece {
   int b, first, n, ctx, kvh, t0, t1, row_base, rows;
-  bool whole;                 // the piece is the whole request: write the result
+  bool whole;                 // the piece is all of these rows: write the result
   int64_t part;               // else: first row of its partial result
+  unsigned long long* word;   // ... and the word that counts the pieces
 };
 
-// Dimensions d0 .. d0 + 3 of a row's result are NaN where a value is that the row sees, among the units that reach the drafts (of the others
+// The piece's query rows: their nodes, and where they lie in q and out (rows past the last repeat it).
+template <typename Sh>
+__device__ __forceinline__ void find_rows(const QuantAttnParams& P, Sh& S, const QuantPiece& J) {
+  const int i = threadIdx.x;
+  if (i >= 16 * kQaBlocks) return;
+  const int row = J.row_base + min(i, J.rows - 1), node = row / P.G;
+  S.node[i] = node;
+  S.row[i] = static_cast<int64_t>(J.first + node) * P.Hq + J.kvh * P.G + (row - node * P.G);
+}
+
+// Dimensions d0 and d0 + 1 of a row's result are NaN where a value is that the row sees, among the units that reach the drafts (of the others
 // every row sees every token, and the products are NaN by themselves).
-template <int D, typename Shared>
-__device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const Shared& S, const QuantPiece& J, int row, int d0, float4& o) {
-  const int node = (J.row_base + row) / P.G;
+template <typename Sh>
+__device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const Sh& S, const QuantPiece& J, int row, int d0, float& lo, float& hi) {
+  constexpr int D = Sh::D;
+  const int node = S.node[row];
   const int end = min(J.t1 * kUnit, J.ctx + J.n);
   for (int tok = max(J.t0 * kUnit, J.ctx & ~(kUnit - 1)); tok < end; ++tok) {
     const int j = tok - J.ctx, lp = tok / kQuantPage;
@@ -180,30 +266,169 @@ __device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const Sh
     if (id < 0 || id >= P.num_pages) continue;
     const unsigned char* v = P.v_pool + (static_cast<int64_t>(id) * P.Hkv + J.kvh) * (kQuantPage * D) + d0 * kQuantPage + tok % kQuantPage;
     const float nan = __builtin_nanf("");
-    if ((v[0] & 0x7f) == 0x7f) o.x = nan;
-    if ((v[kQuantPage] & 0x7f) == 0x7f) o.y = nan;
-    if ((v[2 * kQuantPage] & 0x7f) == 0x7f) o.z = nan;
-    if ((v[3 * kQuantPage] & 0x7f) == 0x7f) o.w = nan;
+    if ((v[0] & 0x7f) == 0x7f) lo = nan;
+    if ((v[kQuantPage] & 0x7f) == 0x7f) hi = nan;
+  }
+}
+
+__device__ __forceinline__ unsigned long long pair_bits(float lo, float hi) {
+  return static_cast<unsigned long long>(__float_as_uint(hi)) << 32 | __float_as_uint(lo);
+}
+
+// Dimensions 2 d2 and 2 d2 + 1 of a row's result from their sums and the row's statistics.
+template <int D>
+__device__ __forceinline__ void put_result(const QuantAttnParams& P, int64_t at, int d2, float lo, float hi, float M, float Z) {
+  const float inv = Z == 0.f ? 0.f : 1.f / Z;                   // a row that sees nothing gives 0 (and -infinity)
+  if (P.out_f32) {
+    reinterpret_cast<float2*>(static_cast<float*>(P.out) + at * D)[d2] = make_float2(lo * inv, hi * inv);
+  } else {
+    const qbf16x2 a = {static_cast<__bf16>(lo * inv), static_cast<__bf16>(hi * inv)};
+    reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(P.out) + at * D)[d2] = __builtin_bit_cast(uint32_t, a);
+  }
+  if (P.lse && d2 == 0) P.lse[at] = (M + log2f(Z)) * static_cast<float>(kLn2);
+}
+
+// The pieces of a request count themselves in a word {count : the call's tag}.  What an earlier call left there is first replaced by a count
+// of none: one attempt, since only another piece of this call can have been quicker.  (Counting by compare-and-swap alone, pieces that finish
+// together wait for each other, 1.2 us apiece.)  Thread 0; seen: the word as it was before.
+__device__ __forceinline__ void open_count(unsigned long long* word, unsigned long long seen, unsigned long long tag) {
+  if (!have_tag<1>(&seen, tag))
+    __hip_atomic_compare_exchange_strong(word, &seen, tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Counts this workgroup's piece as done; true in all threads of the workgroup that finishes the last of `pieces`.
+__device__ __forceinline__ bool last_piece(unsigned long long* word, int pieces, int* last) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // this wave's partial results have arrived
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const unsigned long long before = __hip_atomic_fetch_add(word, 1ull << kTagBits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *last = static_cast<int>(before >> kTagBits) + 1 == pieces;
+  }
+  __syncthreads();
+  return *last != 0;
+}
+
+// Merges the partial results of a request's pieces, in their order; `pair`: the KV head's first range.
+template <typename Sh>
+__device__ __forceinline__ void merge_pieces(const QuantAttnParams& P, Sh& S, const QuantPiece& J, int64_t pair, const Pieces& all) {
+  constexpr int D = Sh::D, kFly = 8, kThreads = Sh::kThreads;
+  const int tid = threadIdx.x;
+  const int pieces = all.count;
+  auto part = [&](int i) { return ((pair + (i == 0 ? all.first : all.rest + i - 1)) * 2 + (i == 0 ? 1 : 0)) * P.rows; };
+  const int chunk = min(J.rows, max(1, kMergeRoom / pieces));
+  for (int r0 = 0; r0 < J.rows; r0 += chunk) {
+    const int rows = min(chunk, J.rows - r0);
+    __syncthreads();
+    for (int at = tid; at < rows * pieces; at += kThreads) {
+      const unsigned long long w = ld_dev(reinterpret_cast<const unsigned long long*>(P.ws_ml + part(at / rows) + r0 + at % rows));
+      S.merge.m[at] = __uint_as_float(static_cast<unsigned>(w));
+      S.merge.l[at] = __uint_as_float(static_cast<unsigned>(w >> 32));
+    }
+    __syncthreads();
+    for (int r = tid; r < rows; r += kThreads) {
+      float M = -INFINITY, Z = 0.f;
+      for (int i = 0; i < pieces; ++i) M = fmaxf(M, S.merge.m[i * rows + r]);
+      for (int i = 0; i < pieces; ++i) {
+        const float m = S.merge.m[i * rows + r];
+        const float f = m == -INFINITY ? 0.f : fast_exp2(m - M);
+        Z += m == -INFINITY ? 0.f : S.merge.l[i * rows + r] * f;
+        S.merge.m[i * rows + r] = f;
+      }
+      S.top[r] = M;
+      S.sum[r] = Z;
+    }
+    __syncthreads();
+    for (int at = tid; at < rows * (D / 2); at += kThreads) {
+      const int r = at / (D / 2), d2 = at % (D / 2);
+      float lo = 0.f, hi = 0.f;
+      for (int i0 = 0; i0 < pieces; i0 += kFly) {
+        unsigned long long x[kFly];
+#pragma unroll
+        for (int k = 0; k < kFly; ++k)
+          x[k] = ld_dev(reinterpret_cast<const unsigned long long*>(P.ws_o + (part(min(i0 + k, pieces - 1)) + r0 + r) * D) + d2);
+#pragma unroll
+        for (int k = 0; k < kFly; ++k) {
+          if (i0 + k >= pieces) break;
+          const float f = S.merge.m[(i0 + k) * rows + r];
+          lo += __uint_as_float(static_cast<unsigned>(x[k])) * f;
+          hi += __uint_as_float(static_cast<unsigned>(x[k] >> 32)) * f;
+        }
+      }
+      put_result<D>(P, S.row[r0 + r], d2, lo, hi, S.top[r], S.sum[r]);
+    }
   }
 }
 
 // SANITIZE: NaN among the drafts' values are taken out of the products (where a row does not see a draft its weight is zero, and zero times
 // NaN would be NaN) and put back into the results of the rows that see them.  Without, a piece that meets one writes nothing and
 // says so in S.nans.
-template <int D, int NB, int TERMS, bool SANITIZE, typename Shared>
-__device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S, const QuantPiece& J) {
+template <int NB, int TERMS, bool SANITIZE, typename Sh>
+__device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, const QuantPiece& J) {
+  constexpr int D = Sh::D, kWaves = Sh::kWaves;
   constexpr int kH = D / 64;                                   // K: 16-byte chunks of a lane per token
   constexpr int kDT = D / 16;                                  // 16-dimension tiles of the output
-  const int tid = threadIdx.x, lane = tid & 63;
+  constexpr int kLoads = D / 64;                               // 1 KB loads per page of K or V
+  const int tid = static_cast<int>(threadIdx.x) + opaque_zero(), lane = tid & 63;
+  __builtin_assume(tid >= 0 && tid < Sh::kThreads);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rn = lane & 15, g = lane >> 4;                     // query row of the block (matrix column), lane group
   const int L = J.ctx + J.n;
-  const int total_blocks = (J.rows + 15) / 16;
-  const int kinds = (total_blocks + NB - 1) / NB > 2 ? 4 : (total_blocks + NB - 1) / NB;   // groups of waves with rows of their own: 1, 2 or 4
-  const int slices = kQaWaves / kinds, kind = wave % kinds, slice = wave / kinds;
   const bool touches_drafts = J.t1 * kUnit > J.ctx;
 
+  const unsigned long long count_seen = SANITIZE || J.whole || tid > 0 ? 0ull : ld_dev(J.word);
   __syncthreads();                                              // the LDS of the piece before is free
+
+  // ---- a unit's loads: page ids through the scalar cache, a page of a head is contiguous; lane i brings bytes 16 i .. + 16 of each 1 KB ----
+  const int64_t page_bytes = static_cast<int64_t>(P.Hkv) * Sh::kPageBytes;
+  const unsigned char* k_head = P.k_pool + static_cast<int64_t>(J.kvh) * Sh::kPageBytes;
+  const unsigned char* v_head = P.v_pool + static_cast<int64_t>(J.kvh) * Sh::kPageBytes;
+  const const_i32* bt = (const const_i32*)(P.block_table + static_cast<int64_t>(J.b) * P.max_pages);
+  const int last_page = min((L - 1) / kQuantPage, P.max_pages - 1);
+  int k_id0 = 0, k_id1 = 0, v_id0 = 0, v_id1 = 0;               // of the units whose K and V go out next; -1: no page of the pool
+  auto fetch_ids = [&](int t) __attribute__((always_inline)) {
+    if (t < J.t1) {
+      k_id0 = bt[min(2 * t, last_page)];
+      k_id1 = bt[min(2 * t + 1, last_page)];
+      k_id0 = k_id0 >= 0 && k_id0 < P.num_pages && 2 * t < P.max_pages ? k_id0 : -1;
+      k_id1 = k_id1 >= 0 && k_id1 < P.num_pages && 2 * t + 1 < P.max_pages ? k_id1 : -1;
+    }
+  };
+  const unsigned ring = lds_address(&S.ring[wave][0][0]), scales = lds_address(reinterpret_cast<unsigned char*>(&S.scales[wave][0]));
+  auto issue_k = [&](unsigned to) __attribute__((always_inline)) {
+    const unsigned char* a = k_head + max(k_id0, 0) * page_bytes;
+    const unsigned char* b = k_head + max(k_id1, 0) * page_bytes;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(a, 16 * lane, to, j);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(b, 16 * (lane ^ 4), to + Sh::kPageBytes, j);   // (see k_at)
+  };
+  auto issue_v = [&] __attribute__((always_inline)) {
+    const unsigned char* a = v_head + max(v_id0, 0) * page_bytes;
+    const unsigned char* b = v_head + max(v_id1, 0) * page_bytes;
+    // a page that is none of the pool's holds nothing: its scale reads as 0, what is read instead is page 0
+    const int id = lane & 2 ? v_id1 : v_id0;
+    const float* at = (lane & 1 ? P.v_scale : P.k_scale) + static_cast<int64_t>(id) * P.Hkv + J.kvh;
+    at = id >= 0 ? at : kNoScale;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(a, 16 * lane, ring + 2 * Sh::kHalf, j);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_to_lds(b, 16 * lane, ring + 2 * Sh::kHalf + Sh::kPageBytes, j);
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" :: "{m0}"(scales), "v"(at) : "memory");
+  };
+  constexpr int kKLoads = 2 * kLoads, kVLoads = 2 * kLoads + 1;
+
+  int t = J.t0 + wave;
+  const int mine = t < J.t1 ? (J.t1 - t + kWaves - 1) / kWaves : 0;      // units of this wave
+  if (mine > 0) {
+    fetch_ids(t);
+    issue_k(ring);
+    v_id0 = k_id0; v_id1 = k_id1;
+    fetch_ids(t + kWaves);
+    if (mine > 1) issue_k(ring + Sh::kHalf);
+    issue_v();
+    v_id0 = k_id0; v_id1 = k_id1;
+    fetch_ids(t + 2 * kWaves);
+  }
+
   if (!SANITIZE && tid == 0) S.nans = 0;
   if (touches_drafts) {
     if (P.parent && tid < J.n) S.parent[tid] = P.parent[J.first + tid];
@@ -226,44 +451,22 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
       S.anc[tid][0] = w[0];
       S.anc[tid][1] = w[1];
     }
-    __syncthreads();
   }
+  // ---- query operands, to LDS: step 2 h + e, lane group g: dimensions 16 (4 h + g) + 8 e .. + 8 (what a lane's 16 bytes of K hold) ----
+  for (int f = wave; f < NB * 2 * kH; f += kWaves) {
+    const int s = f % (2 * kH), row = J.row_base + min(16 * (f / (2 * kH)) + rn, J.rows - 1);    // (columns past the last row repeat it)
+    const uint16_t* qp = P.q + (static_cast<int64_t>(J.first + row / P.G) * P.Hq + J.kvh * P.G + row % P.G) * D + 16 * g;
+    S.q[f][lane] = *reinterpret_cast<const raw4*>(qp + 64 * (s >> 1) + 8 * (s & 1));
+  }
+  find_rows(P, S, J);
+  __syncthreads();
 
-  auto node_of = [&](int qi) __attribute__((always_inline)) { return (J.row_base + min(16 * (kind * NB + qi) + rn, J.rows - 1)) / P.G; };
-  const int64_t page_bytes = static_cast<int64_t>(P.Hkv) * kQuantPage * D;
-  const unsigned char* k_lane = P.k_pool + static_cast<int64_t>(J.kvh) * kQuantPage * D + g * 256 + (8 * ((rn >> 2) & 1) + (rn & 3)) * 16;
-  const unsigned char* v_lane = P.v_pool + static_cast<int64_t>(J.kvh) * kQuantPage * D + rn * 16 + 8 * (g & 1);
-  const int32_t* bt = P.block_table + static_cast<int64_t>(J.b) * P.max_pages;
-  const int last_page = min((L - 1) / kQuantPage, P.max_pages - 1);
-
-  int id_k, id_v;                                               // of the unit whose loads go out next; lane: page rn / 8 of K, page g / 2 of V
-  auto fetch_ids = [&](int t) __attribute__((always_inline)) {
-    id_k = bt[min(2 * t + (rn >> 3), last_page)];
-    id_v = bt[min(2 * t + (g >> 1), last_page)];
-  };
-  raw4 kr[kH][2];
-  uint2 vr[kDT];
-  float ks, vs;
-  bool page_ok;
-  // a page that is none of the pool's holds nothing: its tokens are masked, what is read instead is page 0
-  auto usable = [&](int id) __attribute__((always_inline)) { return id >= 0 && id < P.num_pages; };
-  auto issue_k = [&] __attribute__((always_inline)) {
-    const unsigned char* at = k_lane + (usable(id_k) ? id_k : 0) * page_bytes;
-#pragma unroll
-    for (int h = 0; h < kH; ++h)
-#pragma unroll
-      for (int st = 0; st < 2; ++st) kr[h][st] = *reinterpret_cast<const raw4*>(at + 1024 * h + 64 * st);
-  };
-  auto issue_v = [&](int t) __attribute__((always_inline)) {
-    const bool ok = usable(id_v);
-    const int id = ok ? id_v : 0;
-    const unsigned char* at = v_lane + id * page_bytes;
-#pragma unroll
-    for (int d = 0; d < kDT; ++d) vr[d] = *reinterpret_cast<const uint2*>(at + 256 * d);
-    ks = P.k_scale[static_cast<int64_t>(id) * P.Hkv + J.kvh];
-    vs = P.v_scale[static_cast<int64_t>(id) * P.Hkv + J.kvh];
-    page_ok = ok && 2 * t + (g >> 1) < P.max_pages;
-  };
+  // Operand reads.  K, lane group g: chunk 4 h + g; lane: page rn / 8, token 8 (rn / 4 % 2) + 4 st + rn % 4.  The second page lies with tokens
+  // 4 i .. + 3 and their neighbours 4 (i ^ 1) .. exchanged: 16 lanes take their 256 bytes from as many banks.
+  const unsigned k_at = ring + (rn >> 3) * Sh::kPageBytes + g * 256 + (8 * ((rn >> 2) & 1) + (rn & 3)) * 16;
+  const unsigned k_flip = 64 * (rn >> 3);                       // sub-tile st at k_at + (64 st ^ k_flip)
+  const unsigned v_at = ring + 2 * Sh::kHalf + (g >> 1) * Sh::kPageBytes + rn * 16 + 8 * (g & 1);
+  const unsigned s_at = scales + 8 * (g >> 1);
 
   // ref: what a row's weights are relative to, in log2 units; sum: of this lane's tokens; v_ref: what the results are relative to
   float ref[NB], sum[NB], v_ref = __uint_as_float(static_cast<uint32_t>(kLeastScaleExp + 127) << 23);
@@ -276,28 +479,59 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
     for (int d = 0; d < kDT; ++d) oacc[qi][d] = qf32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // One unit.  MORE: the next unit's loads go out on the way.
-  auto unit = [&](int t, int next, auto more_tag) __attribute__((always_inline)) {
-    constexpr bool MORE = decltype(more_tag)::value;
-    // ---- scores ----
+  for (int i = 0; i < mine; ++i, t += kWaves) {
+    const unsigned at = (i & 1) * Sh::kHalf;
+    const int behind = mine - 1 - i;                            // units of this wave after this one
+    // K of this unit is here: behind it the next one's K, and V
+    if (behind > 0) wait_loads<kKLoads + kVLoads>();
+    else wait_loads<kVLoads>();
+    // ---- scores: K at once, the queries' operands a step ahead of the products (four blocks: of the first two, registers are short) ----
+    constexpr int kAhead = NB < 4 ? NB : 2;
     qf32x4 s[NB][2];
+    raw4 kr[kH][2], qr[2][NB];
 #pragma unroll
-    for (int h = 0; h < kH; ++h)
+    for (int h = 0; h < kH; ++h) {
+      kr[h][0] = *lds_raw4(k_at + at + (0u ^ k_flip) + 1024 * h);
+      kr[h][1] = *lds_raw4(k_at + at + (64u ^ k_flip) + 1024 * h);
+    }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const qbf16x8 a0 = operand_bf16(kr[h][0][2 * e], kr[h][0][2 * e + 1]), a1 = operand_bf16(kr[h][1][2 * e], kr[h][1][2 * e + 1]);
+    for (int qi = 0; qi < kAhead; ++qi) qr[0][qi] = S.q[qi * 2 * kH][lane];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K has been read
+    if (behind > 1) issue_k(ring + at);
 #pragma unroll
-        for (int qi = 0; qi < NB; ++qi) {
-          const qbf16x8 q = __builtin_bit_cast(qbf16x8, S.q[(kind * NB + qi) * 2 * kH + 2 * h + e][lane]);
-          const qf32x4 zero = {0.f, 0.f, 0.f, 0.f};
-          s[qi][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, q, h + e == 0 ? zero : s[qi][0], 0, 0, 0);
-          s[qi][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, q, h + e == 0 ? zero : s[qi][1], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+    for (int step = 0; step < 2 * kH; ++step) {
+      const int h = step >> 1, e = step & 1;
+      if (step + 1 < 2 * kH) {
+#pragma unroll
+        for (int qi = 0; qi < kAhead; ++qi) qr[(step + 1) & 1][qi] = S.q[qi * 2 * kH + step + 1][lane];
       }
-    const bool ok = page_ok;
-    const float factor = ks * P.c, v_own = ok ? vs : 0.f;
-    if constexpr (MORE) issue_k();
+#pragma unroll
+      for (int qi = kAhead; qi < NB; ++qi) qr[step & 1][qi] = S.q[qi * 2 * kH + step][lane];
+      const qbf16x8 a0 = operand_bf16(kr[h][0][2 * e], kr[h][0][2 * e + 1]), a1 = operand_bf16(kr[h][1][2 * e], kr[h][1][2 * e + 1]);
+#pragma unroll
+      for (int qi = 0; qi < NB; ++qi) {
+        const qbf16x8 q = __builtin_bit_cast(qbf16x8, qr[step & 1][qi]);
+        const qf32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        s[qi][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, q, step == 0 ? zero : s[qi][0], 0, 0, 0);
+        s[qi][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, q, step == 0 ? zero : s[qi][1], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // V of this unit and its scales are here: behind them the K after next
+    if (behind > 1) wait_loads<kKLoads>();
+    else wait_loads<0>();
+    const float ks = *lds_f32(s_at), v_own = *lds_f32(s_at + 4);
+    raw2 vr[kDT];
+#pragma unroll
+    for (int d = 0; d < kDT; ++d) vr[d] = *lds_raw2(v_at + 256 * d);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V has been read
+    if (behind > 0) {
+      issue_v();
+      v_id0 = k_id0; v_id1 = k_id1;
+      fetch_ids(t + 3 * kWaves);
+    }
+    const bool ok = ks != 0.f;
+    const float factor = ok ? ks * P.c : 1.f;                   // (not 0: masked scores are -infinity)
 
     // ---- masks: only where the unit reaches the drafts, or a page is none ----
     const int past = t * kUnit + 16 * (g >> 1) - J.ctx;         // the lane's page starts that far behind the context
@@ -307,7 +541,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
       for (int qi = 0; qi < NB; ++qi) {
         uint32_t seen = 0xffffu;
         if (past > -16) {
-          const int node = node_of(qi);
+          const int node = S.node[16 * qi + rn];
           seen = page_mask(S.anc[node][0], S.anc[node][1], past);
         }
         seen = ok ? seen >> (8 * (g & 1)) : 0u;
@@ -324,7 +558,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
 #pragma unroll
     for (int qi = 0; qi < NB; ++qi) {
       top[qi] = fmaxf(fmaxf(fmaxf(s[qi][0][0], s[qi][0][1]), fmaxf(s[qi][0][2], s[qi][0][3])),
-                      fmaxf(fmaxf(s[qi][1][0], s[qi][1][1]), fmaxf(s[qi][1][2], s[qi][1][3]))) * factor;    // factor > 0
+                      fmaxf(fmaxf(s[qi][1][0], s[qi][1][1]), fmaxf(s[qi][1][2], s[qi][1][3]))) * factor;    // factor >= 0
       ahead |= top[qi] > ref[qi] + kSlack;
     }
     if (any_lane(ahead)) {
@@ -349,7 +583,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
     // fp16 has room for it.
     asm volatile("" : "+v"(v_ref));      // (its inverse worked out on both sides of the branch makes it one with an else part, whose copies cost the
                                          // registers of all results a second time)
-    const float ratio = vs * inverse_scale(v_ref), v_by = fmaxf(ratio, kLeastV), p_by = ratio * inverse_scale(v_by);
+    const float ratio = v_own * inverse_scale(v_ref), v_by = fmaxf(ratio, kLeastV), p_by = ok ? ratio * inverse_scale(v_by) : 1.f;
     const float shift = static_cast<float>(static_cast<int>(__float_as_uint(p_by) >> 23) - 127 + kWeightBias);
     const float unshift = inverse_scale(p_by);
     raw4 hi[NB], lo[TERMS == 2 ? NB : 1];
@@ -378,16 +612,14 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
     uint32_t keep[2] = {~0u, ~0u};
     if (masked) {
       const int valid = ok ? min(max(L - t * kUnit - 8 * g, 0), 8) : 0;
-      uint32_t nans = 0u;
+      keep[0] = spread4((1u << valid) - 1u);
+      keep[1] = spread4(((1u << valid) - 1u) >> 4);
+      if (!SANITIZE && drafts) {
+        uint32_t nans = 0u;
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        keep[w] = spread4(((1u << valid) - 1u) >> (4 * w));
-        if constexpr (!SANITIZE) {
-#pragma unroll
-          for (int d = 0; d < kDT; ++d) nans |= nan_bytes((w ? vr[d].y : vr[d].x) & keep[w]);
-        }
+        for (int d = 0; d < kDT; ++d) nans |= nan_bytes(vr[d].x & keep[0]) | nan_bytes(vr[d].y & keep[1]);
+        if (any_lane(nans != 0u) && lane == 0) S.nans = 1;
       }
-      if (!SANITIZE && drafts && any_lane(nans != 0u) && lane == 0) S.nans = 1;
     }
 #pragma unroll
     for (int d = 0; d < kDT; ++d) {
@@ -407,33 +639,11 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (MORE) {
-      issue_v(next);
-      fetch_ids(min(next + slices, J.t1 - 1));
-    }
-  };
-
-  int t = J.t0 + slice;
-  if (t < J.t1) {
-    fetch_ids(t);
-    issue_k();
-    issue_v(t);
-    fetch_ids(min(t + slices, J.t1 - 1));
-  }
-  // ---- query operands, to LDS: step 2 h + e, lane group g: dimensions 16 (4 h + g) + 8 e .. + 8 (what a lane's 16 bytes of K hold) ----
-  for (int f = wave; f < total_blocks * 2 * kH; f += kQaWaves) {
-    const int s = f % (2 * kH), row = J.row_base + min(16 * (f / (2 * kH)) + rn, J.rows - 1);    // (columns past the last row repeat it)
-    const uint16_t* qp = P.q + (static_cast<int64_t>(J.first + row / P.G) * P.Hq + J.kvh * P.G + row % P.G) * D + 16 * g;
-    S.q[f][lane] = *reinterpret_cast<const raw4*>(qp + 64 * (s >> 1) + 8 * (s & 1));
-  }
-  __syncthreads();
-
-  if (t < J.t1) {
-    for (; t + slices < J.t1; t += slices) unit(t, t + slices, std::true_type{});
-    unit(t, t, std::false_type{});
   }
 
-  // ---- merge the waves that share rows, one block of each wave at a time ----
+  if (!SANITIZE && !J.whole && tid == 0) open_count(J.word, count_seen, P.tag);
+
+  // ---- merge the waves, one block at a time ----
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
     sum[qi] = groups_sum(sum[qi]) * (1.f / (1 << kWeightBias));
@@ -443,178 +653,131 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Shared& S,
       S.l[wave][16 * qi + lane] = sum[qi];
     }
   }
+  __syncthreads();                                              // (the rings are done with, too)
   if constexpr (!SANITIZE) {
-    if (touches_drafts) {
-      __syncthreads();
-      if (S.nans) return;
-    }
+    if (S.nans) return;
+  }
+  if (tid < 16 * NB) {
+    float M = -INFINITY, Z = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, S.m[w][tid]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) Z += S.m[w][tid] == -INFINITY ? 0.f : S.l[w][tid] * fast_exp2(S.m[w][tid] - M);
+    S.top[tid] = M;
+    S.sum[tid] = Z;
   }
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
-    __syncthreads();
+    if (qi > 0) __syncthreads();
     float top = -INFINITY;
-    for (int s = 0; s < slices; ++s) top = fmaxf(top, S.m[kind + kinds * s][16 * qi + rn]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, S.m[w][16 * qi + rn]);
     const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - top - static_cast<float>(kWeightBias)) * v_ref;
 #pragma unroll
     for (int d = 0; d < kDT; ++d)
       *reinterpret_cast<float4*>(&S.o[wave][rn][16 * d + 4 * g]) =
           make_float4(oacc[qi][d][0] * f, oacc[qi][d][1] * f, oacc[qi][d][2] * f, oacc[qi][d][3] * f);
     __syncthreads();
-    constexpr int kQuads = D / 4;
-    for (int at = tid; at < kinds * 16 * kQuads; at += kQaThreads) {
-      const int d4 = at % kQuads, r = at / kQuads % 16, k = at / (16 * kQuads);
-      const int row = 16 * (k * NB + qi) + r;
+    for (int at = tid; at < 16 * (D / 2); at += Sh::kThreads) {
+      const int d2 = at % (D / 2), r = at / (D / 2), row = 16 * qi + r;
       if (row >= J.rows) continue;
-      float M = -INFINITY, Z = 0.f;
-      for (int s = 0; s < slices; ++s) M = fmaxf(M, S.m[k + kinds * s][16 * qi + r]);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int s = 0; s < slices; ++s) {
-        const int w = k + kinds * s;
-        const float mw = S.m[w][16 * qi + r];
-        if (mw != -INFINITY) Z += S.l[w][16 * qi + r] * fast_exp2(mw - M);
-        const float4 x = *reinterpret_cast<const float4*>(&S.o[w][r][4 * d4]);
-        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+      float lo = 0.f, hi = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 x = *reinterpret_cast<const float2*>(&S.o[w][r][2 * d2]);
+        lo += x.x; hi += x.y;
       }
-      if constexpr (SANITIZE) put_back_nans<D>(P, S, J, row, 4 * d4, o);
+      if constexpr (SANITIZE) put_back_nans(P, S, J, row, 2 * d2, lo, hi);
       if (J.whole) {
-        const int ra = J.row_base + row;
-        const int64_t at_row = static_cast<int64_t>(J.first + ra / P.G) * P.Hq + J.kvh * P.G + ra % P.G;
-        const float inv = Z == 0.f ? 0.f : 1.f / Z;             // a row that sees nothing gives 0 (and -inf)
-        if (P.out_f32) {
-          *reinterpret_cast<float4*>(static_cast<float*>(P.out) + at_row * D + 4 * d4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        } else {
-          const qbf16x2 a = {static_cast<__bf16>(o.x * inv), static_cast<__bf16>(o.y * inv)};
-          const qbf16x2 c = {static_cast<__bf16>(o.z * inv), static_cast<__bf16>(o.w * inv)};
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + at_row * D + 4 * d4) =
-              make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
-        }
-        if (P.lse && d4 == 0) P.lse[at_row] = (M + log2f(Z)) * static_cast<float>(kLn2);
+        put_result<D>(P, S.row[row], d2, lo, hi, S.top[row], S.sum[row]);
       } else {
-        *reinterpret_cast<float4*>(P.ws_o + (J.part + row) * D + 4 * d4) = o;
-        if (d4 == 0) P.ws_ml[J.part + row] = make_float2(M, Z);
+        // read by another workgroup of this launch: device-scope stores
+        st_dev(reinterpret_cast<unsigned long long*>(P.ws_o + (J.part + row) * D) + d2, pair_bits(lo, hi));
+        if (d2 == 0) st_dev(reinterpret_cast<unsigned long long*>(P.ws_ml + J.part + row), pair_bits(S.top[row], S.sum[row]));
       }
     }
   }
 }
 
-// MAXB: most 16-row blocks a wave multiplies a unit with; TERMS: fp16 terms of a weight.
-template <int D, int MAXB, int TERMS>
-__global__ __launch_bounds__(kQaThreads, 2) void attn_quant_kernel(QuantAttnParams P) {
-  __shared__ QuantAttnShared<D, MAXB> S;
+// TERMS: fp16 terms of a weight.
+template <int D, int TERMS, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnParams P) {
+  constexpr int kMost = most_blocks(D, TERMS);
+  extern __shared__ __align__(1024) unsigned char smem[];
+  auto& S = *reinterpret_cast<QuantAttnShared<D, NW>*>(smem);
   const int lane = threadIdx.x & 63;
-  const int range = blockIdx.x;
+  // Workgroups go to the 8 XCDs in turn: renumbered so that neighbouring ranges, which may hold groups of rows of one request, share an L2
+  const unsigned id = blockIdx.x, all = gridDim.x;
+  const unsigned logical = all % 8 == 0 ? (id & 7) * (all / 8) + (id >> 3) : id;
+  const int range = logical % P.ranges;
   QuantPiece J;
-  J.kvh = blockIdx.y;
-  J.row_base = 16 * P.blocks * blockIdx.z;
-  const int64_t pair = (static_cast<int64_t>(blockIdx.y) * gridDim.z + blockIdx.z) * P.ranges + range;
+  J.kvh = logical / P.ranges;
+  const int64_t pair = static_cast<int64_t>(J.kvh) * P.ranges;
   const int batches = (P.B + 63) / 64;
-  int64_t units = 0;
+  int total = 0, count = 0;
   Requests r;
   for (int k = batches - 1; k >= 0; --k) {                      // (down: the first 64 requests stay in registers)
-    r = load_requests(P, k, lane);
-    units += r.sum;
+    r = load_requests(P, k, kMost, lane);
+    total += r.sum;
+    count += r.count;
   }
-  const int used = used_ranges(P, units);
-  if (range >= used) return;
-  int64_t at = units * range / used;
-  const int64_t end = units * (range + 1) / used;
-  int64_t base = 0;                                             // units before these 64 requests
-  for (int k = 0; at < end; ) {
-    const unsigned long long later = __ballot(base + r.upto > at);
+  const Cut cut = cut_ranges(P, total, count);
+  if (range >= cut.used) return;
+  const int from = range_start(cut, range), end = range_start(cut, range + 1);
+  int base = 0;                                                 // cost before these 64 requests
+  for (int k = 0, at = from; at < end;) {
+    const unsigned long long later = __builtin_amdgcn_ballot_w64(base + r.upto > at);
     if (later == 0ull) {
       base += r.sum;
       if (++k >= batches) break;
-      r = load_requests(P, k, lane);
+      r = load_requests(P, k, kMost, lane);
       continue;
     }
     const int i = __ffsll(later) - 1;
-    const int u = __builtin_amdgcn_readlane(r.units, i);
-    const int64_t start = base + __builtin_amdgcn_readlane(r.upto, i) - u;
-    const int64_t stop = min(end, start + u);
+    const int groups = __builtin_amdgcn_readlane(r.groups, i), per = __builtin_amdgcn_readlane(r.per, i);
+    Place p;
+    p.units = __builtin_amdgcn_readlane(r.units, i);
+    p.cost = unit_cost(per);
+    const int behind = base + __builtin_amdgcn_readlane(r.upto, i), group_cost = kStartCost + p.units * p.cost;
+    p.start = behind - groups * group_cost;
     J.b = 64 * k + i;
     J.ctx = __builtin_amdgcn_readlane(r.ctx, i);
     J.first = __builtin_amdgcn_readlane(r.first, i);
     J.n = __builtin_amdgcn_readlane(r.n, i);
-    J.t0 = static_cast<int>(at - start);
-    J.t1 = static_cast<int>(stop - start);
-    J.rows = min(J.n * P.G - J.row_base, 16 * P.blocks);
-    J.whole = at == start && stop == start + u;
-    J.part = (pair * 2 + (at == start ? 1 : 0)) * (16 * P.blocks);
-    at = stop;
-    if (J.rows <= 0) continue;
-    const int blocks = (J.rows + 15) / 16;
-    const int kinds = blocks <= MAXB ? 1 : (blocks <= 2 * MAXB ? 2 : 4);
-    const int per_wave = (blocks + kinds - 1) / kinds;
-    [&] {
-      if constexpr (MAXB >= 3) {
-        if (per_wave == 3) return quant_piece<D, 3, TERMS, false>(P, S, J);
+    for (int grp = 0; grp < groups && p.start < end; ++grp, p.start += group_cost) {
+      J.t0 = first_unit(p, from);
+      J.t1 = min(p.units, first_unit(p, end));
+      if (J.t0 >= J.t1) continue;
+      J.row_base = 16 * per * grp;
+      J.rows = min(J.n * P.G - J.row_base, 16 * per);
+      J.whole = J.t0 == 0 && J.t1 == p.units;
+      J.part = ((pair + range) * 2 + (J.t0 == 0 ? 1 : 0)) * P.rows;
+      J.word = P.arrived + (static_cast<int64_t>(J.kvh) * P.groups + grp) * P.B + J.b;
+      switch (per) {
+        case 1: quant_piece<1, TERMS, false>(P, S, J); break;
+        case 2: quant_piece<2, TERMS, false>(P, S, J); break;
+        case 3: quant_piece<3, TERMS, false>(P, S, J); break;
+        default:
+          if constexpr (kMost >= 4) quant_piece<4, TERMS, false>(P, S, J);
       }
-      if constexpr (MAXB >= 2) {
-        if (per_wave == 2) return quant_piece<D, 2, TERMS, false>(P, S, J);
+      if (S.nans) {                                             // (written before a barrier, and next behind one)
+        QuantPiece part = J;
+        for (int row = 0; row < J.rows; row += 16) {
+          part.row_base = J.row_base + row;
+          part.rows = min(J.rows - row, 16);
+          part.part = J.part + row;
+          quant_piece<1, TERMS, true>(P, S, part);
+        }
+        __syncthreads();
+        find_rows(P, S, J);                                     // (of all rows again, for the merge)
       }
-      quant_piece<D, 1, TERMS, false>(P, S, J);
-    }();
-    if (S.nans) {                                               // (written before a barrier, and next behind one)
-      QuantPiece part = J;
-      for (int from = 0; from < J.rows; from += 64) {
-        part.row_base = J.row_base + from;
-        part.rows = min(J.rows - from, 64);
-        part.part = J.part + from;
-        quant_piece<D, 1, TERMS, true>(P, S, part);
+      if (!J.whole) {
+        const Pieces all_pieces = pieces_of(cut, p);
+        if (last_piece(J.word, all_pieces.count, &S.last)) merge_pieces(P, S, J, pair, all_pieces);
       }
     }
+    at = behind;
   }
-}
-
-// Requests whose units lie in more than one range: one row per D / 4 lanes, its partial results one after the other.
-template <int D>
-__global__ __launch_bounds__(256) void attn_quant_combine_kernel(QuantAttnParams P, int groups) {
-  constexpr int kQuads = D / 4, kRows = 256 / kQuads;
-  const int b = blockIdx.x, kvh = blockIdx.y, lane = threadIdx.x & 63;
-  int64_t units = 0, start = 0;
-  int u = 0, first = 0, n = 0;
-  for (int k = (P.B + 63) / 64 - 1; k >= 0; --k) {
-    const Requests r = load_requests(P, k, lane);
-    units += r.sum;
-    if (64 * k + 63 < b) start += r.sum;
-    if (k == b >> 6) {
-      u = __builtin_amdgcn_readlane(r.units, b & 63);
-      start += __builtin_amdgcn_readlane(r.upto, b & 63) - u;
-      first = __builtin_amdgcn_readlane(r.first, b & 63);
-      n = __builtin_amdgcn_readlane(r.n, b & 63);
-    }
-  }
-  if (u == 0) return;
-  const int used = used_ranges(P, units);
-  const int s0 = range_of(start, units, used), s1 = range_of(start + u - 1, units, used);
-  if (s0 == s1) return;
-  const int row = blockIdx.z * kRows + threadIdx.x / kQuads, d4 = threadIdx.x % kQuads;
-  if (row >= n * P.G) return;
-  const int per_group = 16 * P.blocks, grp = row / per_group;
-  const int64_t pair = (static_cast<int64_t>(kvh) * groups + grp) * P.ranges;
-  auto part = [&](int s) { return ((pair + s) * 2 + (s == s0 ? 1 : 0)) * per_group + row % per_group; };
-  float M = -INFINITY;
-  for (int s = s0; s <= s1; ++s) M = fmaxf(M, P.ws_ml[part(s)].x);
-  float Z = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = s0; s <= s1; ++s) {
-    const float2 ml = P.ws_ml[part(s)];
-    const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - M);
-    const float4 x = *reinterpret_cast<const float4*>(P.ws_o + part(s) * D + 4 * d4);
-    Z += ml.y * f;
-    o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
-  }
-  const int64_t at_row = static_cast<int64_t>(first + row / P.G) * P.Hq + kvh * P.G + row % P.G;
-  const float inv = Z == 0.f ? 0.f : 1.f / Z;
-  if (P.out_f32) {
-    *reinterpret_cast<float4*>(static_cast<float*>(P.out) + at_row * D + 4 * d4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  } else {
-    const qbf16x2 a = {static_cast<__bf16>(o.x * inv), static_cast<__bf16>(o.y * inv)};
-    const qbf16x2 c = {static_cast<__bf16>(o.z * inv), static_cast<__bf16>(o.w * inv)};
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + at_row * D + 4 * d4) =
-        make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
-  }
-  if (P.lse && d4 == 0) P.lse[at_row] = (M + log2f(Z)) * static_cast<float>(kLn2);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
@@ -622,35 +785,37 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   QuantAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.Hq / a.Hkv);
   const int blocks = static_cast<int>(std::max<int64_t>(1, (rows + 15) / 16));
-  p.groups = (blocks + kQaBlocks - 1) / kQaBlocks;
-  p.blocks = (blocks + p.groups - 1) / p.groups;
-  p.wave_blocks = std::min(p.blocks, kQaWaveBlocks);
-  const int64_t pairs = static_cast<int64_t>(a.Hkv) * p.groups;
-  const int64_t target = 512;
-  p.ranges = static_cast<int>(std::max<int64_t>(1, target / pairs));
-  p.least_units = 8;
+  const int most = most_blocks(a.D, a.out_dtype == kF32 ? 2 : 1);
+  p.groups = (blocks + most - 1) / most;
+  p.rows = 16 * std::min(blocks, most);
+  p.waves = static_cast<int64_t>(a.Hkv) * a.B < 512 ? 8 : 4;
+  p.ranges = std::max(1, (p.waves == 8 ? 256 : 512) / a.Hkv);
   return p;
 }
 
-static size_t quant_rows(const AttnArgs& a, const QuantAttnPlan& p) {
-  return static_cast<size_t>(a.Hkv) * p.groups * p.ranges * 2 * 16 * p.blocks;
-}
+// Partial results, their statistics, and the words that count a request's pieces.
+static size_t quant_rows(const AttnArgs& a, const QuantAttnPlan& p) { return static_cast<size_t>(a.Hkv) * p.ranges * 2 * p.rows; }
+static size_t quant_words(const AttnArgs& a, const QuantAttnPlan& p) { return static_cast<size_t>(a.Hkv) * p.groups * a.B; }
 size_t quant_attn_workspace_bytes(const AttnArgs& a, const QuantAttnPlan& p) {
-  return quant_rows(a, p) * (static_cast<size_t>(a.D) * sizeof(float) + sizeof(float2));
+  if (p.ranges == 1) return 0;                                  // one range per KV head: nothing is cut
+  return quant_rows(a, p) * (static_cast<size_t>(a.D) * sizeof(float) + sizeof(float2)) + quant_words(a, p) * sizeof(unsigned long long);
 }
 
+template <int D, int TERMS, int NW>
+static int launch_quant(const QuantAttnParams& P, const AttnArgs& a, const QuantAttnPlan& p, hipStream_t stream) {
+  static std::atomic<uint64_t> lds_set{0};
+  constexpr size_t lds = sizeof(QuantAttnShared<D, NW>);
+  static_assert(lds <= (NW == 8 ? 160 : 80) * 1024, "two workgroups of four waves, or one of eight, to a compute unit");
+  if (lds > 65536 && set_lds_once(attn_quant_kernel<D, TERMS, NW>, lds, lds_set) != 0) return -6;
+  hipLaunchKernelGGL((attn_quant_kernel<D, TERMS, NW>), dim3(p.ranges * a.Hkv), dim3(NW * kWave), lds, stream, P);
+  return 0;
+}
 template <int D, int TERMS>
-static void launch_quant(const QuantAttnParams& P, const AttnArgs& a, const QuantAttnPlan& p, hipStream_t stream) {
-  const dim3 grid(p.ranges, a.Hkv, p.groups);
-  auto kernel = p.wave_blocks == 1 ? attn_quant_kernel<D, 1, TERMS> : (p.wave_blocks == 2 ? attn_quant_kernel<D, 2, TERMS> : attn_quant_kernel<D, kQaWaveBlocks, TERMS>);
-  hipLaunchKernelGGL(kernel, grid, dim3(kQaThreads), 0, stream, P);
-  if (p.ranges > 1) {
-    const int rows = a.max_q * (a.Hq / a.Hkv), per = 256 / (D / 4);
-    hipLaunchKernelGGL((attn_quant_combine_kernel<D>), dim3(a.B, a.Hkv, (rows + per - 1) / per), dim3(256), 0, stream, P, p.groups);
-  }
+static int launch_quant_waves(const QuantAttnParams& P, const AttnArgs& a, const QuantAttnPlan& p, hipStream_t stream) {
+  return p.waves == 8 ? launch_quant<D, TERMS, 8>(P, a, p, stream) : launch_quant<D, TERMS, 4>(P, a, p, stream);
 }
 
-void launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_scale, int num_pages, const QuantAttnPlan& p, hipStream_t stream) {
+int launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_scale, int num_pages, const QuantAttnPlan& p, hipStream_t stream) {
   QuantAttnParams P{};
   P.q = static_cast<const uint16_t*>(a.q); P.k_pool = static_cast<const unsigned char*>(a.k_pool);
   P.v_pool = static_cast<const unsigned char*>(a.v_pool); P.k_scale = k_scale; P.v_scale = v_scale;
@@ -658,11 +823,18 @@ void launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_s
   P.out = a.out; P.lse = a.lse;
   P.ws_o = static_cast<float*>(a.workspace);
   P.ws_ml = reinterpret_cast<float2*>(P.ws_o + quant_rows(a, p) * a.D);
-  P.B = a.B; P.Hq = a.Hq; P.Hkv = a.Hkv; P.G = a.Hq / a.Hkv; P.total_q = a.total_q; P.max_pages = a.max_pages; P.num_pages = num_pages;
-  P.ranges = p.ranges; P.least_units = p.least_units; P.blocks = p.blocks;
+  if (p.ranges > 1) {
+    P.arrived = reinterpret_cast<unsigned long long*>(P.ws_ml + quant_rows(a, p));
+    const MessageTag t = next_message_tag(false, stream);
+    if (t.clear) clear_messages(P.arrived, static_cast<int64_t>(quant_words(a, p)), stream);
+    P.tag = t.tag;
+  }
+  P.B = a.B; P.Hq = a.Hq; P.Hkv = a.Hkv; P.G = a.Hq / a.Hkv; P.total_q = a.total_q; P.max_q = std::min(a.max_q, kQaMaxNodes);
+  P.max_pages = a.max_pages; P.num_pages = num_pages;
+  P.ranges = p.ranges; P.groups = p.groups; P.rows = p.rows;
   P.c = a.scale * kLog2e; P.out_f32 = a.out_dtype == kF32;
-  if (a.D == 128) P.out_f32 ? launch_quant<128, 2>(P, a, p, stream) : launch_quant<128, 1>(P, a, p, stream);
-  else P.out_f32 ? launch_quant<64, 2>(P, a, p, stream) : launch_quant<64, 1>(P, a, p, stream);
+  if (a.D == 128) return P.out_f32 ? launch_quant_waves<128, 2>(P, a, p, stream) : launch_quant_waves<128, 1>(P, a, p, stream);
+  return P.out_f32 ? launch_quant_waves<64, 2>(P, a, p, stream) : launch_quant_waves<64, 1>(P, a, p, stream);
 }
 
 }  // namespace specv

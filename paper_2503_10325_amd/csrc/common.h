@@ -171,6 +171,26 @@ __device__ __forceinline__ double row16_sum(double x) {
   return x + dpp_f64<0x121, 0xf>(x);
 }
 
+// A zero the compiler cannot see through.  Added to the thread id at the top of a work item's body, it ties the
+// per-lane constants of that body (lane offsets, LDS addresses) to the item: in a kernel that loops over items
+// of two different bodies they would otherwise be hoisted out of the loop and held in registers across both.
+__device__ __forceinline__ int opaque_zero() {
+  int z = 0;
+  asm volatile("" : "+s"(z));
+  return z;
+}
+
+// 16 bytes per lane from base + off + 1024 j to LDS: lane i's land at byte lds_at + 1024 j + 16 i (the instruction's offset
+// counts on both sides).  Not tracked by the compiler: the loops count these loads themselves (vmcnt).  The LDS address
+// is an operand bound to M0: the compiler writes that register itself and knows when it changes.
+__device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned off, unsigned lds_at, int j) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" :: "{m0}"(lds_at), "v"(off), "s"(base), "n"(1024 * j) : "memory");
+}
+__device__ __forceinline__ unsigned lds_address(unsigned char* p) {
+  return static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)p));
+}
+typedef __attribute__((address_space(4))) int32_t const_i32;       // read through the scalar cache
+
 // Relaxed device-scope accesses: words that workgroups of one kernel exchange.
 template <typename T> __device__ __forceinline__ T ld_dev(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -232,16 +232,15 @@ int launch_attn(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);   
 // ---- attn_quant.hip ---------------------------------------------------------------
 // A pure function of the descriptor, as AttnPlan.
 struct QuantAttnPlan {
-  int blocks;         // 16-row blocks of query rows a workgroup takes (1 .. 8)
-  int groups;         // ... groups of so many blocks that cover a request's rows
-  int wave_blocks;    // most of them a wave multiplies a unit with: 1 or 2
-  int ranges;         // workgroups per KV head and group: equal ranges of the batch's tokens
-  int least_units;    // ... of at least so many 64-token units
+  int rows;           // query rows a workgroup takes at a time, at most (16 .. 64)
+  int groups;         // ... groups of so many that cover a request's rows
+  int waves;          // of a workgroup: 4 or 8
+  int ranges;         // workgroups per KV head: ranges of the batch's tokens and groups of equal cost
 };
 QuantAttnPlan make_quant_attn_plan(const AttnArgs& a);
 size_t quant_attn_workspace_bytes(const AttnArgs& a, const QuantAttnPlan& plan);
-void launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_scale, int num_pages, const QuantAttnPlan& plan,
-                       hipStream_t stream);
+int launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_scale, int num_pages, const QuantAttnPlan& plan,
+                      hipStream_t stream);      // 0 or a negative spec_status
 
 // Vector (16-byte) accesses need 16-byte aligned base pointers; the launchers pick the scalar
 // variants of their kernels when a caller's pointer is not.

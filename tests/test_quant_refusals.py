@@ -65,7 +65,7 @@ def test_attention():
     assert call(ws=None) == WORKSPACE and call(bytes_=need - 1) == WORKSPACE
     assert call(batch=0) == 0 and call(total_q=0) == 0
     assert sv.spec_verify_attn_quant_workspace_size(sv.make_attn_desc(**{**ok, "head_dim": 96})) == 0
-    assert "attn_quant_kernel<128, 1>" in sv.spec_describe_attn_quant_plan(sv.make_attn_desc(**ok))
+    assert "attn_quant_kernel<128, 1, 8>: 16 query rows" in sv.spec_describe_attn_quant_plan(sv.make_attn_desc(**ok))
     with pytest.raises(sv.SpecError):
         sv.spec_describe_attn_quant_plan(sv.make_attn_desc(**{**ok, "head_dim": 96}))
 
