@@ -117,13 +117,6 @@ __device__ __forceinline__ void cl_weights(u32x4 rp, u32x4 rq, const LevelStats&
   }
 }
 
-// Barrier for what the waves of a workgroup exchange through LDS: rows on their way to LDS and stores to memory stay in flight.
-__device__ __forceinline__ void cl_sync() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // 2^x: 2^n by ldexp, 2^f for |f| <= 1/2 by the exponential series, 1 + f (ln 2 + f (...)) with the terms (f ln 2)^k / k! up to k = 13
 // (the first one left out is 3e-18), even and odd powers side by side: the walk is a chain of such values.  The low bits of
 // ln 2 go in with the small terms.  Largest error over [-60, 0] 0.86 of a last place (1.34e-16 relative, rms 4.8e-17), against
@@ -285,7 +278,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
     for (int i = lane; i <= kClNodes; i += kWave)
       if (sh_fc[i] >= kClNodes) sh_fc[i] = -2;    // no child
   }
-  cl_sync();
+  lds_sync();
   // The two logits of every drafted token; the draft row of a sibling group is the one its first child names (the row the
   // slices hold for that group).  Read after the first exchange, whose barriers order it.
   if (!data) {
@@ -371,7 +364,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
     }
     cl_max2(tp, tq);
     if (data) { sh_wm[0][wave] = tp; sh_wm[1][wave] = tq; }     // every lane of the wave stores the same value
-    cl_sync();
+    lds_sync();
     mp = -INFINITY; mq = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kClWaves; w += 4) {
@@ -422,7 +415,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
     }
     cl_sum2(ap, aq);
     if (data) { sh_ws[0][wave] = ap; sh_ws[1][wave] = aq; }
-    cl_sync();
+    lds_sync();
     zp = waves_total(0);
     zq = waves_total(1);
   };
@@ -479,7 +472,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
     }
     acc = wave_sum(acc);
     if (data) sh_ws[0][wave] = acc;
-    cl_sync();
+    lds_sync();
     return waves_total(0);
   };
 
@@ -499,7 +492,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
 
   // Per-(unit, wave) sums of the level-L weights of the held slice, in vocabulary order, for the draw.
   auto slice_parts = [&](const LevelStats& S, int L) {
-    cl_sync();
+    lds_sync();
     if (U != 0 && data) weights_to(S, L);
 #pragma unroll
     for (int u = 0; u < UPT; ++u) {
@@ -512,7 +505,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
       const double d = wave_sum(static_cast<double>(sum));
       sh_part[u * kClWaves + wave] = d;
     }
-    cl_sync();
+    lds_sync();
   };
 
   // ---- messages ---- (byte offsets from P.msg, worked out where they are used: kept in registers they end up in scratch
@@ -567,7 +560,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
       }
       sh_status = status;
     }
-    cl_sync();
+    lds_sync();
     return sh_status;
   };
 
@@ -583,9 +576,9 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
       if (U != 0) {
         float mp, mq;
         double zp, zq;
-        cl_sync();
+        lds_sync();
         slice_stats(sh_fc[node + 1] >= 0, mp, zp, mq, zq);
-        cl_sync();
+        lds_sync();
       }
     };
     for (int guard = 0; guard <= kClNodes + 1; ++guard) {
@@ -605,7 +598,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
         }
         next_start = -1;
         if (node >= -1) slice_stats(sh_fc[node + 1] >= 0, mp, zp, mq, zq);
-        else cl_sync();
+        else lds_sync();
         const int last = chain_node(win, LV - 1);
         fetch_ahead(last >= -1 ? sh_fc[last + 1] : -1);
         const int st = exchange(r, 2, zp, mp, zq, mq);
@@ -621,10 +614,10 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
             held_lv = lv; held_sl = sl;
             slice_stats(sh_fc[node + 1] >= 0, mp, zp, mq, zq);
           }
-          cl_sync();
+          lds_sync();
           if (wave == 0) { sh_val[2 * v] = zp; sh_aux[2 * v] = mp; sh_val[2 * v + 1] = zq; sh_aux[2 * v + 1] = mq; }
         }
-        cl_sync();
+        lds_sync();
       }
       // ---- merge the slices' parts: a wave per (level, row kind), a lane per slice ----
       for (int k = wave; k < 2 * LV; k += kClBlock / kWave) {
@@ -638,7 +631,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
         sh_M[kind][lvw] = M;                                     // every lane stores the same value
         sh_iZ[kind][lvw] = 1.0 / Z;
       }
-      cl_sync();
+      lds_sync();
 
       // ---- decisions, level by level while the walk follows the chain ----
       int j = 0;
@@ -656,7 +649,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
           if (!solo) {
             double mine = 0.0;
             if (my_lv == j) mine = slice_weight_sum(S, L);
-            else cl_sync();
+            else lds_sync();
             fetch_ahead(candidate);
             const int st = exchange(r, 1, mine, 0.f, 0.0, 0.f);
             if (st) { fail = st; return 0.0; }
@@ -664,10 +657,10 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
             for (int sl = 0; sl < SL; ++sl) {
               if (held_lv != j || held_sl != sl) bring(j, sl);
               const double t = slice_weight_sum(S, L);
-              cl_sync();
+              lds_sync();
               if (wave == 0) sh_val[j * SL + sl] = t;
             }
-            cl_sync();
+            lds_sync();
           }
           // total of the slices' sums (every wave of every workgroup: the same wave-level reduction)
           return wave_sum(lane < SL ? sh_val[j * SL + lane] : 0.0);
@@ -827,7 +820,7 @@ __global__ __launch_bounds__(kClBlock) void accept_cluster_kernel(ClusterParams 
     if (wave == 0)
       st_dev(P.msg + ((static_cast<size_t>(b) * 2 + ((lane >> 3) & 1)) * C * 2 + ((lane >> 2) & 1)) * 4 + (lane & 3),
              P.tag + kClAbort);
-    cl_sync();
+    lds_sync();
     solo = true;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no slice is on its way to memory that the workgroup gives back

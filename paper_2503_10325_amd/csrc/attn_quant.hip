@@ -1,9 +1,9 @@
 // Verify-attention over the 8-bit paged cache (quant.h): the draft queries of each request attend over its committed context and
 // their draft ancestors, keys and values read as e4m3 with a scale per (page, KV head).
 //
-// A wave takes units of 32 tokens (2 pages), straight from memory into a ring of its own in LDS (K two units deep, V one: both go on to
-// registers at once): no barrier stands between memory and the matrix cores, and the bytes in flight cost no registers.  Pages are laid
-// out so that a lane's 16 (K) or 8 (V) bytes are matrix operands as they lie, without transposition.
+// A wave takes units of 32 tokens (2 pages), straight from memory into a buffer of its own in LDS, and from there to registers at once,
+// so that the next unit is on its way meanwhile: no barrier stands between memory and the matrix cores, and the bytes in flight cost no
+// registers.  Pages are laid out so that a lane's 16 (K) or 8 (V) bytes are matrix operands as they lie, without transposition.
 //   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, tokens as M.  Row 4 g + i of sub-tile t is token 8 (g % 2) + 4 t + i of page g / 2, so that
 //                 lane group g (lanes 16 g .. 16 g + 15, one query row each) ends up with 8 tokens of one page: its scale is one register, and
 //   O^T = V^T P^T takes those 8 weights as its operand without any exchange between lanes.
@@ -57,6 +57,7 @@ struct QuantAttnParams {
   float* ws_o;        // [KV heads][ranges][2][rows][D] unnormalised partial results
   float2* ws_ml;      // ... [rows] (maximum in log2 units, sum)
   int B, Hq, Hkv, G, total_q, max_q, max_pages, num_pages;
+  uint32_t inverse_G; // 2^31 / G, rounded up
   unsigned long long* arrived;      // [KV heads][groups][B] messages: how many pieces of a request's rows are done
   unsigned long long tag;
   int ranges;         // per KV head, at most
@@ -88,8 +89,8 @@ __device__ __forceinline__ RowGroups group_rows(int rows, int most) {
 }
 // What a unit costs its workgroup by the 16-row blocks it is multiplied with, and what a group of rows costs besides: its start and its end.
 __device__ __forceinline__ int unit_cost(int blocks) { return 24 + 4 * blocks; }
-constexpr int kStartCost = 128;
-constexpr int kWholeCost = 776;               // a group of at most this cost (24 units of few rows) is not cut: its merge would take longer
+constexpr int kStartCost = 300;
+constexpr int kWholeCost = 956;               // a group of at most this cost (24 units of few rows) is not cut: its merge would take longer
 constexpr int kLeastRange = 256;              // ranges cost at least this, or as much as the average group
 
 // The requests, 64 at a time: lane i holds request 64 k + i.
@@ -216,7 +217,7 @@ struct QuantAttnShared {
   static constexpr int kPageBytes = kQuantPage * D;            // of K, or V, of a head
   static constexpr int kHalf = 2 * kPageBytes;                 // a unit's K, or V
   union {
-    __align__(1024) unsigned char ring[NW][3][kHalf];          // K, K, V
+    __align__(1024) unsigned char ring[NW][2][kHalf];          // K, V of a unit
     __align__(16) float o[NW][16][kStride];                    // the merge of the waves, when the units are done with
     struct {
       float m[kMergeRoom], l[kMergeRoom];
@@ -230,7 +231,7 @@ struct QuantAttnShared {
   int last;                                                    // this workgroup finished its request's last piece
   int64_t row[16 * kQaBlocks];                                 // of q and out, of the piece's query rows
   int node[16 * kQaBlocks];
-  float top[16 * kQaBlocks], sum[16 * kQaBlocks];              // a row's statistics
+  float top[16 * kQaBlocks], inv[16 * kQaBlocks];              // a row's maximum, and 1 / the sum of its weights
   float m[NW][16 * kQaBlocks], l[NW][16 * kQaBlocks];
 };
 
@@ -242,14 +243,20 @@ struct QuantPiece {
   unsigned long long* word;   // ... and the word that counts the pieces
 };
 
+// Query row r of a KV head is head r % G of node r / G (fewer than 2^17 rows, G up to 2^10: exact).
+__device__ __forceinline__ int node_of(const QuantAttnParams& P, int row) { return static_cast<int>(__umulhi(2u * row, P.inverse_G)); }
+__device__ __forceinline__ int64_t query_row(const QuantAttnParams& P, const QuantPiece& J, int row) {
+  const int node = node_of(P, row);
+  return static_cast<int64_t>(J.first + node) * P.Hq + J.kvh * P.G + (row - node * P.G);
+}
+
 // The piece's query rows: their nodes, and where they lie in q and out (rows past the last repeat it).
 template <typename Sh>
-__device__ __forceinline__ void find_rows(const QuantAttnParams& P, Sh& S, const QuantPiece& J) {
-  const int i = threadIdx.x;
+__device__ __forceinline__ void find_rows(const QuantAttnParams& P, Sh& S, const QuantPiece& J, int i) {
   if (i >= 16 * kQaBlocks) return;
-  const int row = J.row_base + min(i, J.rows - 1), node = row / P.G;
-  S.node[i] = node;
-  S.row[i] = static_cast<int64_t>(J.first + node) * P.Hq + J.kvh * P.G + (row - node * P.G);
+  const int row = J.row_base + min(i, J.rows - 1);
+  S.node[i] = node_of(P, row);
+  S.row[i] = query_row(P, J, row);
 }
 
 // Dimensions d0 and d0 + 1 of a row's result are NaN where a value is that the row sees, among the units that reach the drafts (of the others
@@ -275,17 +282,20 @@ __device__ __forceinline__ unsigned long long pair_bits(float lo, float hi) {
   return static_cast<unsigned long long>(__float_as_uint(hi)) << 32 | __float_as_uint(lo);
 }
 
-// Dimensions 2 d2 and 2 d2 + 1 of a row's result from their sums and the row's statistics.
+// Dimensions 4 d4 .. + 3 of a row's result from their sums; inv: 1 / the row's sum of weights (0: it sees nothing, and gives 0).
 template <int D>
-__device__ __forceinline__ void put_result(const QuantAttnParams& P, int64_t at, int d2, float lo, float hi, float M, float Z) {
-  const float inv = Z == 0.f ? 0.f : 1.f / Z;                   // a row that sees nothing gives 0 (and -infinity)
+__device__ __forceinline__ void put_result(const QuantAttnParams& P, int64_t at, int d4, float4 x, float inv) {
   if (P.out_f32) {
-    reinterpret_cast<float2*>(static_cast<float*>(P.out) + at * D)[d2] = make_float2(lo * inv, hi * inv);
+    reinterpret_cast<float4*>(static_cast<float*>(P.out) + at * D)[d4] = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
   } else {
-    const qbf16x2 a = {static_cast<__bf16>(lo * inv), static_cast<__bf16>(hi * inv)};
-    reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(P.out) + at * D)[d2] = __builtin_bit_cast(uint32_t, a);
+    const qbf16x2 lo = {static_cast<__bf16>(x.x * inv), static_cast<__bf16>(x.y * inv)}, hi = {static_cast<__bf16>(x.z * inv), static_cast<__bf16>(x.w * inv)};
+    reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + at * D)[d4] = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
   }
-  if (P.lse && d2 == 0) P.lse[at] = (M + log2f(Z)) * static_cast<float>(kLn2);
+}
+// ... and its log-sum-exp (nothing seen: -infinity) from the maximum in log2 units and the sum; returns 1 / sum
+__device__ __forceinline__ float put_lse(const QuantAttnParams& P, int64_t at, float M, float Z) {
+  if (P.lse) P.lse[at] = (M + log2f(Z)) * static_cast<float>(kLn2);
+  return Z == 0.f ? 0.f : 1.f / Z;
 }
 
 // The pieces of a request count themselves in a word {count : the call's tag}.  What an earlier call left there is first replaced by a count
@@ -310,20 +320,20 @@ __device__ __forceinline__ bool last_piece(unsigned long long* word, int pieces,
 // Merges the partial results of a request's pieces, in their order; `pair`: the KV head's first range.
 template <typename Sh>
 __device__ __forceinline__ void merge_pieces(const QuantAttnParams& P, Sh& S, const QuantPiece& J, int64_t pair, const Pieces& all) {
-  constexpr int D = Sh::D, kFly = 8, kThreads = Sh::kThreads;
+  constexpr int D = Sh::D, kFly = 4, kThreads = Sh::kThreads;
   const int tid = threadIdx.x;
   const int pieces = all.count;
   auto part = [&](int i) { return ((pair + (i == 0 ? all.first : all.rest + i - 1)) * 2 + (i == 0 ? 1 : 0)) * P.rows; };
   const int chunk = min(J.rows, max(1, kMergeRoom / pieces));
   for (int r0 = 0; r0 < J.rows; r0 += chunk) {
     const int rows = min(chunk, J.rows - r0);
-    __syncthreads();
+    lds_sync();
     for (int at = tid; at < rows * pieces; at += kThreads) {
       const unsigned long long w = ld_dev(reinterpret_cast<const unsigned long long*>(P.ws_ml + part(at / rows) + r0 + at % rows));
       S.merge.m[at] = __uint_as_float(static_cast<unsigned>(w));
       S.merge.l[at] = __uint_as_float(static_cast<unsigned>(w >> 32));
     }
-    __syncthreads();
+    lds_sync();
     for (int r = tid; r < rows; r += kThreads) {
       float M = -INFINITY, Z = 0.f;
       for (int i = 0; i < pieces; ++i) M = fmaxf(M, S.merge.m[i * rows + r]);
@@ -333,27 +343,31 @@ __device__ __forceinline__ void merge_pieces(const QuantAttnParams& P, Sh& S, co
         Z += m == -INFINITY ? 0.f : S.merge.l[i * rows + r] * f;
         S.merge.m[i * rows + r] = f;
       }
-      S.top[r] = M;
-      S.sum[r] = Z;
+      S.inv[r] = put_lse(P, S.row[r0 + r], M, Z);
     }
-    __syncthreads();
-    for (int at = tid; at < rows * (D / 2); at += kThreads) {
-      const int r = at / (D / 2), d2 = at % (D / 2);
-      float lo = 0.f, hi = 0.f;
+    lds_sync();
+    for (int at = tid; at < rows * (D / 4); at += kThreads) {
+      const int r = at / (D / 4), d4 = at % (D / 4);
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int i0 = 0; i0 < pieces; i0 += kFly) {
-        unsigned long long x[kFly];
+        unsigned long long x[kFly][2];
 #pragma unroll
-        for (int k = 0; k < kFly; ++k)
-          x[k] = ld_dev(reinterpret_cast<const unsigned long long*>(P.ws_o + (part(min(i0 + k, pieces - 1)) + r0 + r) * D) + d2);
+        for (int k = 0; k < kFly; ++k) {
+          const unsigned long long* from = reinterpret_cast<const unsigned long long*>(P.ws_o + (part(min(i0 + k, pieces - 1)) + r0 + r) * D) + 2 * d4;
+          x[k][0] = ld_dev(from);
+          x[k][1] = ld_dev(from + 1);
+        }
 #pragma unroll
         for (int k = 0; k < kFly; ++k) {
           if (i0 + k >= pieces) break;
           const float f = S.merge.m[(i0 + k) * rows + r];
-          lo += __uint_as_float(static_cast<unsigned>(x[k])) * f;
-          hi += __uint_as_float(static_cast<unsigned>(x[k] >> 32)) * f;
+          sum.x += __uint_as_float(static_cast<unsigned>(x[k][0])) * f;
+          sum.y += __uint_as_float(static_cast<unsigned>(x[k][0] >> 32)) * f;
+          sum.z += __uint_as_float(static_cast<unsigned>(x[k][1])) * f;
+          sum.w += __uint_as_float(static_cast<unsigned>(x[k][1] >> 32)) * f;
         }
       }
-      put_result<D>(P, S.row[r0 + r], d2, lo, hi, S.top[r], S.sum[r]);
+      put_result<D>(P, S.row[r0 + r], d4, sum, S.inv[r]);
     }
   }
 }
@@ -373,9 +387,6 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   const int rn = lane & 15, g = lane >> 4;                     // query row of the block (matrix column), lane group
   const int L = J.ctx + J.n;
   const bool touches_drafts = J.t1 * kUnit > J.ctx;
-
-  const unsigned long long count_seen = SANITIZE || J.whole || tid > 0 ? 0ull : ld_dev(J.word);
-  __syncthreads();                                              // the LDS of the piece before is free
 
   // ---- a unit's loads: page ids through the scalar cache, a page of a head is contiguous; lane i brings bytes 16 i .. + 16 of each 1 KB ----
   const int64_t page_bytes = static_cast<int64_t>(P.Hkv) * Sh::kPageBytes;
@@ -409,30 +420,44 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
     const float* at = (lane & 1 ? P.v_scale : P.k_scale) + static_cast<int64_t>(id) * P.Hkv + J.kvh;
     at = id >= 0 ? at : kNoScale;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) load_to_lds(a, 16 * lane, ring + 2 * Sh::kHalf, j);
+    for (int j = 0; j < kLoads; ++j) load_to_lds(a, 16 * lane, ring + Sh::kHalf, j);
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) load_to_lds(b, 16 * lane, ring + 2 * Sh::kHalf + Sh::kPageBytes, j);
+    for (int j = 0; j < kLoads; ++j) load_to_lds(b, 16 * lane, ring + Sh::kHalf + Sh::kPageBytes, j);
     asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" :: "{m0}"(scales), "v"(at) : "memory");
   };
   constexpr int kKLoads = 2 * kLoads, kVLoads = 2 * kLoads + 1;
 
   int t = J.t0 + wave;
   const int mine = t < J.t1 ? (J.t1 - t + kWaves - 1) / kWaves : 0;      // units of this wave
+
+  // ---- all that the piece needs besides its pages is on its way at once, and stored before its pages are asked for ----
+  // query operands: step 2 h + e, lane group g: dimensions 16 (4 h + g) + 8 e .. + 8 (what a lane's 16 bytes of K hold)
+  constexpr int kFrags = NB * 2 * kH, kMine = (kFrags + kWaves - 1) / kWaves;
+  raw4 qv[kMine];
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    const int f = min(wave + j * kWaves, kFrags - 1), s = f % (2 * kH), row = J.row_base + min(16 * (f / (2 * kH)) + rn, J.rows - 1);    // (columns past the last row repeat it)
+    qv[j] = *reinterpret_cast<const raw4*>(P.q + query_row(P, J, row) * D + 16 * g + 64 * (s >> 1) + 8 * (s & 1));
+  }
+  int parent = -1;
+  if (touches_drafts && P.parent && tid < J.n) parent = P.parent[J.first + tid];
+  const unsigned long long count_seen = SANITIZE || J.whole || tid > 0 ? 0ull : ld_dev(J.word);
+  if (mine > 0) fetch_ids(t);
+  lds_sync();                                                   // the LDS of the piece before is free
+#pragma unroll
+  for (int j = 0; j < kMine; ++j)
+    if (wave + j * kWaves < kFrags) S.q[wave + j * kWaves][lane] = qv[j];
+  if (tid < J.n) S.parent[tid] = parent;
   if (mine > 0) {
-    fetch_ids(t);
     issue_k(ring);
     v_id0 = k_id0; v_id1 = k_id1;
-    fetch_ids(t + kWaves);
-    if (mine > 1) issue_k(ring + Sh::kHalf);
     issue_v();
-    v_id0 = k_id0; v_id1 = k_id1;
-    fetch_ids(t + 2 * kWaves);
+    fetch_ids(t + kWaves);
   }
-
   if (!SANITIZE && tid == 0) S.nans = 0;
+  find_rows(P, S, J, tid);
   if (touches_drafts) {
-    if (P.parent && tid < J.n) S.parent[tid] = P.parent[J.first + tid];
-    __syncthreads();
+    lds_sync();
     if (tid < kQaMaxNodes) {
       unsigned long long w[2] = {0ull, 0ull};
       if (tid < J.n) {
@@ -452,20 +477,13 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       S.anc[tid][1] = w[1];
     }
   }
-  // ---- query operands, to LDS: step 2 h + e, lane group g: dimensions 16 (4 h + g) + 8 e .. + 8 (what a lane's 16 bytes of K hold) ----
-  for (int f = wave; f < NB * 2 * kH; f += kWaves) {
-    const int s = f % (2 * kH), row = J.row_base + min(16 * (f / (2 * kH)) + rn, J.rows - 1);    // (columns past the last row repeat it)
-    const uint16_t* qp = P.q + (static_cast<int64_t>(J.first + row / P.G) * P.Hq + J.kvh * P.G + row % P.G) * D + 16 * g;
-    S.q[f][lane] = *reinterpret_cast<const raw4*>(qp + 64 * (s >> 1) + 8 * (s & 1));
-  }
-  find_rows(P, S, J);
-  __syncthreads();
+  lds_sync();
 
   // Operand reads.  K, lane group g: chunk 4 h + g; lane: page rn / 8, token 8 (rn / 4 % 2) + 4 st + rn % 4.  The second page lies with tokens
   // 4 i .. + 3 and their neighbours 4 (i ^ 1) .. exchanged: 16 lanes take their 256 bytes from as many banks.
   const unsigned k_at = ring + (rn >> 3) * Sh::kPageBytes + g * 256 + (8 * ((rn >> 2) & 1) + (rn & 3)) * 16;
   const unsigned k_flip = 64 * (rn >> 3);                       // sub-tile st at k_at + (64 st ^ k_flip)
-  const unsigned v_at = ring + 2 * Sh::kHalf + (g >> 1) * Sh::kPageBytes + rn * 16 + 8 * (g & 1);
+  const unsigned v_at = ring + Sh::kHalf + (g >> 1) * Sh::kPageBytes + rn * 16 + 8 * (g & 1);
   const unsigned s_at = scales + 8 * (g >> 1);
 
   // ref: what a row's weights are relative to, in log2 units; sum: of this lane's tokens; v_ref: what the results are relative to
@@ -480,11 +498,10 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   }
 
   for (int i = 0; i < mine; ++i, t += kWaves) {
-    const unsigned at = (i & 1) * Sh::kHalf;
+    const unsigned at = 0;
     const int behind = mine - 1 - i;                            // units of this wave after this one
     // K of this unit is here: behind it the next one's K, and V
-    if (behind > 0) wait_loads<kKLoads + kVLoads>();
-    else wait_loads<kVLoads>();
+    wait_loads<kVLoads>();
     // ---- scores: K at once, the queries' operands a step ahead of the products (four blocks: of the first two, registers are short) ----
     constexpr int kAhead = NB < 4 ? NB : 2;
     qf32x4 s[NB][2];
@@ -497,7 +514,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
 #pragma unroll
     for (int qi = 0; qi < kAhead; ++qi) qr[0][qi] = S.q[qi * 2 * kH][lane];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K has been read
-    if (behind > 1) issue_k(ring + at);
+    if (behind > 0) issue_k(ring + at);
 #pragma unroll
     for (int step = 0; step < 2 * kH; ++step) {
       const int h = step >> 1, e = step & 1;
@@ -518,7 +535,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       __builtin_amdgcn_sched_barrier(0);
     }
     // V of this unit and its scales are here: behind them the K after next
-    if (behind > 1) wait_loads<kKLoads>();
+    if (behind > 0) wait_loads<kKLoads>();
     else wait_loads<0>();
     const float ks = *lds_f32(s_at), v_own = *lds_f32(s_at + 4);
     raw2 vr[kDT];
@@ -526,9 +543,9 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
     for (int d = 0; d < kDT; ++d) vr[d] = *lds_raw2(v_at + 256 * d);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V has been read
     if (behind > 0) {
-      issue_v();
       v_id0 = k_id0; v_id1 = k_id1;
-      fetch_ids(t + 3 * kWaves);
+      issue_v();
+      fetch_ids(t + 2 * kWaves);
     }
     const bool ok = ks != 0.f;
     const float factor = ok ? ks * P.c : 1.f;                   // (not 0: masked scores are -infinity)
@@ -653,7 +670,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       S.l[wave][16 * qi + lane] = sum[qi];
     }
   }
-  __syncthreads();                                              // (the rings are done with, too)
+  lds_sync();                                              // (the rings are done with, too)
   if constexpr (!SANITIZE) {
     if (S.nans) return;
   }
@@ -664,36 +681,44 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) Z += S.m[w][tid] == -INFINITY ? 0.f : S.l[w][tid] * fast_exp2(S.m[w][tid] - M);
     S.top[tid] = M;
-    S.sum[tid] = Z;
+    if (tid < J.rows) {
+      if (J.whole) S.inv[tid] = put_lse(P, S.row[tid], M, Z);
+      else st_dev(reinterpret_cast<unsigned long long*>(P.ws_ml + J.part + tid), pair_bits(M, Z));
+    }
   }
+  lds_sync();
+  constexpr int kItems = 16 * (D / 4) / Sh::kThreads > 0 ? 16 * (D / 4) / Sh::kThreads : 1;     // of a thread and block: four dimensions of a row
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
-    if (qi > 0) __syncthreads();
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, S.m[w][16 * qi + rn]);
-    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - top - static_cast<float>(kWeightBias)) * v_ref;
+    if (qi > 0) lds_sync();
+    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - S.top[16 * qi + rn] - static_cast<float>(kWeightBias)) * v_ref;
 #pragma unroll
     for (int d = 0; d < kDT; ++d)
       *reinterpret_cast<float4*>(&S.o[wave][rn][16 * d + 4 * g]) =
           make_float4(oacc[qi][d][0] * f, oacc[qi][d][1] * f, oacc[qi][d][2] * f, oacc[qi][d][3] * f);
-    __syncthreads();
-    for (int at = tid; at < 16 * (D / 2); at += Sh::kThreads) {
-      const int d2 = at % (D / 2), r = at / (D / 2), row = 16 * qi + r;
-      if (row >= J.rows) continue;
-      float lo = 0.f, hi = 0.f;
+    lds_sync();
+#pragma unroll
+    for (int item = 0; item < kItems; ++item) {
+      const int at = tid + item * Sh::kThreads, d4 = at % (D / 4), r = at / (D / 4), row = 16 * qi + r;
+      if (r >= 16 || row >= J.rows) continue;
+      float4 x[kWaves], sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) x[w] = *reinterpret_cast<const float4*>(&S.o[w][r][4 * d4]);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float2 x = *reinterpret_cast<const float2*>(&S.o[w][r][2 * d2]);
-        lo += x.x; hi += x.y;
+        sum.x += x[w].x; sum.y += x[w].y; sum.z += x[w].z; sum.w += x[w].w;
       }
-      if constexpr (SANITIZE) put_back_nans(P, S, J, row, 2 * d2, lo, hi);
+      if constexpr (SANITIZE) {
+        put_back_nans(P, S, J, row, 4 * d4, sum.x, sum.y);
+        put_back_nans(P, S, J, row, 4 * d4 + 2, sum.z, sum.w);
+      }
       if (J.whole) {
-        put_result<D>(P, S.row[row], d2, lo, hi, S.top[row], S.sum[row]);
+        put_result<D>(P, S.row[row], d4, sum, S.inv[row]);
       } else {
         // read by another workgroup of this launch: device-scope stores
-        st_dev(reinterpret_cast<unsigned long long*>(P.ws_o + (J.part + row) * D) + d2, pair_bits(lo, hi));
-        if (d2 == 0) st_dev(reinterpret_cast<unsigned long long*>(P.ws_ml + J.part + row), pair_bits(S.top[row], S.sum[row]));
+        unsigned long long* to = reinterpret_cast<unsigned long long*>(P.ws_o + (J.part + row) * D) + 2 * d4;
+        st_dev(to, pair_bits(sum.x, sum.y));
+        st_dev(to + 1, pair_bits(sum.z, sum.w));
       }
     }
   }
@@ -769,7 +794,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
           quant_piece<1, TERMS, true>(P, S, part);
         }
         __syncthreads();
-        find_rows(P, S, J);                                     // (of all rows again, for the merge)
+        find_rows(P, S, J, threadIdx.x);                                     // (of all rows again, for the merge)
       }
       if (!J.whole) {
         const Pieces all_pieces = pieces_of(cut, p);
@@ -788,7 +813,7 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   const int most = most_blocks(a.D, a.out_dtype == kF32 ? 2 : 1);
   p.groups = (blocks + most - 1) / most;
   p.rows = 16 * std::min(blocks, most);
-  p.waves = static_cast<int64_t>(a.Hkv) * a.B < 512 ? 8 : 4;
+  p.waves = static_cast<int64_t>(a.Hkv) * a.B * p.groups < 512 ? 8 : 4;
   p.ranges = std::max(1, (p.waves == 8 ? 256 : 512) / a.Hkv);
   return p;
 }
@@ -829,7 +854,7 @@ int launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_sc
     if (t.clear) clear_messages(P.arrived, static_cast<int64_t>(quant_words(a, p)), stream);
     P.tag = t.tag;
   }
-  P.B = a.B; P.Hq = a.Hq; P.Hkv = a.Hkv; P.G = a.Hq / a.Hkv; P.total_q = a.total_q; P.max_q = std::min(a.max_q, kQaMaxNodes);
+  P.B = a.B; P.Hq = a.Hq; P.Hkv = a.Hkv; P.G = a.Hq / a.Hkv; P.inverse_G = ((1u << 31) + P.G - 1) / P.G; P.total_q = a.total_q; P.max_q = std::min(a.max_q, kQaMaxNodes);
   P.max_pages = a.max_pages; P.num_pages = num_pages;
   P.ranges = p.ranges; P.groups = p.groups; P.rows = p.rows;
   P.c = a.scale * kLog2e; P.out_f32 = a.out_dtype == kF32;

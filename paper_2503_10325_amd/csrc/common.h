@@ -191,6 +191,13 @@ __device__ __forceinline__ unsigned lds_address(unsigned char* p) {
 }
 typedef __attribute__((address_space(4))) int32_t const_i32;       // read through the scalar cache
 
+// Barrier for what the waves of a workgroup exchange through LDS: loads on their way to LDS and stores to memory stay in flight.
+__device__ __forceinline__ void lds_sync() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Relaxed device-scope accesses: words that workgroups of one kernel exchange.
 template <typename T> __device__ __forceinline__ T ld_dev(const T* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
