@@ -470,6 +470,7 @@ int32_t spec_verify_attn_quant(const spec_attn_desc* desc, int32_t num_pages, co
   AttnArgs a = attn_args_from(desc);
   if (a.scale == 0.f) a.scale = 1.0f / sqrtf(static_cast<float>(a.D));
   const QuantAttnPlan plan = make_quant_attn_plan(a);
+  if (plan.shift >= kQuantMaxShift) return SPEC_ERR_UNSUPPORTED;          // millions of groups of query rows
   const size_t need = quant_attn_workspace_bytes(a, plan);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SPEC_ERR_WORKSPACE;
   a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.block_table = block_table; a.ctx_len = ctx_len;

@@ -42,6 +42,8 @@ constexpr float kSlack = 8.f;                 // the reference of a row's softma
 constexpr float kLeastV = 3.0517578125e-5f;   // 2^-15: what V may be scaled by and still be exact in fp16
 static __device__ const float kNoScale[1] = {0.f};      // read in place of the scale of a page that is none
 
+constexpr int ilog2(int x) { return x <= 1 ? 0 : 1 + ilog2(x / 2); }
+
 struct QuantAttnParams {
   const uint16_t* q;
   const unsigned char* k_pool;
@@ -63,11 +65,28 @@ struct QuantAttnParams {
   int ranges;         // per KV head, at most
   int groups;         // of query rows, at most
   int rows;           // of a group, at most
+  int halves;         // 2: rows that are too many for a wave are dealt to two halves of a workgroup's waves
+  int shift;          // units are counted in chunks of 2^shift
   float c;            // scale * log2(e)
   int out_f32;
 };
 
-__device__ __forceinline__ int wave_scan_i32(int x, int lane) {
+// The kernel's arguments where the launch has put them, read through the scalar cache when they are needed: kept in registers across the pieces'
+// loop, they and what follows from them would need more lanes of vector registers than there are.
+typedef const __attribute__((address_space(4))) QuantAttnParams KernelParams;
+__device__ __forceinline__ KernelParams& kernel_params() {
+  uint64_t at = reinterpret_cast<uint64_t>((const __attribute__((address_space(4))) void*)__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(at));
+  return *(KernelParams*)at;
+}
+// A scalar that the compiler knows no origin of: it is neither read again in a loop, nor is what follows from it kept across one.
+template <typename T>
+__device__ __forceinline__ T keep_scalar(T x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+
+__device__ __forceinline__ int wave_scan(int x, int lane) {
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) {
     const int y = __shfl_up(x, d);
@@ -76,30 +95,40 @@ __device__ __forceinline__ int wave_scan_i32(int x, int lane) {
   return x;
 }
 
-// A request's 16-row blocks in groups of at most `most`, alike.
+// A request's 16-row blocks in groups, alike: `per` blocks for each wave (at most `most`), with `halves` = 2 of other blocks for the second half of
+// a workgroup's waves, which then share the units' bytes.
 struct RowGroups {
-  int groups, per;
+  int groups, per, halves;
 };
-__device__ __forceinline__ RowGroups group_rows(int rows, int most) {
+__device__ __forceinline__ RowGroups group_rows(int rows, int most, int halves) {
   const int blocks = (rows + 15) >> 4;
   RowGroups r;
+  r.halves = blocks > most ? halves : 1;
+  most *= r.halves;
   r.groups = (blocks + most - 1) / most;
-  r.per = (blocks + r.groups - 1) / max(r.groups, 1);
+  const int each = (blocks + r.groups - 1) / max(r.groups, 1);
+  r.per = (each + r.halves - 1) / r.halves;
   return r;
 }
 // What a unit costs its workgroup by the 16-row blocks it is multiplied with, and what a group of rows costs besides: its start and its end.
 __device__ __forceinline__ int unit_cost(int blocks) { return 24 + 4 * blocks; }
-constexpr int kStartCost = 300;
-constexpr int kWholeCost = 956;               // a group of at most this cost (24 units of few rows) is not cut: its merge would take longer
-constexpr int kLeastRange = 256;              // ranges cost at least this, or as much as the average group
+// Units are counted in chunks of 2^shift (0 unless the block table has room for so many that the batch's cost would pass 31 bits).
+__device__ __forceinline__ int chunks_of(int units, int shift) { return (units + (1 << shift) - 1) >> shift; }
+constexpr int kMostCost = 24 + 4 * kQaBlocks;
+__device__ __forceinline__ int head_cost(int blocks) { return 300 + 60 * blocks; }
+constexpr int kMostHead = 300 + 60 * kQaBlocks;
+constexpr int kWholeCost = 456;               // a group whose units cost at most this (16 of few rows) is not cut: its merge would take longer
+constexpr int kLeastRange = 256;              // ranges cost at least this, and
+constexpr float kRangeRoot = 7.5f;            // this times the root of what a group costs (or as much as a group): n pieces of a group take a time of group / n
+                                              // and their merge one of n
 
 // The requests, 64 at a time: lane i holds request 64 k + i.
 struct Requests {
-  int ctx, first, n, units, groups, per;        // of this lane's request
+  int ctx, first, n, units, groups, per, halves;        // of this lane's request
   int upto;                                     // cost up to its end, within these 64
   int sum, count;                               // cost of these 64, and their groups
 };
-__device__ __forceinline__ Requests load_requests(const QuantAttnParams& P, int k, int most, int lane) {
+__device__ __forceinline__ Requests load_requests(KernelParams& P, int k, int most, int lane) {
   Requests r;
   const int b = 64 * k + lane;
   r.ctx = r.first = r.n = 0;
@@ -108,40 +137,50 @@ __device__ __forceinline__ Requests load_requests(const QuantAttnParams& P, int 
     r.first = P.q_offsets[b];
     r.n = max(min(min(P.q_offsets[b + 1], P.total_q) - r.first, P.max_q), 0);
   }
-  r.units = r.n > 0 ? static_cast<int>((static_cast<unsigned>(r.ctx) + r.n + kUnit - 1) / kUnit) : 0;
-  const RowGroups g = group_rows(r.n * P.G, most);
+  r.units = r.n > 0 ? min(static_cast<int>((static_cast<unsigned>(r.ctx) + r.n + kUnit - 1) / kUnit), (P.max_pages + 1) / 2) : 0;
+  const RowGroups g = group_rows(r.n * P.G, most, P.halves);
   r.groups = g.groups;
   r.per = g.per;
-  r.upto = wave_scan_i32(r.groups * (kStartCost + r.units * unit_cost(r.per)), lane);
+  r.halves = g.halves;
+  r.upto = wave_scan(r.groups * (head_cost(r.per) + chunks_of(r.units, P.shift) * r.halves * unit_cost(r.per)), lane);
   r.sum = __builtin_amdgcn_readlane(r.upto, 63);
-  r.count = __builtin_amdgcn_readlane(wave_scan_i32(r.groups, lane), 63);
+  r.count = __builtin_amdgcn_readlane(wave_scan(r.groups, lane), 63);
   return r;
 }
 
-// The cost of the batch in `used` ranges of equal cost (one more in the first `more`): range s starts at s * each + min(s, more).
+// The batch's cost in `used` ranges: range s starts at the whole part of s * total / used, so that of alike groups, with as many ranges for each,
+// every one starts a range.  each, more: total / used and the remainder.
 struct Cut {
   int used, each, more;
 };
-__device__ __forceinline__ Cut cut_ranges(const QuantAttnParams& P, int total, int count) {
+__device__ __forceinline__ Cut cut_ranges(int most, int total, int count) {
   Cut c;
-  c.used = min(max(max(total / kLeastRange, count), 1), P.ranges);
+  const float group = static_cast<float>(total) / static_cast<float>(max(count, 1));
+  const float least = fmaxf(kLeastRange, kRangeRoot * __builtin_amdgcn_sqrtf(group));
+  c.used = min(max(max(static_cast<int>(static_cast<float>(total) / least), count), 1), most);
+  const int alike = c.used - c.used % max(count, 1);            // as many for each group
+  if (4 * alike >= 3 * c.used) c.used = alike;
+  c.used = __builtin_amdgcn_readfirstlane(c.used);
   c.each = total / c.used;
   c.more = total - c.each * c.used;
   return c;
 }
-__device__ __forceinline__ int range_start(const Cut& c, int s) { return s * c.each + min(s, c.more); }
+__device__ __forceinline__ int range_start(const Cut& c, int s) { return s * c.each + s * c.more / c.used; }
 __device__ __forceinline__ int range_of(const Cut& c, int at) {
-  const int wide = c.more * (c.each + 1);
-  return at < wide ? at / (c.each + 1) : c.more + (at - wide) / c.each;
+  int s = at / (c.each + 1);                                    // at most two too low (ranges cost at least as much as there are)
+  while (s + 1 < c.used && range_start(c, s + 1) <= at) ++s;
+  return s;
 }
-// A group of a request's rows that starts at `start` has its units there if it is not cut, else unit 0 there and unit k at start + kStartCost + k * cost; a
-// unit belongs to the range that its place is in.  Ranges cost more than any unit, so those behind the second unit's hold one each.
+// A group of a request's rows that starts at `start` has its units there if it is not cut, else unit 0 there and unit k at start + head + k * cost; a
+// unit belongs to the range that its place is in.  (Chunks, where units come in chunks.)  Ranges cost more than any unit, so those behind the second unit's hold one each.
 struct Place {
-  int start, units, cost;
+  int start, head, units, cost, shift;          // cost: of a unit
 };
-__device__ __forceinline__ bool is_whole(const Place& p) { return kStartCost + p.units * p.cost <= kWholeCost; }
+__device__ __forceinline__ bool is_whole(const Place& p) { return chunks_of(p.units, p.shift) * p.cost <= kWholeCost; }
 __device__ __forceinline__ int first_unit(const Place& p, int at) {           // at or behind `at`
-  return at <= p.start ? 0 : (is_whole(p) ? p.units : max(1, (at - p.start - kStartCost + p.cost - 1) / p.cost));
+  if (at <= p.start) return 0;
+  if (is_whole(p)) return p.units;
+  return min(max(1, (at - p.start - p.head + p.cost - 1) / p.cost), chunks_of(p.units, p.shift)) << p.shift;
 }
 // The pieces of a group that is cut: piece 0 in range `first`, the others in `rest` and those behind it.
 struct Pieces {
@@ -150,8 +189,8 @@ struct Pieces {
 __device__ __forceinline__ Pieces pieces_of(const Cut& c, const Place& p) {
   Pieces r;
   r.first = range_of(c, p.start);
-  r.rest = max(range_of(c, p.start + kStartCost + p.cost), r.first + 1);
-  r.count = 1 + max(range_of(c, p.start + kStartCost + (p.units - 1) * p.cost) - r.rest + 1, 0);
+  r.rest = max(range_of(c, p.start + p.head + p.cost), r.first + 1);
+  r.count = 1 + max(range_of(c, p.start + p.head + (chunks_of(p.units, p.shift) - 1) * p.cost) - r.rest + 1, 0);
   return r;
 }
 
@@ -223,37 +262,37 @@ struct QuantAttnShared {
       float m[kMergeRoom], l[kMergeRoom];
     } merge;                                                   // ... of the pieces
   };
-  __align__(16) raw4 q[kQaBlocks * 2 * (D / 64)][kWave];       // query operands: [block, step][lane]
+  __align__(16) raw4 q[2 * kQaBlocks * 2 * (D / 64)][kWave];   // query operands: [half, block, step][lane]
   float scales[NW][kWave];                                     // of a unit's pages: lane i: page i / 2 % 2, K or V i % 2
   unsigned long long anc[kQaMaxNodes][2];
   int parent[kQaMaxNodes];
   int nans;                                                    // a draft's value is NaN
   int last;                                                    // this workgroup finished its request's last piece
-  int64_t row[16 * kQaBlocks];                                 // of q and out, of the piece's query rows
-  int node[16 * kQaBlocks];
-  float top[16 * kQaBlocks], inv[16 * kQaBlocks];              // a row's maximum, and 1 / the sum of its weights
+  int64_t row[32 * kQaBlocks];                                 // of q and out, of the piece's query rows
+  int node[32 * kQaBlocks];
+  float top[32 * kQaBlocks], inv[32 * kQaBlocks];              // a row's maximum, and 1 / the sum of its weights
   float m[NW][16 * kQaBlocks], l[NW][16 * kQaBlocks];
 };
 
 // One piece of a request: units [t0, t1) of it, for the query rows [row_base, row_base + rows) of a KV head.
 struct QuantPiece {
-  int b, first, n, ctx, kvh, t0, t1, row_base, rows;
+  int b, first, n, ctx, kvh, t0, t1, row_base, rows, halves;
   bool whole;                 // the piece is all of these rows: write the result
   int64_t part;               // else: first row of its partial result
   unsigned long long* word;   // ... and the word that counts the pieces
 };
 
 // Query row r of a KV head is head r % G of node r / G (fewer than 2^17 rows, G up to 2^10: exact).
-__device__ __forceinline__ int node_of(const QuantAttnParams& P, int row) { return static_cast<int>(__umulhi(2u * row, P.inverse_G)); }
-__device__ __forceinline__ int64_t query_row(const QuantAttnParams& P, const QuantPiece& J, int row) {
+__device__ __forceinline__ int node_of(KernelParams& P, int row) { return static_cast<int>(__umulhi(2u * row, P.inverse_G)); }
+__device__ __forceinline__ int64_t query_row(KernelParams& P, const QuantPiece& J, int row) {
   const int node = node_of(P, row);
   return static_cast<int64_t>(J.first + node) * P.Hq + J.kvh * P.G + (row - node * P.G);
 }
 
 // The piece's query rows: their nodes, and where they lie in q and out (rows past the last repeat it).
 template <typename Sh>
-__device__ __forceinline__ void find_rows(const QuantAttnParams& P, Sh& S, const QuantPiece& J, int i) {
-  if (i >= 16 * kQaBlocks) return;
+__device__ __forceinline__ void find_rows(KernelParams& P, Sh& S, const QuantPiece& J, int i) {
+  if (i >= 32 * kQaBlocks) return;
   const int row = J.row_base + min(i, J.rows - 1);
   S.node[i] = node_of(P, row);
   S.row[i] = query_row(P, J, row);
@@ -262,7 +301,7 @@ __device__ __forceinline__ void find_rows(const QuantAttnParams& P, Sh& S, const
 // Dimensions d0 and d0 + 1 of a row's result are NaN where a value is that the row sees, among the units that reach the drafts (of the others
 // every row sees every token, and the products are NaN by themselves).
 template <typename Sh>
-__device__ __forceinline__ void put_back_nans(const QuantAttnParams& P, const Sh& S, const QuantPiece& J, int row, int d0, float& lo, float& hi) {
+__device__ __forceinline__ void put_back_nans(KernelParams& P, const Sh& S, const QuantPiece& J, int row, int d0, float& lo, float& hi) {
   constexpr int D = Sh::D;
   const int node = S.node[row];
   const int end = min(J.t1 * kUnit, J.ctx + J.n);
@@ -284,7 +323,7 @@ __device__ __forceinline__ unsigned long long pair_bits(float lo, float hi) {
 
 // Dimensions 4 d4 .. + 3 of a row's result from their sums; inv: 1 / the row's sum of weights (0: it sees nothing, and gives 0).
 template <int D>
-__device__ __forceinline__ void put_result(const QuantAttnParams& P, int64_t at, int d4, float4 x, float inv) {
+__device__ __forceinline__ void put_result(KernelParams& P, int64_t at, int d4, float4 x, float inv) {
   if (P.out_f32) {
     reinterpret_cast<float4*>(static_cast<float*>(P.out) + at * D)[d4] = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
   } else {
@@ -293,7 +332,7 @@ __device__ __forceinline__ void put_result(const QuantAttnParams& P, int64_t at,
   }
 }
 // ... and its log-sum-exp (nothing seen: -infinity) from the maximum in log2 units and the sum; returns 1 / sum
-__device__ __forceinline__ float put_lse(const QuantAttnParams& P, int64_t at, float M, float Z) {
+__device__ __forceinline__ float put_lse(KernelParams& P, int64_t at, float M, float Z) {
   if (P.lse) P.lse[at] = (M + log2f(Z)) * static_cast<float>(kLn2);
   return Z == 0.f ? 0.f : 1.f / Z;
 }
@@ -319,8 +358,9 @@ __device__ __forceinline__ bool last_piece(unsigned long long* word, int pieces,
 
 // Merges the partial results of a request's pieces, in their order; `pair`: the KV head's first range.
 template <typename Sh>
-__device__ __forceinline__ void merge_pieces(const QuantAttnParams& P, Sh& S, const QuantPiece& J, int64_t pair, const Pieces& all) {
-  constexpr int D = Sh::D, kFly = 4, kThreads = Sh::kThreads;
+__device__ __forceinline__ void merge_pieces(Sh& S, const QuantPiece& J, int64_t pair, const Pieces& all) {
+  KernelParams& P = kernel_params();
+  constexpr int D = Sh::D, kThreads = Sh::kThreads;
   const int tid = threadIdx.x;
   const int pieces = all.count;
   auto part = [&](int i) { return ((pair + (i == 0 ? all.first : all.rest + i - 1)) * 2 + (i == 0 ? 1 : 0)) * P.rows; };
@@ -346,29 +386,45 @@ __device__ __forceinline__ void merge_pieces(const QuantAttnParams& P, Sh& S, co
       S.inv[r] = put_lse(P, S.row[r0 + r], M, Z);
     }
     lds_sync();
-    for (int at = tid; at < rows * (D / 4); at += kThreads) {
-      const int r = at / (D / 4), d4 = at % (D / 4);
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i0 = 0; i0 < pieces; i0 += kFly) {
-        unsigned long long x[kFly][2];
+    // four dimensions of kRows rows at a time, of kFly pieces: as many loads on their way for few pieces of many rows as for many of few
+    auto combine = [&](auto rows_at_once, auto fly) __attribute__((always_inline)) {
+      constexpr int kRows = decltype(rows_at_once)::value, kFly = decltype(fly)::value, kApart = kThreads / (D / 4);
+      const int d4 = tid % (D / 4);
+      for (int r1 = tid / (D / 4); r1 < rows; r1 += kRows * kApart) {
+        float4 sum[kRows];
 #pragma unroll
-        for (int k = 0; k < kFly; ++k) {
-          const unsigned long long* from = reinterpret_cast<const unsigned long long*>(P.ws_o + (part(min(i0 + k, pieces - 1)) + r0 + r) * D) + 2 * d4;
-          x[k][0] = ld_dev(from);
-          x[k][1] = ld_dev(from + 1);
+        for (int j = 0; j < kRows; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i0 = 0; i0 < pieces; i0 += kFly) {
+          unsigned long long x[kFly][kRows][2];
+#pragma unroll
+          for (int k = 0; k < kFly; ++k)
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+              const unsigned long long* from = reinterpret_cast<const unsigned long long*>(
+                  P.ws_o + (part(min(i0 + k, pieces - 1)) + r0 + min(r1 + j * kApart, rows - 1)) * D) + 2 * d4;
+              x[k][j][0] = ld_dev(from);
+              x[k][j][1] = ld_dev(from + 1);
+            }
+#pragma unroll
+          for (int k = 0; k < kFly; ++k) {
+            if (i0 + k >= pieces) break;
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+              const float f = S.merge.m[(i0 + k) * rows + min(r1 + j * kApart, rows - 1)];
+              sum[j].x += __uint_as_float(static_cast<unsigned>(x[k][j][0])) * f;
+              sum[j].y += __uint_as_float(static_cast<unsigned>(x[k][j][0] >> 32)) * f;
+              sum[j].z += __uint_as_float(static_cast<unsigned>(x[k][j][1])) * f;
+              sum[j].w += __uint_as_float(static_cast<unsigned>(x[k][j][1] >> 32)) * f;
+            }
+          }
         }
 #pragma unroll
-        for (int k = 0; k < kFly; ++k) {
-          if (i0 + k >= pieces) break;
-          const float f = S.merge.m[(i0 + k) * rows + r];
-          sum.x += __uint_as_float(static_cast<unsigned>(x[k][0])) * f;
-          sum.y += __uint_as_float(static_cast<unsigned>(x[k][0] >> 32)) * f;
-          sum.z += __uint_as_float(static_cast<unsigned>(x[k][1])) * f;
-          sum.w += __uint_as_float(static_cast<unsigned>(x[k][1] >> 32)) * f;
-        }
+        for (int j = 0; j < kRows; ++j)
+          if (r1 + j * kApart < rows) put_result<D>(P, S.row[r0 + r1 + j * kApart], d4, sum[j], S.inv[r1 + j * kApart]);
       }
-      put_result<D>(P, S.row[r0 + r], d4, sum, S.inv[r]);
-    }
+    };
+    if (rows > kThreads / (D / 4)) combine(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+    else combine(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
   }
 }
 
@@ -376,7 +432,8 @@ __device__ __forceinline__ void merge_pieces(const QuantAttnParams& P, Sh& S, co
 // NaN would be NaN) and put back into the results of the rows that see them.  Without, a piece that meets one writes nothing and
 // says so in S.nans.
 template <int NB, int TERMS, bool SANITIZE, typename Sh>
-__device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, const QuantPiece& J) {
+__device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
+  KernelParams& P = kernel_params();
   constexpr int D = Sh::D, kWaves = Sh::kWaves;
   constexpr int kH = D / 64;                                   // K: 16-byte chunks of a lane per token
   constexpr int kDT = D / 16;                                  // 16-dimension tiles of the output
@@ -393,14 +450,18 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   const unsigned char* k_head = P.k_pool + static_cast<int64_t>(J.kvh) * Sh::kPageBytes;
   const unsigned char* v_head = P.v_pool + static_cast<int64_t>(J.kvh) * Sh::kPageBytes;
   const const_i32* bt = (const const_i32*)(P.block_table + static_cast<int64_t>(J.b) * P.max_pages);
-  const int last_page = min((L - 1) / kQuantPage, P.max_pages - 1);
+  const int num_pages = keep_scalar(P.num_pages), max_pages = keep_scalar(P.max_pages), Hkv = keep_scalar(P.Hkv);
+  const float* const k_scale = keep_scalar(P.k_scale) + J.kvh;
+  const float* const v_scale = keep_scalar(P.v_scale) + J.kvh;
+  const float c = keep_scalar(P.c);
+  const int last_page = min((L - 1) / kQuantPage, max_pages - 1);
   int k_id0 = 0, k_id1 = 0, v_id0 = 0, v_id1 = 0;               // of the units whose K and V go out next; -1: no page of the pool
   auto fetch_ids = [&](int t) __attribute__((always_inline)) {
     if (t < J.t1) {
       k_id0 = bt[min(2 * t, last_page)];
       k_id1 = bt[min(2 * t + 1, last_page)];
-      k_id0 = k_id0 >= 0 && k_id0 < P.num_pages && 2 * t < P.max_pages ? k_id0 : -1;
-      k_id1 = k_id1 >= 0 && k_id1 < P.num_pages && 2 * t + 1 < P.max_pages ? k_id1 : -1;
+      k_id0 = k_id0 >= 0 && k_id0 < num_pages && 2 * t < max_pages ? k_id0 : -1;
+      k_id1 = k_id1 >= 0 && k_id1 < num_pages && 2 * t + 1 < max_pages ? k_id1 : -1;
     }
   };
   const unsigned ring = lds_address(&S.ring[wave][0][0]), scales = lds_address(reinterpret_cast<unsigned char*>(&S.scales[wave][0]));
@@ -417,7 +478,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
     const unsigned char* b = v_head + max(v_id1, 0) * page_bytes;
     // a page that is none of the pool's holds nothing: its scale reads as 0, what is read instead is page 0
     const int id = lane & 2 ? v_id1 : v_id0;
-    const float* at = (lane & 1 ? P.v_scale : P.k_scale) + static_cast<int64_t>(id) * P.Hkv + J.kvh;
+    const float* at = (lane & 1 ? v_scale : k_scale) + static_cast<int64_t>(id) * Hkv;
     at = id >= 0 ? at : kNoScale;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) load_to_lds(a, 16 * lane, ring + Sh::kHalf, j);
@@ -427,16 +488,20 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   };
   constexpr int kKLoads = 2 * kLoads, kVLoads = 2 * kLoads + 1;
 
-  int t = J.t0 + wave;
-  const int mine = t < J.t1 ? (J.t1 - t + kWaves - 1) / kWaves : 0;      // units of this wave
+  const bool split = !SANITIZE && J.halves == 2;
+  const int per_half = split ? kWaves / 2 : kWaves, half = split ? wave / (kWaves / 2) : 0, row0 = 16 * NB * half;    // waves; this wave's half, its first row
+  int t = J.t0 + wave - half * per_half;
+  const int mine = t < J.t1 ? (J.t1 - t + per_half - 1) >> (split ? ilog2(kWaves / 2) : ilog2(kWaves)) : 0;  // units of this wave
 
   // ---- all that the piece needs besides its pages is on its way at once, and stored before its pages are asked for ----
   // query operands: step 2 h + e, lane group g: dimensions 16 (4 h + g) + 8 e .. + 8 (what a lane's 16 bytes of K hold)
-  constexpr int kFrags = NB * 2 * kH, kMine = (kFrags + kWaves - 1) / kWaves;
+  constexpr int kMine = (2 * NB * 2 * kH + kWaves - 1) / kWaves;
+  const int frags = (split ? 2 : 1) * NB * 2 * kH;
   raw4 qv[kMine];
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
-    const int f = min(wave + j * kWaves, kFrags - 1), s = f % (2 * kH), row = J.row_base + min(16 * (f / (2 * kH)) + rn, J.rows - 1);    // (columns past the last row repeat it)
+    if (wave + j * kWaves >= frags) break;
+    const int f = wave + j * kWaves, s = f % (2 * kH), row = J.row_base + min(16 * (f / (2 * kH)) + rn, J.rows - 1);    // (columns past the last row repeat it)
     qv[j] = *reinterpret_cast<const raw4*>(P.q + query_row(P, J, row) * D + 16 * g + 64 * (s >> 1) + 8 * (s & 1));
   }
   int parent = -1;
@@ -446,13 +511,13 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   lds_sync();                                                   // the LDS of the piece before is free
 #pragma unroll
   for (int j = 0; j < kMine; ++j)
-    if (wave + j * kWaves < kFrags) S.q[wave + j * kWaves][lane] = qv[j];
+    if (wave + j * kWaves < frags) S.q[wave + j * kWaves][lane] = qv[j];
   if (tid < J.n) S.parent[tid] = parent;
   if (mine > 0) {
     issue_k(ring);
     v_id0 = k_id0; v_id1 = k_id1;
     issue_v();
-    fetch_ids(t + kWaves);
+    fetch_ids(t + per_half);
   }
   if (!SANITIZE && tid == 0) S.nans = 0;
   find_rows(P, S, J, tid);
@@ -485,6 +550,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   const unsigned k_flip = 64 * (rn >> 3);                       // sub-tile st at k_at + (64 st ^ k_flip)
   const unsigned v_at = ring + Sh::kHalf + (g >> 1) * Sh::kPageBytes + rn * 16 + 8 * (g & 1);
   const unsigned s_at = scales + 8 * (g >> 1);
+  const raw4* q_mine = &S.q[half * NB * 2 * kH][lane];
 
   // ref: what a row's weights are relative to, in log2 units; sum: of this lane's tokens; v_ref: what the results are relative to
   float ref[NB], sum[NB], v_ref = __uint_as_float(static_cast<uint32_t>(kLeastScaleExp + 127) << 23);
@@ -497,7 +563,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
     for (int d = 0; d < kDT; ++d) oacc[qi][d] = qf32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int i = 0; i < mine; ++i, t += kWaves) {
+  for (int i = 0; i < mine; ++i, t += per_half) {
     const unsigned at = 0;
     const int behind = mine - 1 - i;                            // units of this wave after this one
     // K of this unit is here: behind it the next one's K, and V
@@ -512,18 +578,19 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       kr[h][1] = *lds_raw4(k_at + at + (64u ^ k_flip) + 1024 * h);
     }
 #pragma unroll
-    for (int qi = 0; qi < kAhead; ++qi) qr[0][qi] = S.q[qi * 2 * kH][lane];
+    for (int qi = 0; qi < kAhead; ++qi) qr[0][qi] = q_mine[qi * 2 * kH * kWave];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K has been read
     if (behind > 0) issue_k(ring + at);
+    __builtin_amdgcn_s_setprio(1);                              // products before another wave's softmax
 #pragma unroll
     for (int step = 0; step < 2 * kH; ++step) {
       const int h = step >> 1, e = step & 1;
       if (step + 1 < 2 * kH) {
 #pragma unroll
-        for (int qi = 0; qi < kAhead; ++qi) qr[(step + 1) & 1][qi] = S.q[qi * 2 * kH + step + 1][lane];
+        for (int qi = 0; qi < kAhead; ++qi) qr[(step + 1) & 1][qi] = q_mine[(qi * 2 * kH + step + 1) * kWave];
       }
 #pragma unroll
-      for (int qi = kAhead; qi < NB; ++qi) qr[step & 1][qi] = S.q[qi * 2 * kH + step][lane];
+      for (int qi = kAhead; qi < NB; ++qi) qr[step & 1][qi] = q_mine[(qi * 2 * kH + step) * kWave];
       const qbf16x8 a0 = operand_bf16(kr[h][0][2 * e], kr[h][0][2 * e + 1]), a1 = operand_bf16(kr[h][1][2 * e], kr[h][1][2 * e + 1]);
 #pragma unroll
       for (int qi = 0; qi < NB; ++qi) {
@@ -534,6 +601,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     // V of this unit and its scales are here: behind them the K after next
     if (behind > 0) wait_loads<kKLoads>();
     else wait_loads<0>();
@@ -545,10 +613,10 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
     if (behind > 0) {
       v_id0 = k_id0; v_id1 = k_id1;
       issue_v();
-      fetch_ids(t + 2 * kWaves);
+      fetch_ids(t + 2 * per_half);
     }
     const bool ok = ks != 0.f;
-    const float factor = ok ? ks * P.c : 1.f;                   // (not 0: masked scores are -infinity)
+    const float factor = ok ? ks * c : 1.f;                   // (not 0: masked scores are -infinity)
 
     // ---- masks: only where the unit reaches the drafts, or a page is none ----
     const int past = t * kUnit + 16 * (g >> 1) - J.ctx;         // the lane's page starts that far behind the context
@@ -558,7 +626,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       for (int qi = 0; qi < NB; ++qi) {
         uint32_t seen = 0xffffu;
         if (past > -16) {
-          const int node = S.node[16 * qi + rn];
+          const int node = S.node[row0 + 16 * qi + rn];
           seen = page_mask(S.anc[node][0], S.anc[node][1], past);
         }
         seen = ok ? seen >> (8 * (g & 1)) : 0u;
@@ -638,6 +706,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
         if (any_lane(nans != 0u) && lane == 0) S.nans = 1;
       }
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int d = 0; d < kDT; ++d) {
       uint32_t x = vr[d].x & keep[0], y = vr[d].y & keep[1];
@@ -656,6 +725,7 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   if (!SANITIZE && !J.whole && tid == 0) open_count(J.word, count_seen, P.tag);
@@ -674,12 +744,15 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
   if constexpr (!SANITIZE) {
     if (S.nans) return;
   }
-  if (tid < 16 * NB) {
+  if (tid < 16 * NB * (split ? 2 : 1)) {
+    const int w0 = tid < 16 * NB ? 0 : kWaves / 2, local = tid < 16 * NB ? tid : tid - 16 * NB;
     float M = -INFINITY, Z = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, S.m[w][tid]);
+    for (int w = 0; w < kWaves; ++w)
+      if (w < kWaves / 2 || !split) M = fmaxf(M, S.m[w0 + w][local]);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) Z += S.m[w][tid] == -INFINITY ? 0.f : S.l[w][tid] * fast_exp2(S.m[w][tid] - M);
+    for (int w = 0; w < kWaves; ++w)
+      if (w < kWaves / 2 || !split) Z += S.m[w0 + w][local] == -INFINITY ? 0.f : S.l[w0 + w][local] * fast_exp2(S.m[w0 + w][local] - M);
     S.top[tid] = M;
     if (tid < J.rows) {
       if (J.whole) S.inv[tid] = put_lse(P, S.row[tid], M, Z);
@@ -687,25 +760,26 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
     }
   }
   lds_sync();
-  constexpr int kItems = 16 * (D / 4) / Sh::kThreads > 0 ? 16 * (D / 4) / Sh::kThreads : 1;     // of a thread and block: four dimensions of a row
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
     if (qi > 0) lds_sync();
-    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - S.top[16 * qi + rn] - static_cast<float>(kWeightBias)) * v_ref;
+    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - S.top[row0 + 16 * qi + rn] - static_cast<float>(kWeightBias)) * v_ref;
 #pragma unroll
     for (int d = 0; d < kDT; ++d)
       *reinterpret_cast<float4*>(&S.o[wave][rn][16 * d + 4 * g]) =
           make_float4(oacc[qi][d][0] * f, oacc[qi][d][1] * f, oacc[qi][d][2] * f, oacc[qi][d][3] * f);
     lds_sync();
-#pragma unroll
-    for (int item = 0; item < kItems; ++item) {
-      const int at = tid + item * Sh::kThreads, d4 = at % (D / 4), r = at / (D / 4), row = 16 * qi + r;
-      if (r >= 16 || row >= J.rows) continue;
+#pragma unroll 2
+    for (int at = tid; at < 16 * (D / 4) * (split ? 2 : 1); at += Sh::kThreads) {      // four dimensions of a row
+      const int d4 = at % (D / 4), r = at / (D / 4) % 16, other = at / (16 * (D / 4)), row = 16 * (NB * other + qi) + r;
+      if (row >= J.rows) continue;
       float4 x[kWaves], sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) x[w] = *reinterpret_cast<const float4*>(&S.o[w][r][4 * d4]);
+      for (int w = 0; w < kWaves; ++w)
+        if (w < kWaves / 2 || !split) x[w] = *reinterpret_cast<const float4*>(&S.o[other * (kWaves / 2) + w][r][4 * d4]);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
+        if (w >= kWaves / 2 && split) break;
         sum.x += x[w].x; sum.y += x[w].y; sum.z += x[w].z; sum.w += x[w].w;
       }
       if constexpr (SANITIZE) {
@@ -726,18 +800,13 @@ __device__ __forceinline__ void quant_piece(const QuantAttnParams& P, Sh& S, con
 
 // TERMS: fp16 terms of a weight.
 template <int D, int TERMS, int NW>
-__global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnParams P) {
+__global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnParams) {
+  KernelParams& P = kernel_params();
   constexpr int kMost = most_blocks(D, TERMS);
   extern __shared__ __align__(1024) unsigned char smem[];
   auto& S = *reinterpret_cast<QuantAttnShared<D, NW>*>(smem);
   const int lane = threadIdx.x & 63;
-  // Workgroups go to the 8 XCDs in turn: renumbered so that neighbouring ranges, which may hold groups of rows of one request, share an L2
-  const unsigned id = blockIdx.x, all = gridDim.x;
-  const unsigned logical = all % 8 == 0 ? (id & 7) * (all / 8) + (id >> 3) : id;
-  const int range = logical % P.ranges;
   QuantPiece J;
-  J.kvh = logical / P.ranges;
-  const int64_t pair = static_cast<int64_t>(J.kvh) * P.ranges;
   const int batches = (P.B + 63) / 64;
   int total = 0, count = 0;
   Requests r;
@@ -746,8 +815,14 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
     total += r.sum;
     count += r.count;
   }
-  const Cut cut = cut_ranges(P, total, count);
-  if (range >= cut.used) return;
+  const Cut cut = cut_ranges(P.ranges, total, count);
+  // Workgroups go to the 8 XCDs in turn: renumbered so that neighbouring ranges, which may hold groups of rows of one request, share an L2, with as
+  // many in each
+  const int all = cut.used * P.Hkv, each = (all + 7) >> 3, xcd = blockIdx.x & 7, place = blockIdx.x >> 3, logical = xcd * each + place;
+  if (place >= each || logical >= all) return;
+  J.kvh = logical / cut.used;
+  const int range = logical - J.kvh * cut.used;
+  const int64_t pair = static_cast<int64_t>(J.kvh) * P.ranges;
   const int from = range_start(cut, range), end = range_start(cut, range + 1);
   int base = 0;                                                 // cost before these 64 requests
   for (int k = 0, at = from; at < end;) {
@@ -762,8 +837,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
     const int groups = __builtin_amdgcn_readlane(r.groups, i), per = __builtin_amdgcn_readlane(r.per, i);
     Place p;
     p.units = __builtin_amdgcn_readlane(r.units, i);
-    p.cost = unit_cost(per);
-    const int behind = base + __builtin_amdgcn_readlane(r.upto, i), group_cost = kStartCost + p.units * p.cost;
+    J.halves = __builtin_amdgcn_readlane(r.halves, i);
+    p.cost = J.halves * unit_cost(per);
+    p.shift = P.shift;
+    p.head = head_cost(per);
+    const int behind = base + __builtin_amdgcn_readlane(r.upto, i), group_cost = p.head + chunks_of(p.units, p.shift) * p.cost;
     p.start = behind - groups * group_cost;
     J.b = 64 * k + i;
     J.ctx = __builtin_amdgcn_readlane(r.ctx, i);
@@ -773,32 +851,33 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
       J.t0 = first_unit(p, from);
       J.t1 = min(p.units, first_unit(p, end));
       if (J.t0 >= J.t1) continue;
-      J.row_base = 16 * per * grp;
-      J.rows = min(J.n * P.G - J.row_base, 16 * per);
+      J.row_base = 16 * per * J.halves * grp;
+      J.rows = min(J.n * P.G - J.row_base, 16 * per * J.halves);
       J.whole = J.t0 == 0 && J.t1 == p.units;
       J.part = ((pair + range) * 2 + (J.t0 == 0 ? 1 : 0)) * P.rows;
       J.word = P.arrived + (static_cast<int64_t>(J.kvh) * P.groups + grp) * P.B + J.b;
       switch (per) {
-        case 1: quant_piece<1, TERMS, false>(P, S, J); break;
-        case 2: quant_piece<2, TERMS, false>(P, S, J); break;
-        case 3: quant_piece<3, TERMS, false>(P, S, J); break;
+        case 1: quant_piece<1, TERMS, false>(S, J); break;
+        case 2: quant_piece<2, TERMS, false>(S, J); break;
+        case 3: quant_piece<3, TERMS, false>(S, J); break;
         default:
-          if constexpr (kMost >= 4) quant_piece<4, TERMS, false>(P, S, J);
+          if constexpr (kMost >= 4) quant_piece<4, TERMS, false>(S, J);
       }
       if (S.nans) {                                             // (written before a barrier, and next behind one)
         QuantPiece part = J;
+        part.halves = 1;
         for (int row = 0; row < J.rows; row += 16) {
           part.row_base = J.row_base + row;
           part.rows = min(J.rows - row, 16);
           part.part = J.part + row;
-          quant_piece<1, TERMS, true>(P, S, part);
+          quant_piece<1, TERMS, true>(S, part);
         }
         __syncthreads();
         find_rows(P, S, J, threadIdx.x);                                     // (of all rows again, for the merge)
       }
       if (!J.whole) {
         const Pieces all_pieces = pieces_of(cut, p);
-        if (last_piece(J.word, all_pieces.count, &S.last)) merge_pieces(P, S, J, pair, all_pieces);
+        if (last_piece(J.word, all_pieces.count, &S.last)) merge_pieces(S, J, pair, all_pieces);
       }
     }
     at = behind;
@@ -810,11 +889,18 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   QuantAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.Hq / a.Hkv);
   const int blocks = static_cast<int>(std::max<int64_t>(1, (rows + 15) / 16));
-  const int most = most_blocks(a.D, a.out_dtype == kF32 ? 2 : 1);
+  int most = most_blocks(a.D, a.out_dtype == kF32 ? 2 : 1);
   p.groups = (blocks + most - 1) / most;
-  p.rows = 16 * std::min(blocks, most);
+  p.halves = p.groups > 1 && static_cast<int64_t>(a.Hkv) * a.B * p.groups >= 1024 ? 2 : 1;
+  most *= p.halves;
+  p.groups = (blocks + most - 1) / most;
+  p.rows = 16 * std::min(blocks + p.halves - 1, most);
   p.waves = static_cast<int64_t>(a.Hkv) * a.B * p.groups < 512 ? 8 : 4;
   p.ranges = std::max(1, (p.waves == 8 ? 256 : 512) / a.Hkv);
+  // the cost of the batch stays below 2^31 (no chunk is long enough where there are millions of groups: shift is then 30 and the call is refused)
+  const int64_t groups = std::min<int64_t>(static_cast<int64_t>(a.B) * p.groups, static_cast<int64_t>(a.total_q) * (a.Hq / a.Hkv) / 16 + a.B);
+  const int64_t units = (static_cast<int64_t>(a.max_pages) + 1) / 2;
+  while (p.shift < kQuantMaxShift && groups * (kMostHead + ((units >> p.shift) + 1) * p.halves * kMostCost) >= (int64_t{1} << 31)) ++p.shift;
   return p;
 }
 
@@ -832,7 +918,7 @@ static int launch_quant(const QuantAttnParams& P, const AttnArgs& a, const Quant
   constexpr size_t lds = sizeof(QuantAttnShared<D, NW>);
   static_assert(lds <= (NW == 8 ? 160 : 80) * 1024, "two workgroups of four waves, or one of eight, to a compute unit");
   if (lds > 65536 && set_lds_once(attn_quant_kernel<D, TERMS, NW>, lds, lds_set) != 0) return -6;
-  hipLaunchKernelGGL((attn_quant_kernel<D, TERMS, NW>), dim3(p.ranges * a.Hkv), dim3(NW * kWave), lds, stream, P);
+  hipLaunchKernelGGL((attn_quant_kernel<D, TERMS, NW>), dim3((p.ranges * a.Hkv + 7) / 8 * 8), dim3(NW * kWave), lds, stream, P);
   return 0;
 }
 template <int D, int TERMS>
@@ -856,7 +942,7 @@ int launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_sc
   }
   P.B = a.B; P.Hq = a.Hq; P.Hkv = a.Hkv; P.G = a.Hq / a.Hkv; P.inverse_G = ((1u << 31) + P.G - 1) / P.G; P.total_q = a.total_q; P.max_q = std::min(a.max_q, kQaMaxNodes);
   P.max_pages = a.max_pages; P.num_pages = num_pages;
-  P.ranges = p.ranges; P.groups = p.groups; P.rows = p.rows;
+  P.ranges = p.ranges; P.groups = p.groups; P.rows = p.rows; P.halves = p.halves; P.shift = p.shift;
   P.c = a.scale * kLog2e; P.out_f32 = a.out_dtype == kF32;
   if (a.D == 128) return P.out_f32 ? launch_quant_waves<128, 2>(P, a, p, stream) : launch_quant_waves<128, 1>(P, a, p, stream);
   return P.out_f32 ? launch_quant_waves<64, 2>(P, a, p, stream) : launch_quant_waves<64, 1>(P, a, p, stream);

@@ -231,10 +231,13 @@ int launch_attn(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);   
 
 // ---- attn_quant.hip ---------------------------------------------------------------
 // A pure function of the descriptor, as AttnPlan.
+constexpr int kQuantMaxShift = 30;
 struct QuantAttnPlan {
-  int rows;           // query rows a workgroup takes at a time, at most (16 .. 64)
+  int rows;           // query rows a workgroup takes at a time, at most (16 .. 128)
   int groups;         // ... groups of so many that cover a request's rows
+  int halves;         // 2: of more rows than a wave takes, each half of a workgroup's waves takes half
   int waves;          // of a workgroup: 4 or 8
+  int shift;          // units of the tokens come in chunks of 2^shift
   int ranges;         // workgroups per KV head: ranges of the batch's tokens and groups of equal cost
 };
 QuantAttnPlan make_quant_attn_plan(const AttnArgs& a);
