@@ -412,67 +412,92 @@ def make_append_desc(batch, num_q_heads, num_kv_heads, head_dim, total_q, max_q_
                           num_pages, rotary_dim, int(interleaved), rotary_scale)
 
 
+_types = None
+
+
+def _tensor_types():
+    # looked up once: an import statement and three attributes of torch cost 0.4 us a call
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.int32, torch.float32, torch.bfloat16)
+    return _types
+
+
 def _typed(t, dtype, what):
     """The pointer of a contiguous tensor of that type (None: NULL); another type would be read as this one's bits."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} expected, not {t.dtype}")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise AssertionError("tensors handed to the library must be contiguous")
+    return t.data_ptr()
+
+
+def _stream_beside(stream, t) -> int:
+    """The stream's handle (None: the current one); the cache `t` has to lie on its device."""
+    at = t.get_device()
+    if at >= 0:
+        import torch
+        on = torch.cuda.current_device() if stream is None else stream.device_index
+        if on != at:
+            raise ValueError(f"the cache lies on device {at}, the stream belongs to device {on}")
+    return _stream(stream)
 
 
 def _rows(t, heads, head_dim, rows, what):
     """(pointer, elements between tokens) of a [tokens, heads, head_dim] bf16 tensor whose tokens may lie apart."""
-    import torch
     if t is None:
         return None, 0
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not _tensor_types()[2]:
         raise TypeError(f"{what}: torch.bfloat16 expected, not {t.dtype}")
-    if tuple(t.shape) != (rows, heads, head_dim) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+    apart, head, one = t.stride()                     # (ValueError for another number of dimensions)
+    if t.shape != (rows, heads, head_dim) or one != 1 or (heads > 1 and head != head_dim):
         raise ValueError(f"{what}: [{rows}, {heads}, {head_dim}] with contiguous heads expected")
-    return t.data_ptr(), t.stride(0) if rows > 1 else heads * head_dim
+    return t.data_ptr(), apart if rows > 1 else heads * head_dim
 
 
 def _quant_pools(k_pool, v_pool, k_scale, v_scale):
     """Pointers of an 8-bit cache: k_pool [num_pages, Hkv, D / 16, 16, 16] and v_pool [num_pages, Hkv, D, 16] of torch.float8_e4m3fn
     or torch.uint8, scales [num_pages, Hkv] float32."""
-    import torch
     if k_pool.element_size() != 1 or v_pool.element_size() != 1:
         raise TypeError("the pools of the 8-bit cache have one byte per entry")
     pages, heads, dim, page = v_pool.shape
-    if tuple(k_pool.shape) != (pages, heads, dim // 16, page, 16) or tuple(k_scale.shape) != (pages, heads) or k_scale.shape != v_scale.shape:
+    if k_pool.shape != (pages, heads, dim // 16, page, 16) or k_scale.shape != (pages, heads) or v_scale.shape != (pages, heads):
         raise ValueError("k_pool [num_pages, Hkv, D / 16, 16, 16], v_pool [num_pages, Hkv, D, 16] and scales [num_pages, Hkv] expected")
-    return (_ptr(k_pool), _ptr(v_pool), _typed(k_scale, torch.float32, "k_scale"), _typed(v_scale, torch.float32, "v_scale"))
+    f32 = _tensor_types()[1]
+    return (_ptr(k_pool), _ptr(v_pool), _typed(k_scale, f32, "k_scale"), _typed(v_scale, f32, "v_scale"))
 
 
 def _append(fn, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream):
-    import torch
-    D, i32 = desc.head_dim, torch.int32
-    qp, qs = _rows(q, desc.num_q_heads, D, desc.total_q, "q")
-    kp, ks = _rows(k, desc.num_kv_heads, D, desc.total_q, "k")
-    vp, vs = _rows(v, desc.num_kv_heads, D, desc.total_q, "v")
-    rc = getattr(lib(), fn)(ctypes.byref(desc), qp, qs, kp, ks, vp, vs, _typed(inv_freq, torch.float32, "inv_freq"),
-                            _typed(positions, i32, "positions"), *pools, _typed(block_table, i32, "block_table"),
-                            _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"), _typed(parent, i32, "parent"),
-                            _typed(q_out, torch.bfloat16, "q_out"), _stream(stream))
+    i32, f32, bf16 = _tensor_types()
+    D, total, Hkv = desc.head_dim, desc.total_q, desc.num_kv_heads
+    qp, qs = _rows(q, desc.num_q_heads, D, total, "q")
+    kp, ks = _rows(k, Hkv, D, total, "k")
+    vp, vs = _rows(v, Hkv, D, total, "v")
+    rc = fn(desc, qp, qs, kp, ks, vp, vs, _typed(inv_freq, f32, "inv_freq"), _typed(positions, i32, "positions"), *pools,
+            _typed(block_table, i32, "block_table"), _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
+            _typed(parent, i32, "parent"), _typed(q_out, bf16, "q_out"), stream)
     if rc != SPEC_OK:
-        raise SpecError(fn, rc)
+        raise SpecError(fn.__name__, rc)
 
 
 def spec_append_kv(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, block_table, ctx_len, q_offsets, parent, q_out,
                    positions=None, stream=None) -> None:
     """Device tensors: q [total_q, Hq, D], k and v [total_q, Hkv, D] bf16 (tokens may lie apart, as slices of one projection do),
     inv_freq [rotary_dim / 2] float32, pools [num_pages, Hkv, 16, D] bf16 (modified), the rest int32; q_out [total_q, Hq, D] bf16."""
-    import torch
-    pools = (_typed(k_pool, torch.bfloat16, "k_pool"), _typed(v_pool, torch.bfloat16, "v_pool"))
-    _append("spec_append_kv", desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream)
+    bf16 = _tensor_types()[2]
+    pools = (_typed(k_pool, bf16, "k_pool"), _typed(v_pool, bf16, "v_pool"))
+    _append(lib().spec_append_kv, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions,
+            _stream_beside(stream, k_pool))
 
 
 def spec_append_kv_quant(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets,
                          parent, q_out, positions=None, stream=None) -> None:
     """spec_append_kv into an 8-bit cache (pools and scales modified)."""
-    _append("spec_append_kv_quant", desc, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale), block_table, ctx_len,
-            q_offsets, parent, q_out, positions, stream)
+    _append(lib().spec_append_kv_quant, desc, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale), block_table, ctx_len,
+            q_offsets, parent, q_out, positions, _stream_beside(stream, k_pool))
 
 
 def spec_verify_attn_quant_workspace_size(desc: SpecAttnDesc) -> int:
@@ -482,15 +507,13 @@ def spec_verify_attn_quant_workspace_size(desc: SpecAttnDesc) -> int:
 def spec_verify_attn_quant(desc: SpecAttnDesc, q, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, out,
                            lse=None, workspace=None, stream=None) -> None:
     """spec_verify_attn over an 8-bit cache; workspace uint8 of at least spec_verify_attn_quant_workspace_size(desc) bytes."""
-    import torch
-    i32 = torch.int32
+    i32, f32, bf16 = _tensor_types()
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().spec_verify_attn_quant(ctypes.byref(desc), k_pool.shape[0], _typed(q, torch.bfloat16, "q"),
+    rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _typed(q, bf16, "q"),
                                       *_quant_pools(k_pool, v_pool, k_scale, v_scale), _typed(block_table, i32, "block_table"),
                                       _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
-                                      _typed(parent, i32, "parent"),
-                                      _typed(out, torch.float32 if desc.out_dtype == SPEC_F32 else torch.bfloat16, "out"),
-                                      _typed(lse, torch.float32, "lse"), _ptr(workspace), ws_bytes, _stream(stream))
+                                      _typed(parent, i32, "parent"), _typed(out, f32 if desc.out_dtype == SPEC_F32 else bf16, "out"),
+                                      _typed(lse, f32, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, k_pool))
     if rc != SPEC_OK:
         raise SpecError("spec_verify_attn_quant", rc)
 
@@ -506,13 +529,12 @@ def spec_describe_attn_quant_plan(desc: SpecAttnDesc) -> str:
 def spec_compact_kv_quant(k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, stop_node, new_len=None,
                           stream=None) -> None:
     """spec_compact_kv over an 8-bit cache (pools and scales modified in place); the rest int32 device tensors."""
-    import torch
-    i32 = torch.int32
+    i32 = _tensor_types()[0]
     pages, heads, dim, page = v_pool.shape
     rc = lib().spec_compact_kv_quant(ctx_len.shape[0], heads, dim, page, block_table.shape[1], pages,
                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale), _typed(block_table, i32, "block_table"),
                                      _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
                                      _typed(parent, i32, "parent"), _typed(stop_node, i32, "stop_node"),
-                                     _typed(new_len, i32, "new_len"), _stream(stream))
+                                     _typed(new_len, i32, "new_len"), _stream_beside(stream, k_pool))
     if rc != SPEC_OK:
         raise SpecError("spec_compact_kv_quant", rc)

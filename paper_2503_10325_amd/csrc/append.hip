@@ -14,6 +14,8 @@
 //
 // 8-bit cache (quant.h): one wave takes the K or V of one (page, head): the largest entry, the scale, the codes; entries that the page
 // already holds are rewritten where the scale grows.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "quant.h"
@@ -43,6 +45,7 @@ struct AppendParams {
   uint16_t* q_out;
   int B, Hq, Hkv, total_q, max_pages, num_pages, rotary, interleaved;
   float rotary_scale;
+  int kv_shares, q_shares;
 };
 
 // The new tokens of one page: request, first token (row of q, k, v) and first slot, how many, the pool page (-1: none).
@@ -273,14 +276,25 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P) 
   __shared__ __align__(16) float2 sh_cs[kQuantPage][kAngleStride];
   __shared__ int sh_parent[kAppendMaxTree];
   __shared__ int sh_pos[kQuantPage];
+  __shared__ float sh_freq[64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   PageRun R;
-  R.b = __builtin_amdgcn_readfirstlane(request_of_slot(P.q_offsets, P.B, blockIdx.x, lane));
-  R.first = P.q_offsets[R.b];
-  R.n = min(P.q_offsets[R.b + 1], P.total_q) - R.first;
+  if (P.B <= kWave) {                                           // one load for which request it is and what there is to know of it
+    const int b = min(lane, P.B - 1), off = P.q_offsets[b], next = P.q_offsets[b + 1], ctx = P.ctx_len[b];
+    const bool le = lane < P.B && (off >> 4) + 2 * lane <= static_cast<int>(blockIdx.x);
+    R.b = max(__popcll(__builtin_amdgcn_ballot_w64(le)) - 1, 0);
+    R.first = __builtin_amdgcn_readlane(off, R.b);
+    R.n = __builtin_amdgcn_readlane(next, R.b);
+    R.ctx = __builtin_amdgcn_readlane(ctx, R.b);
+  } else {
+    R.b = __builtin_amdgcn_readfirstlane(request_of_slot(P.q_offsets, P.B, blockIdx.x, lane));
+    R.first = P.q_offsets[R.b];
+    R.n = P.q_offsets[R.b + 1];
+    R.ctx = P.ctx_len[R.b];
+  }
+  R.n = min(R.n, P.total_q) - R.first;
   if (P.parent) R.n = min(R.n, kAppendMaxTree);
-  R.ctx = P.ctx_len[R.b];
   if (R.ctx < 0 || R.first < 0) return;
   const int64_t lp64 = static_cast<int64_t>(R.ctx >> 4) + (static_cast<int>(blockIdx.x) - (R.first >> 4) - 2 * R.b);
   const int64_t from = max(static_cast<int64_t>(R.ctx), 16 * lp64), to = min(static_cast<int64_t>(R.ctx) + R.n, 16 * lp64 + 16);
@@ -289,41 +303,48 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P) 
   R.slot0 = static_cast<int>(from & 15);
   R.row0 = R.first + static_cast<int>(from - R.ctx);
   R.page = lp64 < P.max_pages ? P.block_table[static_cast<int64_t>(R.b) * P.max_pages + lp64] : -1;
-  if (R.page < 0 || R.page >= P.num_pages) R.page = -1;
 
-  // ---- angles of the page's tokens ----
+  // ---- angles of the page's tokens: what they take is asked for at once ----
   const int half = P.rotary >> 1;
+  const bool tree = half > 0 && P.positions == nullptr && P.parent;
+  const int up = tree && tid < R.n ? P.parent[R.first + tid] : -1;
+  const int given = half > 0 && P.positions && tid < R.count ? P.positions[R.row0 + tid] : 0;
+  const float freq = tid < half ? P.inv_freq[tid] : 0.f;
   if (half > 0) {
-    if (P.positions == nullptr && P.parent) {
-      if (tid < R.n) sh_parent[tid] = P.parent[R.first + tid];
-      __syncthreads();
-    }
-    if (tid < R.count) {
-      const int i = R.row0 - R.first + tid;
-      int depth = i;
-      if (P.positions == nullptr && P.parent) {
-        depth = 0;
+    if (tid < half) sh_freq[tid] = freq;
+    const int i = R.row0 - R.first + tid;
+    if (tree) {
+      if (tid < R.n) sh_parent[tid] = up;
+      lds_sync();
+      if (tid < R.count) {
+        int depth = 0;
         for (int a = i; depth < kAppendMaxTree; ++depth) {
           const int p = sh_parent[a];
           if (p < 0 || p >= a) break;                           // (a malformed entry is a root)
           a = p;
         }
+        sh_pos[tid] = R.ctx + depth;
       }
-      sh_pos[tid] = P.positions ? P.positions[R.row0 + tid] : R.ctx + depth;
+    } else if (tid < R.count) {
+      sh_pos[tid] = P.positions ? given : R.ctx + i;
     }
-    __syncthreads();
+    lds_sync();
     for (int at = tid; at < R.count * half; at += kAppendThreads) {
       const int t = at / half, p = at - t * half;
-      const double turns = static_cast<double>(sh_pos[t]) * static_cast<double>(P.inv_freq[p]) * 0.15915494309189535;
+      const double turns = static_cast<double>(sh_pos[t]) * static_cast<double>(sh_freq[p]) * 0.15915494309189535;
       const float2 w = cos_sin_turns(turns);
       sh_cs[t][p] = make_float2(w.x * P.rotary_scale, w.y * P.rotary_scale);
     }
-    __syncthreads();
+    lds_sync();
   }
 
-  const int share = blockIdx.y, shares = gridDim.y;
+  if (R.page < 0 || R.page >= P.num_pages) R.page = -1;
+
+  // of a page's workgroups, kv_shares take keys and values (and queries, if q_shares is 0), q_shares queries
+  const bool rows_only = static_cast<int>(blockIdx.y) >= P.kv_shares;
+  const int share = rows_only ? blockIdx.y - P.kv_shares : blockIdx.y, shares = rows_only ? P.q_shares : P.kv_shares;
   if constexpr (QUANT) {
-    if (R.page >= 0) {
+    if (R.page >= 0 && !rows_only) {
       const int jobs = 2 * P.Hkv;
       const int end = static_cast<int>(static_cast<int64_t>(jobs) * (share + 1) / shares);
       for (int j = static_cast<int>(static_cast<int64_t>(jobs) * share / shares) + wave; j < end; j += kAppendWaves) {
@@ -334,6 +355,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P) 
   }
 
   // ---- rows of queries (and of keys and values of the bf16 cache): 32 bytes per lane, the partners of a rotation together ----
+  if (P.q_shares > 0 && !rows_only) return;
   const int q_heads = P.q_out ? P.Hq : 0;
   const int heads = QUANT ? q_heads : q_heads + 2 * P.Hkv;
   const int h0 = static_cast<int>(static_cast<int64_t>(heads) * share / shares);
@@ -410,12 +432,18 @@ void launch_append(const AppendArgs& a, bool quant, hipStream_t stream) {
   P.B = a.B; P.Hq = a.Hq; P.Hkv = a.Hkv; P.total_q = a.total_q; P.max_pages = a.max_pages; P.num_pages = a.num_pages;
   P.rotary = a.rotary; P.interleaved = a.interleaved; P.rotary_scale = a.rotary_scale;
   const int64_t slots = static_cast<int64_t>(a.total_q) / kQuantPage + 2 * static_cast<int64_t>(a.B);
-  // shares of the heads: as many as fill the chip with few slots, one where slots are many (the angles are worked out once per share)
-  int64_t shares = 1;
-  const int most = quant ? max(1, 2 * a.Hkv / kAppendWaves) : max(1, (a.Hq + 2 * a.Hkv) / 8);
-  while (shares < most && slots * shares < 2048) shares *= 2;
-  shares = shares < most ? shares : most;
-  const dim3 grid(static_cast<unsigned>(slots), static_cast<unsigned>(shares));
+  // shares of the heads: as many as fill the chip with few slots, one where slots are many (the angles are worked out once per share).  With few
+  // slots, the 8-bit cache's queries have workgroups of their own beside those of its keys and values: one piece of work per wave, and latency
+  // is what counts (64 requests of up to 10 tokens, 64 and 8 heads: 15.2 -> 11.6 us; for prompts, bound by memory, no gain).
+  auto shares_of = [&](int64_t most) {
+    int64_t n = 1;
+    while (n < most && slots * n < (quant ? 1024 : 2048)) n *= 2;
+    return static_cast<int>(std::min(n, most));
+  };
+  const int q_heads = P.q_out ? a.Hq : 0;
+  P.kv_shares = quant ? shares_of(std::max(1, 2 * a.Hkv / kAppendWaves)) : shares_of(std::max(1, (a.Hq + 2 * a.Hkv) / 8));
+  P.q_shares = quant && q_heads > 0 && slots < 1024 ? shares_of(std::max(1, q_heads / 8)) : 0;
+  const dim3 grid(static_cast<unsigned>(slots), static_cast<unsigned>(P.kv_shares + P.q_shares));
   if (a.D == 128) {
     if (quant) hipLaunchKernelGGL((append_kernel<128, true>), grid, dim3(kAppendThreads), 0, stream, P);
     else hipLaunchKernelGGL((append_kernel<128, false>), grid, dim3(kAppendThreads), 0, stream, P);
