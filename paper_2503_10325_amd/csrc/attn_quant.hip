@@ -86,14 +86,19 @@ __device__ __forceinline__ T keep_scalar(T x) {
   return x;
 }
 
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    x += lane >= d ? y : 0;
-  }
-  return x;
+// Sum over the lanes up to this one: within rows of 16 lanes, then over rows (no trip through LDS).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_lane(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true); }
+__device__ __forceinline__ int wave_scan(int x) {
+  x = add_lane<0x111, 0xf>(x);                                  // from the lane 1, 2, 4, 8 before
+  x = add_lane<0x112, 0xf>(x);
+  x = add_lane<0x114, 0xf>(x);
+  x = add_lane<0x118, 0xf>(x);
+  x = add_lane<0x142, 0xa>(x);                                  // lane 15 to the second row, 47 to the fourth
+  return add_lane<0x143, 0xc>(x);                               // lane 31 to the third and fourth
 }
+// n / d for results below 2^12 and d up to 2^9, for d = 1, and for n up to 2^9: half a unit of n is more than the rounding of reciprocal and product.
+__device__ __forceinline__ int small_div(int n, int d) { return static_cast<int>((static_cast<float>(n) + 0.5f) * __builtin_amdgcn_rcpf(static_cast<float>(d))); }
 
 // A request's 16-row blocks in groups, alike: `per` blocks for each wave (at most `most`), with `halves` = 2 of other blocks for the second half of
 // a workgroup's waves, which then share the units' bytes.
@@ -104,9 +109,9 @@ __device__ __forceinline__ RowGroups group_rows(int rows, int most, int halves) 
   const int blocks = (rows + 15) >> 4;
   RowGroups r;
   r.halves = blocks > most ? halves : 1;
-  most *= r.halves;
-  r.groups = (blocks + most - 1) / most;
-  const int each = (blocks + r.groups - 1) / max(r.groups, 1);
+  r.groups = r.halves == 2 ? (blocks + 2 * most - 1) / (2 * most) : (blocks + most - 1) / most;
+  const float groups = static_cast<float>(max(r.groups, 1));    // (at most 8 blocks each: the quotient is exact)
+  const int each = static_cast<int>((static_cast<float>(blocks) + groups - 0.5f) * __builtin_amdgcn_rcpf(groups));
   r.per = (each + r.halves - 1) / r.halves;
   return r;
 }
@@ -142,9 +147,9 @@ __device__ __forceinline__ Requests load_requests(KernelParams& P, int k, int mo
   r.groups = g.groups;
   r.per = g.per;
   r.halves = g.halves;
-  r.upto = wave_scan(r.groups * (head_cost(r.per) + chunks_of(r.units, P.shift) * r.halves * unit_cost(r.per)), lane);
+  r.upto = wave_scan(r.groups * (head_cost(r.per) + chunks_of(r.units, P.shift) * r.halves * unit_cost(r.per)));
   r.sum = __builtin_amdgcn_readlane(r.upto, 63);
-  r.count = __builtin_amdgcn_readlane(wave_scan(r.groups, lane), 63);
+  r.count = __builtin_amdgcn_readlane(wave_scan(r.groups), 63);
   return r;
 }
 
@@ -158,14 +163,14 @@ __device__ __forceinline__ Cut cut_ranges(int most, int total, int count) {
   const float group = static_cast<float>(total) / static_cast<float>(max(count, 1));
   const float least = fmaxf(kLeastRange, kRangeRoot * __builtin_amdgcn_sqrtf(group));
   c.used = min(max(max(static_cast<int>(static_cast<float>(total) / least), count), 1), most);
-  const int alike = c.used - c.used % max(count, 1);            // as many for each group
+  const int alike = small_div(c.used, max(count, 1)) * max(count, 1);      // as many for each group
   if (4 * alike >= 3 * c.used) c.used = alike;
-  c.used = __builtin_amdgcn_readfirstlane(c.used);
+  c.used = __builtin_amdgcn_readfirstlane(c.used);              // (worked out in vector registers)
   c.each = total / c.used;
   c.more = total - c.each * c.used;
   return c;
 }
-__device__ __forceinline__ int range_start(const Cut& c, int s) { return s * c.each + s * c.more / c.used; }
+__device__ __forceinline__ int range_start(const Cut& c, int s) { return s * c.each + __builtin_amdgcn_readfirstlane(small_div(s * c.more, keep_scalar(c.used))); }
 __device__ __forceinline__ int range_of(const Cut& c, int at) {
   int s = at / (c.each + 1);                                    // at most two too low (ranges cost at least as much as there are)
   while (s + 1 < c.used && range_start(c, s + 1) <= at) ++s;
@@ -493,7 +498,7 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
   int t = J.t0 + wave - half * per_half;
   const int mine = t < J.t1 ? (J.t1 - t + per_half - 1) >> (split ? ilog2(kWaves / 2) : ilog2(kWaves)) : 0;  // units of this wave
 
-  // ---- all that the piece needs besides its pages is on its way at once, and stored before its pages are asked for ----
+  // ---- all that the piece needs besides its pages is on its way at once, and its first pages behind it ----
   // query operands: step 2 h + e, lane group g: dimensions 16 (4 h + g) + 8 e .. + 8 (what a lane's 16 bytes of K hold)
   constexpr int kMine = (2 * NB * 2 * kH + kWaves - 1) / kWaves;
   const int frags = (split ? 2 : 1) * NB * 2 * kH;
@@ -509,10 +514,6 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
   const unsigned long long count_seen = SANITIZE || J.whole || tid > 0 ? 0ull : ld_dev(J.word);
   if (mine > 0) fetch_ids(t);
   lds_sync();                                                   // the LDS of the piece before is free
-#pragma unroll
-  for (int j = 0; j < kMine; ++j)
-    if (wave + j * kWaves < frags) S.q[wave + j * kWaves][lane] = qv[j];
-  if (tid < J.n) S.parent[tid] = parent;
   if (mine > 0) {
     issue_k(ring);
     v_id0 = k_id0; v_id1 = k_id1;
@@ -521,6 +522,10 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
   }
   if (!SANITIZE && tid == 0) S.nans = 0;
   find_rows(P, S, J, tid);
+#pragma unroll
+  for (int j = 0; j < kMine; ++j)
+    if (wave + j * kWaves < frags) S.q[wave + j * kWaves][lane] = qv[j];
+  if (tid < J.n) S.parent[tid] = parent;
   if (touches_drafts) {
     lds_sync();
     if (tid < kQaMaxNodes) {
@@ -820,7 +825,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
   // many in each
   const int all = cut.used * P.Hkv, each = (all + 7) >> 3, xcd = blockIdx.x & 7, place = blockIdx.x >> 3, logical = xcd * each + place;
   if (place >= each || logical >= all) return;
-  J.kvh = logical / cut.used;
+  J.kvh = __builtin_amdgcn_readfirstlane(small_div(logical, cut.used));
   const int range = logical - J.kvh * cut.used;
   const int64_t pair = static_cast<int64_t>(J.kvh) * P.ranges;
   const int from = range_start(cut, range), end = range_start(cut, range + 1);
