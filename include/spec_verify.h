@@ -442,11 +442,12 @@ int32_t spec_append_kv(
  *
  * spec_verify_attn_quant is spec_verify_attn over it: same descriptor, masks and results
  * (at most 128 nodes per request, one for plain decoding; at most 1024 query heads per
- * KV head).  Positions whose page is
+ * KV head, and 1.6 million requests times groups of 48 to 128 query rows of a KV head:
+ * SPEC_ERR_UNSUPPORTED otherwise).  Positions whose page is
  * outside [0, num_pages), or behind max_pages_per_req pages, count as not there; a row
  * that sees no position at all gives zeros and lse = -infinity.  Slots behind the last
  * draft are read but take no part, whatever they hold; an entry of a draft that is NaN
- * reaches the rows that see that draft only.  Entries of v below 2^-39 of the largest
+ * reaches the rows that see that draft only.  Entries of v below 2^-35 of the largest
  * scale of v in the context may lose precision.  out is exact to about 2^-12 (fp32: 2^-20)
  * of its row's size before it is rounded.  The workspace need not be cleared.
  *

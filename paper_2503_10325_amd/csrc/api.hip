@@ -450,7 +450,8 @@ int32_t spec_append_kv_quant(const spec_append_desc* desc, const void* q, int64_
 size_t spec_verify_attn_quant_workspace_size(const spec_attn_desc* desc) {
   if (check_attn_desc(desc) != SPEC_OK || desc->num_q_heads / desc->num_kv_heads > kQuantMaxGroup) return 0;
   const AttnArgs a = attn_args_from(desc);
-  return quant_attn_workspace_bytes(a, make_quant_attn_plan(a));
+  const QuantAttnPlan p = make_quant_attn_plan(a);
+  return p.shift >= kQuantMaxShift ? 0 : quant_attn_workspace_bytes(a, p);
 }
 
 int32_t spec_verify_attn_quant(const spec_attn_desc* desc, int32_t num_pages, const void* q, const void* k_pool, const void* v_pool,
@@ -486,6 +487,7 @@ int32_t spec_describe_attn_quant_plan(const spec_attn_desc* desc, char* buf, siz
   const AttnArgs a = attn_args_from(desc);
   if (desc->num_q_heads / desc->num_kv_heads > kQuantMaxGroup) return SPEC_ERR_UNSUPPORTED;
   const QuantAttnPlan p = make_quant_attn_plan(a);
+  if (p.shift >= kQuantMaxShift) return SPEC_ERR_UNSUPPORTED;
   snprintf(buf, buf_bytes, "attn_quant_kernel<%d, %d, %d>: %d query rows at a time, %d group(s) of them, %d range(s) of the tokens per KV head",
            a.D, a.out_dtype == SPEC_F32 ? 2 : 1, p.waves, p.rows, p.groups, p.ranges);
   return SPEC_OK;

@@ -115,13 +115,15 @@ __device__ __forceinline__ RowGroups group_rows(int rows, int most, int halves) 
   r.per = (each + r.halves - 1) / r.halves;
   return r;
 }
-// What a unit costs its workgroup by the 16-row blocks it is multiplied with, and what a group of rows costs besides: its start and its end.
+// What a unit costs its workgroup by the 16-row blocks it is multiplied with, and what a group of rows costs besides (its start, its end and its share
+// of merges: 10 to 15 us beside another workgroup's units, of which there are two in a microsecond).  300 + 60 blocks in place of it: 5 requests
+// of 1001 to 15999 tokens 25.8 -> 28.6 us, the serving batch of 64 alike.
 __device__ __forceinline__ int unit_cost(int blocks) { return 24 + 4 * blocks; }
 // Units are counted in chunks of 2^shift (0 unless the block table has room for so many that the batch's cost would pass 31 bits).
 __device__ __forceinline__ int chunks_of(int units, int shift) { return (units + (1 << shift) - 1) >> shift; }
 constexpr int kMostCost = 24 + 4 * kQaBlocks;
-__device__ __forceinline__ int head_cost(int blocks) { return 300 + 60 * blocks; }
-constexpr int kMostHead = 300 + 60 * kQaBlocks;
+__device__ __forceinline__ int head_cost(int blocks) { return 600 + 150 * blocks; }
+constexpr int kMostHead = 600 + 150 * kQaBlocks;
 constexpr int kWholeCost = 456;               // a group whose units cost at most this (16 of few rows) is not cut: its merge would take longer
 constexpr int kLeastRange = 256;              // ranges cost at least this, and
 constexpr float kRangeRoot = 7.5f;            // this times the root of what a group costs (or as much as a group): n pieces of a group take a time of group / n
@@ -129,27 +131,26 @@ constexpr float kRangeRoot = 7.5f;            // this times the root of what a g
 
 // The requests, 64 at a time: lane i holds request 64 k + i.
 struct Requests {
-  int ctx, first, n, units, groups, per, halves;        // of this lane's request
+  int ctx, first, n;                            // of this lane's request
   int upto;                                     // cost up to its end, within these 64
   int sum, count;                               // cost of these 64, and their groups
 };
+__device__ __forceinline__ int units_of(KernelParams& P, int ctx, int n) {
+  return n > 0 ? min(static_cast<int>((static_cast<unsigned>(ctx) + n + kUnit - 1) / kUnit), (P.max_pages >> 1) + (P.max_pages & 1)) : 0;
+}
 __device__ __forceinline__ Requests load_requests(KernelParams& P, int k, int most, int lane) {
   Requests r;
   const int b = 64 * k + lane;
   r.ctx = r.first = r.n = 0;
   if (b < P.B) {
-    r.ctx = max(P.ctx_len[b], 0);
+    r.ctx = min(max(P.ctx_len[b], 0), 0x7fffff00);              // (the end of the drafts still fits)
     r.first = P.q_offsets[b];
-    r.n = max(min(min(P.q_offsets[b + 1], P.total_q) - r.first, P.max_q), 0);
+    r.n = r.first < 0 ? 0 : max(min(min(P.q_offsets[b + 1], P.total_q) - r.first, P.max_q), 0);
   }
-  r.units = r.n > 0 ? min(static_cast<int>((static_cast<unsigned>(r.ctx) + r.n + kUnit - 1) / kUnit), (P.max_pages + 1) / 2) : 0;
   const RowGroups g = group_rows(r.n * P.G, most, P.halves);
-  r.groups = g.groups;
-  r.per = g.per;
-  r.halves = g.halves;
-  r.upto = wave_scan(r.groups * (head_cost(r.per) + chunks_of(r.units, P.shift) * r.halves * unit_cost(r.per)));
+  r.upto = wave_scan(g.groups * (head_cost(g.per) + chunks_of(units_of(P, r.ctx, r.n), P.shift) * g.halves * unit_cost(g.per)));
   r.sum = __builtin_amdgcn_readlane(r.upto, 63);
-  r.count = __builtin_amdgcn_readlane(wave_scan(r.groups), 63);
+  r.count = __builtin_amdgcn_readlane(wave_scan(g.groups), 63);
   return r;
 }
 
@@ -176,26 +177,27 @@ __device__ __forceinline__ int range_of(const Cut& c, int at) {
   while (s + 1 < c.used && range_start(c, s + 1) <= at) ++s;
   return s;
 }
-// A group of a request's rows that starts at `start` has its units there if it is not cut, else unit 0 there and unit k at start + head + k * cost; a
-// unit belongs to the range that its place is in.  (Chunks, where units come in chunks.)  Ranges cost more than any unit, so those behind the second unit's hold one each.
+// A group of a request's rows that starts at `start` has unit k at start + head + k * cost, or all of them at start + head if it is not cut; a unit
+// belongs to the range that its place is in.  (Chunks, where units come in chunks.)  Ranges cost more than any unit: the pieces of a group lie in
+// consecutive ranges.
 struct Place {
   int start, head, units, cost, shift;          // cost: of a unit
 };
 __device__ __forceinline__ bool is_whole(const Place& p) { return chunks_of(p.units, p.shift) * p.cost <= kWholeCost; }
 __device__ __forceinline__ int first_unit(const Place& p, int at) {           // at or behind `at`
-  if (at <= p.start) return 0;
+  const int ahead = at - p.start - p.head;
+  if (ahead <= 0) return 0;
   if (is_whole(p)) return p.units;
-  return min(max(1, (at - p.start - p.head + p.cost - 1) / p.cost), chunks_of(p.units, p.shift)) << p.shift;
+  return min((ahead + p.cost - 1) / p.cost, chunks_of(p.units, p.shift)) << p.shift;
 }
-// The pieces of a group that is cut: piece 0 in range `first`, the others in `rest` and those behind it.
+// The pieces of a group that is cut: their first range and how many.
 struct Pieces {
-  int first, rest, count;
+  int first, count;
 };
 __device__ __forceinline__ Pieces pieces_of(const Cut& c, const Place& p) {
   Pieces r;
-  r.first = range_of(c, p.start);
-  r.rest = max(range_of(c, p.start + p.head + p.cost), r.first + 1);
-  r.count = 1 + max(range_of(c, p.start + p.head + (chunks_of(p.units, p.shift) - 1) * p.cost) - r.rest + 1, 0);
+  r.first = range_of(c, p.start + p.head);
+  r.count = range_of(c, p.start + p.head + (chunks_of(p.units, p.shift) - 1) * p.cost) - r.first + 1;
   return r;
 }
 
@@ -368,7 +370,7 @@ __device__ __forceinline__ void merge_pieces(Sh& S, const QuantPiece& J, int64_t
   constexpr int D = Sh::D, kThreads = Sh::kThreads;
   const int tid = threadIdx.x;
   const int pieces = all.count;
-  auto part = [&](int i) { return ((pair + (i == 0 ? all.first : all.rest + i - 1)) * 2 + (i == 0 ? 1 : 0)) * P.rows; };
+  auto part = [&](int i) { return ((pair + all.first + i) * 2 + (i == 0 ? 1 : 0)) * P.rows; };
   const int chunk = min(J.rows, max(1, kMergeRoom / pieces));
   for (int r0 = 0; r0 < J.rows; r0 += chunk) {
     const int rows = min(chunk, J.rows - r0);
@@ -511,7 +513,6 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
   }
   int parent = -1;
   if (touches_drafts && P.parent && tid < J.n) parent = P.parent[J.first + tid];
-  const unsigned long long count_seen = SANITIZE || J.whole || tid > 0 ? 0ull : ld_dev(J.word);
   if (mine > 0) fetch_ids(t);
   lds_sync();                                                   // the LDS of the piece before is free
   if (mine > 0) {
@@ -733,7 +734,7 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
     __builtin_amdgcn_s_setprio(0);
   }
 
-  if (!SANITIZE && !J.whole && tid == 0) open_count(J.word, count_seen, P.tag);
+  const unsigned long long count_seen = SANITIZE || J.whole || tid > 0 ? 0ull : ld_dev(J.word);     // (arrives while the waves merge)
 
   // ---- merge the waves, one block at a time ----
 #pragma unroll
@@ -747,9 +748,13 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
   }
   lds_sync();                                              // (the rings are done with, too)
   if constexpr (!SANITIZE) {
-    if (S.nans) return;
+    if (S.nans) {
+      if (!J.whole && tid == 0) open_count(J.word, count_seen, P.tag);
+      return;
+    }
   }
-  if (tid < 16 * NB * (split ? 2 : 1)) {
+  const int halves = SANITIZE ? 1 : keep_scalar(J.halves);
+  if (tid < 16 * NB * halves) {
     const int w0 = tid < 16 * NB ? 0 : kWaves / 2, local = tid < 16 * NB ? tid : tid - 16 * NB;
     float M = -INFINITY, Z = 0.f;
 #pragma unroll
@@ -775,7 +780,7 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
           make_float4(oacc[qi][d][0] * f, oacc[qi][d][1] * f, oacc[qi][d][2] * f, oacc[qi][d][3] * f);
     lds_sync();
 #pragma unroll 2
-    for (int at = tid; at < 16 * (D / 4) * (split ? 2 : 1); at += Sh::kThreads) {      // four dimensions of a row
+    for (int at = tid; at < 16 * (D / 4) * halves; at += Sh::kThreads) {      // four dimensions of a row
       const int d4 = at % (D / 4), r = at / (D / 4) % 16, other = at / (16 * (D / 4)), row = 16 * (NB * other + qi) + r;
       if (row >= J.rows) continue;
       float4 x[kWaves], sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -801,6 +806,7 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
       }
     }
   }
+  if (!SANITIZE && !J.whole && tid == 0) open_count(J.word, count_seen, P.tag);
 }
 
 // TERMS: fp16 terms of a weight.
@@ -839,19 +845,20 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
       continue;
     }
     const int i = __ffsll(later) - 1;
-    const int groups = __builtin_amdgcn_readlane(r.groups, i), per = __builtin_amdgcn_readlane(r.per, i);
+    J.b = 64 * k + i;
+    J.ctx = __builtin_amdgcn_readlane(r.ctx, i);
+    J.first = __builtin_amdgcn_readlane(r.first, i);
+    J.n = __builtin_amdgcn_readlane(r.n, i);
+    const RowGroups g = group_rows(J.n * P.G, kMost, P.halves);
+    const int groups = __builtin_amdgcn_readfirstlane(g.groups), per = __builtin_amdgcn_readfirstlane(g.per);
+    J.halves = __builtin_amdgcn_readfirstlane(g.halves);
     Place p;
-    p.units = __builtin_amdgcn_readlane(r.units, i);
-    J.halves = __builtin_amdgcn_readlane(r.halves, i);
+    p.units = units_of(P, J.ctx, J.n);
     p.cost = J.halves * unit_cost(per);
     p.shift = P.shift;
     p.head = head_cost(per);
     const int behind = base + __builtin_amdgcn_readlane(r.upto, i), group_cost = p.head + chunks_of(p.units, p.shift) * p.cost;
     p.start = behind - groups * group_cost;
-    J.b = 64 * k + i;
-    J.ctx = __builtin_amdgcn_readlane(r.ctx, i);
-    J.first = __builtin_amdgcn_readlane(r.first, i);
-    J.n = __builtin_amdgcn_readlane(r.n, i);
     for (int grp = 0; grp < groups && p.start < end; ++grp, p.start += group_cost) {
       J.t0 = first_unit(p, from);
       J.t1 = min(p.units, first_unit(p, end));
@@ -903,7 +910,7 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   p.waves = static_cast<int64_t>(a.Hkv) * a.B * p.groups < 512 ? 8 : 4;
   p.ranges = std::max(1, (p.waves == 8 ? 256 : 512) / a.Hkv);
   // the cost of the batch stays below 2^31 (no chunk is long enough where there are millions of groups: shift is then 30 and the call is refused)
-  const int64_t groups = std::min<int64_t>(static_cast<int64_t>(a.B) * p.groups, static_cast<int64_t>(a.total_q) * (a.Hq / a.Hkv) / 16 + a.B);
+  const int64_t groups = static_cast<int64_t>(a.B) * p.groups;
   const int64_t units = (static_cast<int64_t>(a.max_pages) + 1) / 2;
   while (p.shift < kQuantMaxShift && groups * (kMostHead + ((units >> p.shift) + 1) * p.halves * kMostCost) >= (int64_t{1} << 31)) ++p.shift;
   return p;

@@ -129,3 +129,16 @@ def test_reference_codes_match_torch():
 def test_reference_scales():
     assert R.page_scale(448.0) == 1.0 and R.page_scale(np.nextafter(448.0, 999)) == 2.0 and R.page_scale(0.0) == 2.0 ** -100
     assert R.page_scale(224.0) == 0.5 and R.page_scale(1.0) == 2.0 ** -8
+
+
+def test_millions_of_groups_of_rows():
+    """More requests times groups of query rows than the cut of the batch can count in 31 bits."""
+    big = dict(batch=65535, num_q_heads=1024, num_kv_heads=1, head_dim=64, total_q=65535 * 128, max_q_per_req=128, max_pages_per_req=10)
+    desc = sv.make_attn_desc(**big)
+    assert sv.spec_verify_attn_quant_workspace_size(desc) == 0
+    rc = sv.lib().spec_verify_attn_quant(ctypes.byref(desc), 30, P, P, P, P, P, P, P, P, None, P, None, P, 1 << 40, None)
+    assert rc == UNSUPPORTED
+    with pytest.raises(sv.SpecError):
+        sv.spec_describe_attn_quant_plan(desc)
+    # a wide block table alone is no reason
+    assert sv.spec_verify_attn_quant_workspace_size(sv.make_attn_desc(**{**big, "batch": 64, "max_pages_per_req": 2**31 - 1})) > 0
