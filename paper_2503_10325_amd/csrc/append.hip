@@ -10,7 +10,8 @@
 // Work: a workgroup takes the (up to 16) new tokens of one page, for a share of the heads; the angles of those tokens are
 // worked out once, in LDS, for all of them.  Page slots are numbered without a scan: request b's start at q_offsets[b] / 16 + 2 b, which
 // leaves room for the at most n / 16 + 2 pages that n tokens touch; slots without a page return at once.
-// Bound by memory for prompts, by latency (offsets -> page id -> store) for a few tokens.
+// Bound by memory for prompts (22000 tokens x 32 heads of q, k and v: 230 us, 4.7 TB/s; 16384 tokens into the 8-bit cache 136 us, 4.7), by latency
+// (offsets -> page id -> store) for a few tokens: 4 us for one request, 9 for 16 trees of 64 nodes, 11 for an 8-bit serving batch.
 //
 // 8-bit cache (quant.h): one wave takes the K or V of one (page, head): the largest entry, the scale, the codes; entries that the page
 // already holds are rewritten where the scale grows.
