@@ -458,7 +458,7 @@ def _rows(t, heads, head_dim, rows, what):
     return t.data_ptr(), apart if rows > 1 else heads * head_dim
 
 
-def _quant_pools(k_pool, v_pool, k_scale, v_scale):
+def _quant_pools(k_pool, v_pool, k_scale, v_scale, desc=None):
     """Pointers of an 8-bit cache: k_pool [num_pages, Hkv, D / 16, 16, 16] and v_pool [num_pages, Hkv, D, 16] of torch.float8_e4m3fn
     or torch.uint8, scales [num_pages, Hkv] float32."""
     if k_pool.element_size() != 1 or v_pool.element_size() != 1:
@@ -466,6 +466,8 @@ def _quant_pools(k_pool, v_pool, k_scale, v_scale):
     pages, heads, dim, page = v_pool.shape
     if k_pool.shape != (pages, heads, dim // 16, page, 16) or k_scale.shape != (pages, heads) or v_scale.shape != (pages, heads):
         raise ValueError("k_pool [num_pages, Hkv, D / 16, 16, 16], v_pool [num_pages, Hkv, D, 16] and scales [num_pages, Hkv] expected")
+    if desc is not None and (heads != desc.num_kv_heads or dim != desc.head_dim):
+        raise ValueError(f"a cache of {heads} heads of {dim} dimensions, the descriptor has {desc.num_kv_heads} of {desc.head_dim}")
     f32 = _tensor_types()[1]
     return (_ptr(k_pool), _ptr(v_pool), _typed(k_scale, f32, "k_scale"), _typed(v_scale, f32, "v_scale"))
 
@@ -488,6 +490,9 @@ def spec_append_kv(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, bloc
     """Device tensors: q [total_q, Hq, D], k and v [total_q, Hkv, D] bf16 (tokens may lie apart, as slices of one projection do),
     inv_freq [rotary_dim / 2] float32, pools [num_pages, Hkv, 16, D] bf16 (modified), the rest int32; q_out [total_q, Hq, D] bf16."""
     bf16 = _tensor_types()[2]
+    want = (desc.num_pages, desc.num_kv_heads, desc.page_size, desc.head_dim)
+    if k_pool.shape != want or v_pool.shape != want:
+        raise ValueError(f"pools of {want} expected, as in the descriptor")
     pools = (_typed(k_pool, bf16, "k_pool"), _typed(v_pool, bf16, "v_pool"))
     _append(lib().spec_append_kv, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions,
             _stream_beside(stream, k_pool))
@@ -496,8 +501,10 @@ def spec_append_kv(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, bloc
 def spec_append_kv_quant(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets,
                          parent, q_out, positions=None, stream=None) -> None:
     """spec_append_kv into an 8-bit cache (pools and scales modified)."""
-    _append(lib().spec_append_kv_quant, desc, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale), block_table, ctx_len,
-            q_offsets, parent, q_out, positions, _stream_beside(stream, k_pool))
+    if k_pool.shape[0] != desc.num_pages:
+        raise ValueError(f"pools of {desc.num_pages} pages expected, as in the descriptor")
+    _append(lib().spec_append_kv_quant, desc, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale, desc), block_table,
+            ctx_len, q_offsets, parent, q_out, positions, _stream_beside(stream, k_pool))
 
 
 def spec_verify_attn_quant_workspace_size(desc: SpecAttnDesc) -> int:
@@ -510,7 +517,7 @@ def spec_verify_attn_quant(desc: SpecAttnDesc, q, k_pool, v_pool, k_scale, v_sca
     i32, f32, bf16 = _tensor_types()
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _typed(q, bf16, "q"),
-                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale), _typed(block_table, i32, "block_table"),
+                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, desc), _typed(block_table, i32, "block_table"),
                                       _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
                                       _typed(parent, i32, "parent"), _typed(out, f32 if desc.out_dtype == SPEC_F32 else bf16, "out"),
                                       _typed(lse, f32, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, k_pool))

@@ -113,3 +113,11 @@ def test_alike_requests(B):
     """As many pieces for each of alike requests, for numbers that divide nothing."""
     c = U.batch(40 + B, ctx=[450] * B, n=[2] * B, heads=(2, 1))
     check(c, U.quant_pools(c), False)
+
+
+@pytest.mark.parametrize("heads", [100, 130, 300])
+def test_as_many_heads_as_workgroups(heads):
+    """Few ranges per KV head, or one: whole requests and no workspace then."""
+    c = U.batch(50, heads=(heads, heads), D=64, ctx=[70, 0, 300], n=[2, 1, 3])
+    assert (sv.spec_verify_attn_quant_workspace_size(sv.make_attn_desc(3, heads, heads, 64, 6, 3, c["table"].shape[1])) == 0) == (heads > 128)
+    check(c, U.quant_pools(c), False)

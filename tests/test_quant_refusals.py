@@ -142,3 +142,27 @@ def test_millions_of_groups_of_rows():
         sv.spec_describe_attn_quant_plan(desc)
     # a wide block table alone is no reason
     assert sv.spec_verify_attn_quant_workspace_size(sv.make_attn_desc(**{**big, "batch": 64, "max_pages_per_req": 2**31 - 1})) > 0
+
+
+def test_binding_refuses_pools_that_are_not_the_descriptors():
+    torch = pytest.importorskip("torch")
+    t = lambda shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    desc = sv.make_append_desc(**{**OK, "rotary_dim": 0})
+    rows = (t((8, 8, 128)), t((8, 2, 128)), t((8, 2, 128)), None)
+    rest = (i32(2, 10), i32(2), i32(3), None, t((8, 8, 128)))
+    for shape in ((29, 2, 16, 128), (30, 1, 16, 128), (30, 2, 16, 64)):
+        with pytest.raises(ValueError):
+            sv.spec_append_kv(desc, *rows, t(shape), t(shape), *rest, stream=_Stream())
+
+    def quant(pages, heads, dim):
+        return (t((pages, heads, dim // 16, 16, 16), torch.uint8), t((pages, heads, dim, 16), torch.uint8),
+                t((pages, heads), torch.float32), t((pages, heads), torch.float32))
+
+    attn = sv.make_attn_desc(2, 8, 2, 128, 8, 4, 10)
+    for pages, heads, dim in ((29, 2, 128), (30, 1, 128), (30, 2, 64)):
+        with pytest.raises(ValueError):
+            sv.spec_append_kv_quant(desc, *rows, *quant(pages, heads, dim), *rest, stream=_Stream())
+        if (heads, dim) != (2, 128):
+            with pytest.raises(ValueError):
+                sv.spec_verify_attn_quant(attn, rows[0], *quant(pages, heads, dim), *rest[:4], rest[4], stream=_Stream())
