@@ -223,6 +223,9 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The largest of three, NaN if one is: one instruction, where fmaxf first makes quiet NaN of each operand, one instruction apiece.
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+
 // Eight e4m3 bytes as an operand of eight bf16, or, times a power of two, of eight fp16.
 __device__ __forceinline__ qbf16x8 operand_bf16(uint32_t lo, uint32_t hi) {
   const qbf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
@@ -652,8 +655,8 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
     bool ahead = v_own > v_ref;
 #pragma unroll
     for (int qi = 0; qi < NB; ++qi) {
-      top[qi] = fmaxf(fmaxf(fmaxf(s[qi][0][0], s[qi][0][1]), fmaxf(s[qi][0][2], s[qi][0][3])),
-                      fmaxf(fmaxf(s[qi][1][0], s[qi][1][1]), fmaxf(s[qi][1][2], s[qi][1][3]))) * factor;    // factor >= 0
+      top[qi] = max3(max3(s[qi][0][0], s[qi][0][1], s[qi][0][2]), max3(s[qi][0][3], s[qi][1][0], s[qi][1][1]),
+                     __builtin_elementwise_maximum(s[qi][1][2], s[qi][1][3])) * factor;                   // factor >= 0
       ahead |= top[qi] > ref[qi] + kSlack;
     }
     if (any_lane(ahead)) {
