@@ -435,6 +435,22 @@ def _typed(t, dtype, what):
     return t.data_ptr()
 
 
+def _pointers(dtype, names, *tensors):
+    """_typed for several: one call for all of them."""
+    out = []
+    for i, t in enumerate(tensors):
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not dtype or not t.is_contiguous():
+            _typed(t, dtype, names[i])
+        out.append(t.data_ptr())
+    return out
+
+
+_PLACES = ("block_table", "ctx_len", "q_offsets", "parent", "stop_node", "new_len")
+
+
 def _stream_beside(stream, t) -> int:
     """The stream's handle (None: the current one); the cache `t` has to lie on its device."""
     at = t.get_device()
@@ -469,7 +485,11 @@ def _quant_pools(k_pool, v_pool, k_scale, v_scale, desc=None):
     if desc is not None and (heads != desc.num_kv_heads or dim != desc.head_dim):
         raise ValueError(f"a cache of {heads} heads of {dim} dimensions, the descriptor has {desc.num_kv_heads} of {desc.head_dim}")
     f32 = _tensor_types()[1]
-    return (_ptr(k_pool), _ptr(v_pool), _typed(k_scale, f32, "k_scale"), _typed(v_scale, f32, "v_scale"))
+    if k_scale.dtype is not f32 or v_scale.dtype is not f32:
+        raise TypeError("k_scale, v_scale: torch.float32 expected")
+    if not (k_pool.is_contiguous() and v_pool.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
+        raise AssertionError("tensors handed to the library must be contiguous")
+    return k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
 
 
 def _append(fn, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream):
@@ -479,8 +499,7 @@ def _append(fn, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets,
     kp, ks = _rows(k, Hkv, D, total, "k")
     vp, vs = _rows(v, Hkv, D, total, "v")
     rc = fn(desc, qp, qs, kp, ks, vp, vs, _typed(inv_freq, f32, "inv_freq"), _typed(positions, i32, "positions"), *pools,
-            _typed(block_table, i32, "block_table"), _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
-            _typed(parent, i32, "parent"), _typed(q_out, bf16, "q_out"), stream)
+            *_pointers(i32, _PLACES, block_table, ctx_len, q_offsets, parent), _typed(q_out, bf16, "q_out"), stream)
     if rc != SPEC_OK:
         raise SpecError(fn.__name__, rc)
 
@@ -517,9 +536,9 @@ def spec_verify_attn_quant(desc: SpecAttnDesc, q, k_pool, v_pool, k_scale, v_sca
     i32, f32, bf16 = _tensor_types()
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _typed(q, bf16, "q"),
-                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, desc), _typed(block_table, i32, "block_table"),
-                                      _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
-                                      _typed(parent, i32, "parent"), _typed(out, f32 if desc.out_dtype == SPEC_F32 else bf16, "out"),
+                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, desc),
+                                      *_pointers(i32, _PLACES, block_table, ctx_len, q_offsets, parent),
+                                      _typed(out, f32 if desc.out_dtype == SPEC_F32 else bf16, "out"),
                                       _typed(lse, f32, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, k_pool))
     if rc != SPEC_OK:
         raise SpecError("spec_verify_attn_quant", rc)
@@ -536,12 +555,10 @@ def spec_describe_attn_quant_plan(desc: SpecAttnDesc) -> str:
 def spec_compact_kv_quant(k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, stop_node, new_len=None,
                           stream=None) -> None:
     """spec_compact_kv over an 8-bit cache (pools and scales modified in place); the rest int32 device tensors."""
-    i32 = _tensor_types()[0]
+    pools = _quant_pools(k_pool, v_pool, k_scale, v_scale)
     pages, heads, dim, page = v_pool.shape
-    rc = lib().spec_compact_kv_quant(ctx_len.shape[0], heads, dim, page, block_table.shape[1], pages,
-                                     *_quant_pools(k_pool, v_pool, k_scale, v_scale), _typed(block_table, i32, "block_table"),
-                                     _typed(ctx_len, i32, "ctx_len"), _typed(q_offsets, i32, "q_offsets"),
-                                     _typed(parent, i32, "parent"), _typed(stop_node, i32, "stop_node"),
-                                     _typed(new_len, i32, "new_len"), _stream_beside(stream, k_pool))
+    places = _pointers(_tensor_types()[0], _PLACES, block_table, ctx_len, q_offsets, parent, stop_node, new_len)
+    rc = lib().spec_compact_kv_quant(ctx_len.shape[0], heads, dim, page, block_table.shape[1], pages, *pools, *places,
+                                     _stream_beside(stream, k_pool))
     if rc != SPEC_OK:
         raise SpecError("spec_compact_kv_quant", rc)

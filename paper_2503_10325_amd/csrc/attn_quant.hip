@@ -892,7 +892,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void attn_quant_kernel(QuantAttnPara
           quant_piece<1, TERMS, true>(S, part);
         }
         __syncthreads();
-        find_rows(P, S, J, threadIdx.x);                                     // (of all rows again, for the merge)
+        find_rows(P, S, J, threadIdx.x);                        // (of all rows again, for the merge)
       }
       if (!J.whole) {
         const Pieces all_pieces = pieces_of(cut, p);
