@@ -121,3 +121,19 @@ def test_as_many_heads_as_workgroups(heads):
     c = U.batch(50, heads=(heads, heads), D=64, ctx=[70, 0, 300], n=[2, 1, 3])
     assert (sv.spec_verify_attn_quant_workspace_size(sv.make_attn_desc(3, heads, heads, 64, 6, 3, c["table"].shape[1])) == 0) == (heads > 128)
     check(c, U.quant_pools(c), False)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("heads,n", [((1024, 1), [3]), ((100, 1), [128, 1]), ((75, 3), [40])])
+def test_many_query_heads_per_kv_head(heads, n, f32):
+    c = U.batch(51, heads=heads, D=64, ctx=[70, 5][:len(n)], n=n, tree=True)
+    check(c, U.quant_pools(c), f32)
+
+
+def test_units_in_chunks():
+    """A block table with room for so many tokens that the cost of the batch is counted in chunks of units."""
+    c = U.batch(52, heads=(64, 1), ctx=[300, 2500], n=[128, 100], tree=True)
+    wide = np.full((2, 1 << 21), -1, dtype=np.int32)
+    wide[:, :c["table"].shape[1]] = c["table"]
+    c["table"] = wide
+    check(c, U.quant_pools(c), False)

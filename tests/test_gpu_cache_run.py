@@ -88,6 +88,24 @@ def test_decoding_steps(heads, D, tree):
     assert moved > 5
 
 
+def test_long_prompts():
+    """More than 1024 pages of new tokens: queries go with keys and values, one workgroup for a page's heads."""
+    c = U.batch(60, ctx=[9, 100], n=[9001, 8003], heads=(3, 1), D=64)
+    pools = U.quant_pools(c)
+    d = U.Device(c, fused=True, quant=pools)
+    d.append()
+    q, k, v, ks, vs, truth = R.append_quant(c, *pools)
+    assert U.rotated_close(U.host(d.q_out), q, c["q"], c["rotary"], 2.0 ** -8)
+    assert np.array_equal(U.host(d.v_scale), vs) and np.array_equal(U.host(d.v_pool), v) and np.array_equal(U.host(d.k_scale), ks)
+    got = U.host(d.k_pool)
+    other = got != k
+    for (pg, h, slot), x in truth.items():
+        step = R.e4m3_step(x / ks[pg, h]) * ks[pg, h]
+        assert np.all(np.abs(R.E4M3[got[pg, h, :, slot].reshape(-1)] * ks[pg, h] - x) <= step / 2 + 2.0 ** -20 * np.abs(c["k"]).max())
+        other[pg, h, :, slot] = False
+    assert not other.any()
+
+
 def test_bf16_cache_feeds_attention():
     """Appended keys and values of the bf16 cache are what spec_verify_attn reads: against attention over the rotated tokens."""
     c = U.batch(61, ctx=[37, 0, 16], n=[5, 9, 1], heads=(4, 2), tree=True)
