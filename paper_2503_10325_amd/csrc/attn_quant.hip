@@ -44,6 +44,8 @@ constexpr int most_blocks(int D, int terms) { return D == 128 && terms == 2 ? 3 
 constexpr int kWeightBias = 6;                // weights are fed as fp16(2^6 p): normal down to p = 2^-20, and
 constexpr float kSlack = 8.f;                 // the reference of a row's softmax follows its maximum when that is 2^8 ahead: below 2^14 then
 constexpr float kLeastV = 3.0517578125e-5f;   // 2^-15: what V may be scaled by and still be exact in fp16
+constexpr float kLeastWeight = 0x1p-40f;       // what weights are scaled by at least.  At most 2^(8 + kWeightBias - 40) is 0 in fp16 already, so
+                                              // nothing smaller is fed; the weights' sum, which is of scaled ones, loses no weight above 2^-92
 static __device__ const float kNoScale[1] = {0.f};      // read in place of the scale of a page that is none
 
 constexpr int ilog2(int x) { return x <= 1 ? 0 : 1 + ilog2(x / 2); }
@@ -678,10 +680,10 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
 
     // ---- 2^shift times the weights, as TERMS fp16 terms ----
     // V is fed relative to v_ref, down to 2^-15 of it by itself, exactly; what a page's scale is smaller still goes into its weights, whose
-    // fp16 has room for it.
+    // fp16 has room for it, down to kLeastWeight (further down, weights would leave the range of fp32 too, and be missing from their sum).
     asm volatile("" : "+v"(v_ref));      // (its inverse worked out on both sides of the branch makes it one with an else part, whose copies cost the
                                          // registers of all results a second time)
-    const float ratio = v_own * inverse_scale(v_ref), v_by = fmaxf(ratio, kLeastV), p_by = ok ? ratio * inverse_scale(v_by) : 1.f;
+    const float ratio = v_own * inverse_scale(v_ref), v_by = fmaxf(ratio, kLeastV), p_by = ok ? fmaxf(ratio * inverse_scale(v_by), kLeastWeight) : 1.f;
     const float shift = static_cast<float>(static_cast<int>(__float_as_uint(p_by) >> 23) - 127 + kWeightBias);
     const float unshift = inverse_scale(p_by);
     raw4 hi[NB], lo[TERMS == 2 ? NB : 1];
