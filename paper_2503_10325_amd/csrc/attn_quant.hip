@@ -13,7 +13,7 @@
 // Work: a request's query rows of a KV head are taken in groups of up to 64 (a wave multiplies each unit with up to four 16-row blocks).
 // Per KV head the units of all requests and groups lie end to end and are cut into ranges of equal cost, one per workgroup, whatever the
 // lengths; every workgroup works out from ctx_len and q_offsets which pieces its range holds.  A range that ends inside a request
-// leaves an unnormalised partial result; the workgroup that finishes the last piece merges them, in their order.  The four or
+// leaves a partial result and its sum of weights; the workgroup that finishes the last piece merges them, in their order.  The four or
 // eight waves of a workgroup take units in turn and merge through LDS.
 //
 // Bound by memory up to 48 rows (64 requests x 8 KV heads x 2048 tokens, 8 to 32 rows: 54 to 58 us, 5.0 to 4.7 TB/s; 4096 tokens 5.2), by the
@@ -62,7 +62,7 @@ struct QuantAttnParams {
   const int32_t* parent;
   void* out;
   float* lse;
-  float* ws_o;        // [KV heads][ranges][2][rows][D] unnormalised partial results
+  float* ws_o;        // [KV heads][ranges][2][rows][D] partial results, each by its own sum of weights
   float2* ws_ml;      // ... [rows] (maximum in log2 units, sum)
   int B, Hq, Hkv, G, total_q, max_q, max_pages, num_pages;
   uint32_t inverse_G; // 2^31 / G, rounded up
@@ -337,21 +337,22 @@ __device__ __forceinline__ unsigned long long pair_bits(float lo, float hi) {
   return static_cast<unsigned long long>(__float_as_uint(hi)) << 32 | __float_as_uint(lo);
 }
 
-// Dimensions 4 d4 .. + 3 of a row's result from their sums; inv: 1 / the row's sum of weights (0: it sees nothing, and gives 0).
+// Dimensions 4 d4 .. + 3 of a row's result.
 template <int D>
-__device__ __forceinline__ void put_result(KernelParams& P, int64_t at, int d4, float4 x, float inv) {
+__device__ __forceinline__ void put_result(KernelParams& P, int64_t at, int d4, float4 x) {
   if (P.out_f32) {
-    reinterpret_cast<float4*>(static_cast<float*>(P.out) + at * D)[d4] = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    reinterpret_cast<float4*>(static_cast<float*>(P.out) + at * D)[d4] = x;
   } else {
-    const qbf16x2 lo = {static_cast<__bf16>(x.x * inv), static_cast<__bf16>(x.y * inv)}, hi = {static_cast<__bf16>(x.z * inv), static_cast<__bf16>(x.w * inv)};
+    const qbf16x2 lo = {static_cast<__bf16>(x.x), static_cast<__bf16>(x.y)}, hi = {static_cast<__bf16>(x.z), static_cast<__bf16>(x.w)};
     reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + at * D)[d4] = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
   }
 }
-// ... and its log-sum-exp (nothing seen: -infinity) from the maximum in log2 units and the sum; returns 1 / sum
-__device__ __forceinline__ float put_lse(KernelParams& P, int64_t at, float M, float Z) {
+// ... and its log-sum-exp (nothing seen: -infinity) from the maximum in log2 units and the sum.
+__device__ __forceinline__ void put_lse(KernelParams& P, int64_t at, float M, float Z) {
   if (P.lse) P.lse[at] = (M + log2f(Z)) * static_cast<float>(kLn2);
-  return Z == 0.f ? 0.f : 1.f / Z;
 }
+// What a row's results are multiplied with: 1 / its sum of weights (0: it sees nothing, and gives 0).
+__device__ __forceinline__ float inverse_sum(float Z) { return Z == 0.f ? 0.f : 1.f / Z; }
 
 // The pieces of a request count themselves in a word {count : the call's tag}.  What an earlier call left there is first replaced by a count
 // of none: one attempt, since only another piece of this call can have been quicker.  (Counting by compare-and-swap alone, pieces that finish
@@ -395,11 +396,12 @@ __device__ __forceinline__ void merge_pieces(Sh& S, const QuantPiece& J, int64_t
       for (int i = 0; i < pieces; ++i) M = fmaxf(M, S.merge.m[i * rows + r]);
       for (int i = 0; i < pieces; ++i) {
         const float m = S.merge.m[i * rows + r];
-        const float f = m == -INFINITY ? 0.f : fast_exp2(m - M);
-        Z += m == -INFINITY ? 0.f : S.merge.l[i * rows + r] * f;
-        S.merge.m[i * rows + r] = f;
+        const float share = m == -INFINITY ? 0.f : S.merge.l[i * rows + r] * fast_exp2(m - M);
+        Z += share;
+        S.merge.m[i * rows + r] = share;
       }
-      S.inv[r] = put_lse(P, S.row[r0 + r], M, Z);
+      put_lse(P, S.row[r0 + r], M, Z);
+      S.inv[r] = inverse_sum(Z);
     }
     lds_sync();
     // four dimensions of kRows rows at a time, of kFly pieces: as many loads on their way for few pieces of many rows as for many of few
@@ -408,8 +410,12 @@ __device__ __forceinline__ void merge_pieces(Sh& S, const QuantPiece& J, int64_t
       const int d4 = tid % (D / 4);
       for (int r1 = tid / (D / 4); r1 < rows; r1 += kRows * kApart) {
         float4 sum[kRows];
+        float inv[kRows];
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j = 0; j < kRows; ++j) {
+          sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          inv[j] = S.inv[min(r1 + j * kApart, rows - 1)];
+        }
         for (int i0 = 0; i0 < pieces; i0 += kFly) {
           unsigned long long x[kFly][kRows][2];
 #pragma unroll
@@ -426,7 +432,7 @@ __device__ __forceinline__ void merge_pieces(Sh& S, const QuantPiece& J, int64_t
             if (i0 + k >= pieces) break;
 #pragma unroll
             for (int j = 0; j < kRows; ++j) {
-              const float f = S.merge.m[(i0 + k) * rows + min(r1 + j * kApart, rows - 1)];
+              const float f = S.merge.m[(i0 + k) * rows + min(r1 + j * kApart, rows - 1)] * inv[j];
               sum[j].x += __uint_as_float(static_cast<unsigned>(x[k][j][0])) * f;
               sum[j].y += __uint_as_float(static_cast<unsigned>(x[k][j][0] >> 32)) * f;
               sum[j].z += __uint_as_float(static_cast<unsigned>(x[k][j][1])) * f;
@@ -436,7 +442,7 @@ __device__ __forceinline__ void merge_pieces(Sh& S, const QuantPiece& J, int64_t
         }
 #pragma unroll
         for (int j = 0; j < kRows; ++j)
-          if (r1 + j * kApart < rows) put_result<D>(P, S.row[r0 + r1 + j * kApart], d4, sum[j], S.inv[r1 + j * kApart]);
+          if (r1 + j * kApart < rows) put_result<D>(P, S.row[r0 + r1 + j * kApart], d4, sum[j]);
       }
     };
     if (rows > kThreads / (D / 4)) combine(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
@@ -773,8 +779,9 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
     for (int w = 0; w < kWaves; ++w)
       if (w < kWaves / 2 || !split) Z += S.m[w0 + w][local] == -INFINITY ? 0.f : S.l[w0 + w][local] * fast_exp2(S.m[w0 + w][local] - M);
     S.top[tid] = M;
+    S.inv[tid] = inverse_sum(Z);
     if (tid < J.rows) {
-      if (J.whole) S.inv[tid] = put_lse(P, S.row[tid], M, Z);
+      if (J.whole) put_lse(P, S.row[tid], M, Z);
       else st_dev(reinterpret_cast<unsigned long long*>(P.ws_ml + J.part + tid), pair_bits(M, Z));
     }
   }
@@ -782,7 +789,9 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
 #pragma unroll
   for (int qi = 0; qi < NB; ++qi) {
     if (qi > 0) lds_sync();
-    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - S.top[row0 + 16 * qi + rn] - static_cast<float>(kWeightBias)) * v_ref;
+    // (divided by the sum of weights first: results are no larger than the values then, which may be near the end of fp32's range)
+    const int row = row0 + 16 * qi + rn;
+    const float f = ref[qi] == -INFINITY ? 0.f : fast_exp2(ref[qi] - S.top[row] - static_cast<float>(kWeightBias)) * S.inv[row] * v_ref;
 #pragma unroll
     for (int d = 0; d < kDT; ++d)
       *reinterpret_cast<float4*>(&S.o[wave][rn][16 * d + 4 * g]) =
@@ -806,7 +815,7 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
         put_back_nans(P, S, J, row, 4 * d4 + 2, sum.z, sum.w);
       }
       if (J.whole) {
-        put_result<D>(P, S.row[row], d4, sum, S.inv[row]);
+        put_result<D>(P, S.row[row], d4, sum);
       } else {
         // read by another workgroup of this launch: device-scope stores
         unsigned long long* to = reinterpret_cast<unsigned long long*>(P.ws_o + (J.part + row) * D) + 2 * d4;

@@ -1,4 +1,5 @@
-"""Attention over the 8-bit cache at the ends of what it takes: scales of V as far apart as they can be, which may not reach the weights' sum."""
+"""Attention over the 8-bit cache at the ends of what it takes: scales of V as far apart as they can be, which may not reach the weights' sum,
+and so large that results are near the end of fp32's range."""
 import numpy as np
 import pytest
 
@@ -46,3 +47,13 @@ def test_scales_of_any_size(spec, f32):
     pools = list(U.quant_pools(c, spread=0))
     pools[3][...] = np.exp2(c["rng"].integers(-100, 101, pools[3].shape)).astype(np.float32)
     check(c, pools, f32)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("spec", list(SPECS) + ["cut"])
+def test_largest_values(spec, f32):
+    """Entries up to 448 2^119, 0.87 of the largest fp32 number: sums over the tokens would be beyond it, their mean is not."""
+    c = U.batch(93, **(SPECS[spec] if spec in SPECS else dict(ctx=[3000], n=[3], heads=(2, 1))))
+    pools = list(U.quant_pools(c, spread=0))
+    pools[3][c["rng"].random(pools[3].shape) < 0.7] = np.float32(2.0 ** 119)
+    assert np.isfinite(check(c, pools, f32)).all()
