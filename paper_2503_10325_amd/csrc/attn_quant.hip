@@ -637,7 +637,7 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
       fetch_ids(t + 2 * per_half);
     }
     const bool ok = ks != 0.f;
-    const float factor = ok ? ks * c : 1.f;                   // (not 0: masked scores are -infinity)
+    const float factor = fmaxf(ks * c, 0x1p-126f);              // (not 0: masked scores are -infinity)
 
     // ---- masks: only where the unit reaches the drafts, or a page is none ----
     const int past = t * kUnit + 16 * (g >> 1) - J.ctx;         // the lane's page starts that far behind the context
