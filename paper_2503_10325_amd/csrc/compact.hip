@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
       a = p < a ? p : -1;                                                    // a malformed parent entry ends the path
     }
     sh_depth = depth;
-    if (h == 0 && new_len) new_len[b] = ctx + depth;
+    if (h == 0 && new_len) new_len[b] = static_cast<int>(min(static_cast<unsigned>(ctx) + depth, 0x7fffffffu));
   }
   __syncthreads();
   const int depth = sh_depth;
@@ -134,9 +134,10 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
     const int id = lp < max_pages ? bt[lp] : -1;
     return id >= 0 && id < num_pages ? id : -1;
   };
-  const int lp0 = ctx / kQuantPage, pages = (ctx + depth - 1) / kQuantPage - lp0 + 1, held = ctx % kQuantPage;
+  // places are counted from the start of the first written page: a length may be near 2^31
+  const int lp0 = ctx / kQuantPage, held = ctx % kQuantPage, pages = (held + depth - 1) / kQuantPage + 1;
   if (tid < depth) {
-    const int pos = ctx + sh_path[depth - 1 - tid], id = page_of(pos / kQuantPage);
+    const int pos = held + sh_path[depth - 1 - tid], id = page_of(lp0 + pos / kQuantPage);
     sh_page[tid] = id;
     sh_slot[tid] = pos % kQuantPage;
     sh_scale[0][tid] = id < 0 ? 0.f : k_scale[static_cast<int64_t>(id) * Hkv + h];
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
     const float own = id < 0 ? 0.f : (which ? v_scale : k_scale)[static_cast<int64_t>(id) * Hkv + h];
     float m = j == 0 && held > 0 ? own : 0.f;
     for (int t = 0; t < kQuantPage; ++t) {
-      const int d = (lp0 + j) * kQuantPage + t - ctx;
+      const int d = j * kQuantPage + t - held;
       if (d >= 0 && d < depth) m = fmaxf(m, sh_scale[which][d]);
     }
     sh_old[which][j] = own;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
   }
   __syncthreads();
   if (tid < depth) {
-    const int j = (ctx + tid) / kQuantPage - lp0;
+    const int j = (held + tid) / kQuantPage;
     sh_scale[0][tid] *= inverse_scale(sh_new[0][j]);
     sh_scale[1][tid] *= inverse_scale(sh_new[1][j]);
   }
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
     k_set[r] = v_set[r] = false;
     if (j >= pages || sh_to[j] < 0) continue;
     {
-      const int chunk = in / kQuantPage, t = in % kQuantPage, d = (lp0 + j) * kQuantPage + t - ctx;
+      const int chunk = in / kQuantPage, t = in % kQuantPage, d = j * kQuantPage + t - held;
       int page = -1, slot = t;
       float ratio = 1.f;
       if (d >= 0 && d < depth) {
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
     }
     {
       vw[r] = *reinterpret_cast<const raw4*>(v_pool + at(sh_to[j], in * kQuantPage));
-      const int d0 = (lp0 + j) * kQuantPage - ctx;                          // entry that slot 0 takes
+      const int d0 = j * kQuantPage - held;                                 // entry that slot 0 takes
       if (j == 0 && sh_new[1][0] > sh_old[1][0]) {
         const float ratio = sh_old[1][0] * inverse_scale(sh_new[1][0]);
 #pragma unroll

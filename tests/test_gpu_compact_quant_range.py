@@ -1,0 +1,37 @@
+"""Compaction of the 8-bit cache where lengths and offsets are not those of a cache in order: near 2^31."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import cache_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2503_10325_amd import binding
+    binding.lib()
+
+
+def compacted(c, pools, stop):
+    """Pools and scales after the call, and the lengths; -5 where none is written."""
+    d = U.Device(c, quant=pools)
+    new_len = d.compact(torch.from_numpy(np.asarray(stop, dtype=np.int32)).cuda())
+    torch.cuda.synchronize()
+    return [U.host(x) for x in (d.k_pool, d.v_pool, d.k_scale, d.v_scale)], U.host(new_len)
+
+
+def test_lengths_near_the_end_of_32_bits():
+    """No page holds those places: nothing moves, and the length stays below 2^31."""
+    c = U.batch(101, ctx=[20, 20, 20], n=[100, 9, 40], heads=(2, 2), tree=True)
+    for o, m in ((0, 100), (100, 9), (109, 40)):
+        c["parent"][o:o + m] = [max(i - 2, -1) for i in range(m)]
+    pools = U.quant_pools(c)
+    c["ctx"] = np.array([2**31 - 1, 2**31 - 16, 2**31 - 30], dtype=np.int32)
+    after, new_len = compacted(c, pools, [99, 8, 39])
+    assert all(np.array_equal(x, y) for x, y in zip(after, pools))
+    assert new_len.tolist() == [2**31 - 1, 2**31 - 16 + 5, 2**31 - 30 + 20]
