@@ -106,8 +106,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
   __shared__ int sh_to[kQuantPathPages];                                     // written pages (-1: none)
   __shared__ float sh_old[2][kQuantPathPages], sh_new[2][kQuantPathPages];
   const int o = q_offsets[b];
-  int n = q_offsets[b + 1] - o;
-  n = n < 0 ? 0 : (n > kCompactMaxNodes ? kCompactMaxNodes : n);
+  const int n = o < 0 ? 0 : min(max(q_offsets[b + 1], o) - o, kCompactMaxNodes);      // (no request starts in front of the parents)
   const int ctx = ctx_len[b], stop = stop_node[b];
   if (ctx < 0) return;
   if (parent == nullptr) {                                                   // linear drafts lie where they belong

@@ -1,10 +1,11 @@
-"""Compaction of the 8-bit cache where lengths and offsets are not those of a cache in order: near 2^31."""
+"""Compaction of the 8-bit cache where lengths and offsets are not those of a cache in order: near 2^31, below 0."""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
 import cache_util as U
+from oracle import cache as R
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,15 @@ def test_lengths_near_the_end_of_32_bits():
     after, new_len = compacted(c, pools, [99, 8, 39])
     assert all(np.array_equal(x, y) for x, y in zip(after, pools))
     assert new_len.tolist() == [2**31 - 1, 2**31 - 16 + 5, 2**31 - 30 + 20]
+
+
+def test_negative_offsets_are_no_tokens():
+    """As for attention and appending; the request behind it is compacted as ever."""
+    c = U.batch(102, ctx=[20, 35], n=[9, 11], heads=(2, 2), tree=True)
+    c["parent"][9:] = [max(i - 2, -1) for i in range(11)]
+    pools = U.quant_pools(c)
+    *want, want_len = R.compact_quant(c, *pools, [-1, 10])
+    c["offsets"][0] = -2**31
+    after, new_len = compacted(c, pools, [8, 10])
+    assert all(np.array_equal(x, y) for x, y in zip(after, want))
+    assert np.array_equal(new_len, want_len)
