@@ -454,7 +454,8 @@ int32_t spec_append_kv(
  * spec_compact_kv_quant is spec_compact_kv over it.  A page that entries move to gets the
  * largest of its own scale, if it holds tokens 0 .. ctx_len[b] - 1, and of the scales of
  * the pages that they come from.  Entries whose page (of origin or of destination) is
- * outside the pool stay where they are.  At most 128 nodes per request.
+ * outside the pool stay where they are.  A draft tree has at most 128 nodes; a linear request
+ * (parent == NULL: nothing moves, new_len[b] = ctx_len[b] + stop_node[b] + 1) any number.
  * ---------------------------------------------------------------------------- */
 int32_t spec_append_kv_quant(
     const spec_append_desc* desc, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

@@ -106,13 +106,15 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
   __shared__ int sh_to[kQuantPathPages];                                     // written pages (-1: none)
   __shared__ float sh_old[2][kQuantPathPages], sh_new[2][kQuantPathPages];
   const int o = q_offsets[b];
-  const int n = o < 0 ? 0 : min(max(q_offsets[b + 1], o) - o, kCompactMaxNodes);      // (no request starts in front of the parents)
+  const int tokens = o < 0 ? 0 : max(q_offsets[b + 1], o) - o;               // (no request starts in front of the parents)
   const int ctx = ctx_len[b], stop = stop_node[b];
   if (ctx < 0) return;
-  if (parent == nullptr) {                                                   // linear drafts lie where they belong
-    if (tid == 0 && h == 0 && new_len) new_len[b] = ctx + (stop >= 0 && stop < n ? stop + 1 : 0);
+  if (parent == nullptr) {                                                   // linear drafts, however many, lie where they belong
+    if (tid == 0 && h == 0 && new_len)
+      new_len[b] = static_cast<int>(min(static_cast<unsigned>(ctx) + (stop >= 0 && stop < tokens ? stop + 1 : 0), 0x7fffffffu));
     return;
   }
+  const int n = min(tokens, kCompactMaxNodes);
   if (tid < n) sh_parent[tid] = parent[o + tid];
   __syncthreads();
   if (tid == 0) {

@@ -1,4 +1,5 @@
-"""Compaction of the 8-bit cache where lengths and offsets are not those of a cache in order: near 2^31, below 0."""
+"""Compaction of the 8-bit cache where lengths and offsets are not those of a cache in order: near 2^31, below 0; prompts and
+other linear requests of more than 128 tokens."""
 import numpy as np
 import pytest
 
@@ -48,3 +49,14 @@ def test_negative_offsets_are_no_tokens():
     after, new_len = compacted(c, pools, [8, 10])
     assert all(np.array_equal(x, y) for x, y in zip(after, want))
     assert np.array_equal(new_len, want_len)
+
+
+def test_long_linear_requests():
+    """Nothing moves, the length grows to the last accepted token."""
+    c = U.batch(103, ctx=[5, 0, 7, 9, 40], n=[300, 1000, 129, 128, 200], heads=(2, 1))
+    pools = U.quant_pools(c)
+    stop = [250, 999, 128, 127, 200]                                      # (no token 200 of the last)
+    *want, want_len = R.compact_quant(c, *pools, stop)
+    after, new_len = compacted(c, pools, stop)
+    assert all(np.array_equal(x, y) for x, y in zip(after, want)) and all(np.array_equal(x, y) for x, y in zip(want, pools))
+    assert np.array_equal(new_len, want_len) and new_len.tolist() == [256, 1000, 136, 137, 40]
