@@ -108,7 +108,10 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kv_quant_kernel(
   const int o = q_offsets[b];
   const int tokens = o < 0 ? 0 : max(q_offsets[b + 1], o) - o;               // (no request starts in front of the parents)
   const int ctx = ctx_len[b], stop = stop_node[b];
-  if (ctx < 0) return;
+  if (ctx < 0) {                                                             // no request: nothing of it moves, its length stays
+    if (tid == 0 && h == 0 && new_len) new_len[b] = ctx;
+    return;
+  }
   if (parent == nullptr) {                                                   // linear drafts, however many, lie where they belong
     if (tid == 0 && h == 0 && new_len)
       new_len[b] = static_cast<int>(min(static_cast<unsigned>(ctx) + (stop >= 0 && stop < tokens ? stop + 1 : 0), 0x7fffffffu));

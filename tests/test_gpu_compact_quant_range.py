@@ -60,3 +60,14 @@ def test_long_linear_requests():
     after, new_len = compacted(c, pools, stop)
     assert all(np.array_equal(x, y) for x, y in zip(after, want)) and all(np.array_equal(x, y) for x, y in zip(want, pools))
     assert np.array_equal(new_len, want_len) and new_len.tolist() == [256, 1000, 136, 137, 40]
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_negative_lengths_stay(tree):
+    c = U.batch(104, ctx=[20, 35], n=[9, 11], heads=(2, 2), tree=tree)
+    pools = U.quant_pools(c)
+    *want, want_len = R.compact_quant(c, *pools, [-1, 10])
+    c["ctx"][0] = want_len[0] = -3
+    after, new_len = compacted(c, pools, [8, 10])
+    assert all(np.array_equal(x, y) for x, y in zip(after, want))
+    assert np.array_equal(new_len, want_len)
