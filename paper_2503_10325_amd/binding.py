@@ -424,49 +424,63 @@ def _tensor_types():
     return _types
 
 
-def _typed(t, dtype, what):
-    """The pointer of a contiguous tensor of that type (None: NULL); another type would be read as this one's bits."""
+def _tensor(t, dtype, entries, what):
+    """The pointer of a contiguous tensor of that type, of at least so many entries (None: NULL).  The calls follow the descriptor: another type
+    would be read as this one's bits, and a smaller tensor beyond its end."""
     if t is None:
         return None
+    if t.dtype is dtype and t.is_contiguous() and t.numel() >= entries:
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} expected, not {t.dtype}")
     if not t.is_contiguous():
         raise AssertionError("tensors handed to the library must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{what}: {entries} entries expected, not {t.numel()}")
 
 
-def _pointers(dtype, names, *tensors):
-    """_typed for several: one call for all of them."""
-    out = []
-    for i, t in enumerate(tensors):
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype is not dtype or not t.is_contiguous():
-            _typed(t, dtype, names[i])
-        out.append(t.data_ptr())
-    return out
+def _places(batch, width, tokens, i32, block_table, ctx_len, q_offsets, parent):
+    """Pointers of what says where a batch's tokens lie; the block table has rows of `width` pages (of one request, or flat: as many at least)."""
+    try:                                              # (_tensor four times over costs 0.4 us more)
+        if (block_table.dtype is i32 and ctx_len.dtype is i32 and q_offsets.dtype is i32
+                and block_table.shape == (batch, width) and ctx_len.numel() >= batch and q_offsets.numel() > batch
+                and block_table.is_contiguous() and ctx_len.is_contiguous() and q_offsets.is_contiguous()
+                and (parent is None or (parent.dtype is i32 and parent.numel() >= tokens and parent.is_contiguous()))):
+            return block_table.data_ptr(), ctx_len.data_ptr(), q_offsets.data_ptr(), None if parent is None else parent.data_ptr()
+    except AttributeError:                            # (None, which the library refuses itself)
+        pass
+    if block_table is not None and batch > 1 and block_table.dim() == 2 and block_table.shape[1] != width:
+        raise ValueError(f"block_table: rows of {width} pages expected, not of {block_table.shape[1]}")
+    return (_tensor(block_table, i32, batch * width, "block_table"), _tensor(ctx_len, i32, batch, "ctx_len"),
+            _tensor(q_offsets, i32, batch and batch + 1, "q_offsets"), _tensor(parent, i32, tokens, "parent"))
 
 
-_PLACES = ("block_table", "ctx_len", "q_offsets", "parent", "stop_node", "new_len")
+_current_device = None
 
 
-def _stream_beside(stream, t) -> int:
-    """The stream's handle (None: the current one); the cache `t` has to lie on its device."""
-    at = t.get_device()
-    if at >= 0:
-        import torch
-        on = torch.cuda.current_device() if stream is None else stream.device_index
-        if on != at:
-            raise ValueError(f"the cache lies on device {at}, the stream belongs to device {on}")
-    return _stream(stream)
+def _stream_beside(stream, at) -> int:
+    """The stream's handle (None: the current one) for a call on tensors of device `at`."""
+    global _current_device
+    if at < 0:
+        return _stream(stream)
+    if stream is not None:
+        on, handle = stream.device_index, stream.cuda_stream
+    else:
+        if _current_device is None:
+            import torch
+            _stream(None)                             # (the tensors exist: nothing is left to initialise)
+            _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        on = _current_device()
+        handle = _raw_stream(on)
+    if on != at:
+        raise ValueError(f"the cache lies on device {at}, the stream belongs to device {on}")
+    return handle
 
 
-def _rows(t, heads, head_dim, rows, what):
+def _rows(t, heads, head_dim, rows, bf16, what):
     """(pointer, elements between tokens) of a [tokens, heads, head_dim] bf16 tensor whose tokens may lie apart."""
     if t is None:
         return None, 0
-    if t.dtype is not _tensor_types()[2]:
+    if t.dtype is not bf16:
         raise TypeError(f"{what}: torch.bfloat16 expected, not {t.dtype}")
     apart, head, one = t.stride()                     # (ValueError for another number of dimensions)
     if t.shape != (rows, heads, head_dim) or one != 1 or (heads > 1 and head != head_dim):
@@ -474,17 +488,17 @@ def _rows(t, heads, head_dim, rows, what):
     return t.data_ptr(), apart if rows > 1 else heads * head_dim
 
 
-def _quant_pools(k_pool, v_pool, k_scale, v_scale, desc=None):
+def _quant_pools(k_pool, v_pool, k_scale, v_scale, f32, desc=None):
     """Pointers of an 8-bit cache: k_pool [num_pages, Hkv, D / 16, 16, 16] and v_pool [num_pages, Hkv, D, 16] of torch.float8_e4m3fn
     or torch.uint8, scales [num_pages, Hkv] float32."""
     if k_pool.element_size() != 1 or v_pool.element_size() != 1:
         raise TypeError("the pools of the 8-bit cache have one byte per entry")
     pages, heads, dim, page = v_pool.shape
-    if k_pool.shape != (pages, heads, dim // 16, page, 16) or k_scale.shape != (pages, heads) or v_scale.shape != (pages, heads):
+    scales = (pages, heads)
+    if k_pool.shape != (pages, heads, dim // 16, page, 16) or k_scale.shape != scales or v_scale.shape != scales:
         raise ValueError("k_pool [num_pages, Hkv, D / 16, 16, 16], v_pool [num_pages, Hkv, D, 16] and scales [num_pages, Hkv] expected")
     if desc is not None and (heads != desc.num_kv_heads or dim != desc.head_dim):
         raise ValueError(f"a cache of {heads} heads of {dim} dimensions, the descriptor has {desc.num_kv_heads} of {desc.head_dim}")
-    f32 = _tensor_types()[1]
     if k_scale.dtype is not f32 or v_scale.dtype is not f32:
         raise TypeError("k_scale, v_scale: torch.float32 expected")
     if not (k_pool.is_contiguous() and v_pool.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
@@ -492,14 +506,16 @@ def _quant_pools(k_pool, v_pool, k_scale, v_scale, desc=None):
     return k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
 
 
-def _append(fn, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream):
-    i32, f32, bf16 = _tensor_types()
-    D, total, Hkv = desc.head_dim, desc.total_q, desc.num_kv_heads
-    qp, qs = _rows(q, desc.num_q_heads, D, total, "q")
-    kp, ks = _rows(k, Hkv, D, total, "k")
-    vp, vs = _rows(v, Hkv, D, total, "v")
-    rc = fn(desc, qp, qs, kp, ks, vp, vs, _typed(inv_freq, f32, "inv_freq"), _typed(positions, i32, "positions"), *pools,
-            *_pointers(i32, _PLACES, block_table, ctx_len, q_offsets, parent), _typed(q_out, bf16, "q_out"), stream)
+def _append(fn, desc, types, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream, at):
+    i32, f32, bf16 = types
+    Hq, D, total, Hkv = desc.num_q_heads, desc.head_dim, desc.total_q, desc.num_kv_heads
+    qp, qs = _rows(q, Hq, D, total, bf16, "q")
+    kp, ks = _rows(k, Hkv, D, total, bf16, "k")
+    vp, vs = _rows(v, Hkv, D, total, bf16, "v")
+    rc = fn(desc, qp, qs, kp, ks, vp, vs, _tensor(inv_freq, f32, desc.rotary_dim // 2, "inv_freq"),
+            _tensor(positions, i32, total, "positions"), *pools,
+            *_places(desc.batch, desc.max_pages_per_req, total, i32, block_table, ctx_len, q_offsets, parent),
+            _tensor(q_out, bf16, total * Hq * D, "q_out"), _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError(fn.__name__, rc)
 
@@ -508,13 +524,16 @@ def spec_append_kv(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, bloc
                    positions=None, stream=None) -> None:
     """Device tensors: q [total_q, Hq, D], k and v [total_q, Hkv, D] bf16 (tokens may lie apart, as slices of one projection do),
     inv_freq [rotary_dim / 2] float32, pools [num_pages, Hkv, 16, D] bf16 (modified), the rest int32; q_out [total_q, Hq, D] bf16."""
-    bf16 = _tensor_types()[2]
+    types = _tensor_types()
     want = (desc.num_pages, desc.num_kv_heads, desc.page_size, desc.head_dim)
     if k_pool.shape != want or v_pool.shape != want:
         raise ValueError(f"pools of {want} expected, as in the descriptor")
-    pools = (_typed(k_pool, bf16, "k_pool"), _typed(v_pool, bf16, "v_pool"))
-    _append(lib().spec_append_kv, desc, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions,
-            _stream_beside(stream, k_pool))
+    bf16, at = types[2], k_pool.get_device()
+    if (k_pool.dtype is bf16 and v_pool.dtype is bf16 and k_pool.is_contiguous() and v_pool.is_contiguous()):
+        pools = (k_pool.data_ptr(), v_pool.data_ptr())
+    else:
+        pools = (_tensor(k_pool, bf16, 0, "k_pool"), _tensor(v_pool, bf16, 0, "v_pool"))
+    _append(lib().spec_append_kv, desc, types, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream, at)
 
 
 def spec_append_kv_quant(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets,
@@ -522,8 +541,9 @@ def spec_append_kv_quant(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool
     """spec_append_kv into an 8-bit cache (pools and scales modified)."""
     if k_pool.shape[0] != desc.num_pages:
         raise ValueError(f"pools of {desc.num_pages} pages expected, as in the descriptor")
-    _append(lib().spec_append_kv_quant, desc, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale, desc), block_table,
-            ctx_len, q_offsets, parent, q_out, positions, _stream_beside(stream, k_pool))
+    types, at = _tensor_types(), k_pool.get_device()
+    _append(lib().spec_append_kv_quant, desc, types, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale, types[1], desc),
+            block_table, ctx_len, q_offsets, parent, q_out, positions, stream, at)
 
 
 def spec_verify_attn_quant_workspace_size(desc: SpecAttnDesc) -> int:
@@ -532,14 +552,19 @@ def spec_verify_attn_quant_workspace_size(desc: SpecAttnDesc) -> int:
 
 def spec_verify_attn_quant(desc: SpecAttnDesc, q, k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, out,
                            lse=None, workspace=None, stream=None) -> None:
-    """spec_verify_attn over an 8-bit cache; workspace uint8 of at least spec_verify_attn_quant_workspace_size(desc) bytes."""
+    """spec_verify_attn over an 8-bit cache; workspace of at least spec_verify_attn_quant_workspace_size(desc) bytes."""
     i32, f32, bf16 = _tensor_types()
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _typed(q, bf16, "q"),
-                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, desc),
-                                      *_pointers(i32, _PLACES, block_table, ctx_len, q_offsets, parent),
-                                      _typed(out, f32 if desc.out_dtype == SPEC_F32 else bf16, "out"),
-                                      _typed(lse, f32, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, k_pool))
+    at, total = k_pool.get_device(), desc.total_q
+    rows = total * desc.num_q_heads
+    entries = rows * desc.head_dim
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.nbytes
+    rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _tensor(q, bf16, entries, "q"),
+                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, f32, desc),
+                                      *_places(desc.batch, desc.max_pages_per_req, total, i32, block_table, ctx_len, q_offsets, parent),
+                                      _tensor(out, f32 if desc.out_dtype == SPEC_F32 else bf16, entries, "out"),
+                                      _tensor(lse, f32, rows, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError("spec_verify_attn_quant", rc)
 
@@ -554,11 +579,15 @@ def spec_describe_attn_quant_plan(desc: SpecAttnDesc) -> str:
 
 def spec_compact_kv_quant(k_pool, v_pool, k_scale, v_scale, block_table, ctx_len, q_offsets, parent, stop_node, new_len=None,
                           stream=None) -> None:
-    """spec_compact_kv over an 8-bit cache (pools and scales modified in place); the rest int32 device tensors."""
-    pools = _quant_pools(k_pool, v_pool, k_scale, v_scale)
+    """spec_compact_kv over an 8-bit cache (pools and scales modified in place); the rest int32 device tensors.  parent, if given, has an entry for
+    every token up to the last of q_offsets, whose value only the device knows."""
+    (i32, f32, _), at = _tensor_types(), k_pool.get_device()
+    pools = _quant_pools(k_pool, v_pool, k_scale, v_scale, f32)
     pages, heads, dim, page = v_pool.shape
-    places = _pointers(_tensor_types()[0], _PLACES, block_table, ctx_len, q_offsets, parent, stop_node, new_len)
-    rc = lib().spec_compact_kv_quant(ctx_len.shape[0], heads, dim, page, block_table.shape[1], pages, *pools, *places,
-                                     _stream_beside(stream, k_pool))
+    B, width = ctx_len.shape[0], block_table.shape[1]
+    rc = lib().spec_compact_kv_quant(B, heads, dim, page, width, pages, *pools,
+                                     *_places(B, width, 0, i32, block_table, ctx_len, q_offsets, parent),
+                                     _tensor(stop_node, i32, B, "stop_node"), _tensor(new_len, i32, B, "new_len"),
+                                     _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError("spec_compact_kv_quant", rc)
