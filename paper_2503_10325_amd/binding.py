@@ -424,34 +424,37 @@ def _tensor_types():
     return _types
 
 
-def _tensor(t, dtype, entries, what):
-    """The pointer of a contiguous tensor of that type, of at least so many entries (None: NULL).  The calls follow the descriptor: another type
-    would be read as this one's bits, and a smaller tensor beyond its end."""
+def _tensor(t, dtype, entries, at, what):
+    """The pointer of a contiguous tensor of that type, of at least so many entries, on device `at` (None: NULL).  The calls follow the descriptor: another
+    type would be read as this one's bits, and a smaller tensor, or one of another device, beyond its end."""
     if t is None:
         return None
-    if t.dtype is dtype and t.is_contiguous() and t.numel() >= entries:
+    if t.dtype is dtype and t.is_contiguous() and t.numel() >= entries and t.get_device() == at:
         return t.data_ptr()
     if t.dtype is not dtype:
         raise TypeError(f"{what}: {dtype} expected, not {t.dtype}")
     if not t.is_contiguous():
         raise AssertionError("tensors handed to the library must be contiguous")
-    raise ValueError(f"{what}: {entries} entries expected, not {t.numel()}")
+    if t.numel() < entries:
+        raise ValueError(f"{what}: {entries} entries expected, not {t.numel()}")
+    raise ValueError(f"{what} lies on {t.device}, the cache does not")
 
 
-def _places(batch, width, tokens, i32, block_table, ctx_len, q_offsets, parent):
+def _places(batch, width, tokens, at, i32, block_table, ctx_len, q_offsets, parent):
     """Pointers of what says where a batch's tokens lie; the block table has rows of `width` pages (of one request, or flat: as many at least)."""
     try:                                              # (_tensor four times over costs 0.4 us more)
         if (block_table.dtype is i32 and ctx_len.dtype is i32 and q_offsets.dtype is i32
                 and block_table.shape == (batch, width) and ctx_len.numel() >= batch and q_offsets.numel() > batch
                 and block_table.is_contiguous() and ctx_len.is_contiguous() and q_offsets.is_contiguous()
-                and (parent is None or (parent.dtype is i32 and parent.numel() >= tokens and parent.is_contiguous()))):
+                and block_table.get_device() == at and ctx_len.get_device() == at and q_offsets.get_device() == at
+                and (parent is None or (parent.dtype is i32 and parent.numel() >= tokens and parent.is_contiguous() and parent.get_device() == at))):
             return block_table.data_ptr(), ctx_len.data_ptr(), q_offsets.data_ptr(), None if parent is None else parent.data_ptr()
     except AttributeError:                            # (None, which the library refuses itself)
         pass
     if block_table is not None and batch > 1 and block_table.dim() == 2 and block_table.shape[1] != width:
         raise ValueError(f"block_table: rows of {width} pages expected, not of {block_table.shape[1]}")
-    return (_tensor(block_table, i32, batch * width, "block_table"), _tensor(ctx_len, i32, batch, "ctx_len"),
-            _tensor(q_offsets, i32, batch and batch + 1, "q_offsets"), _tensor(parent, i32, tokens, "parent"))
+    return (_tensor(block_table, i32, batch * width, at, "block_table"), _tensor(ctx_len, i32, batch, at, "ctx_len"),
+            _tensor(q_offsets, i32, batch and batch + 1, at, "q_offsets"), _tensor(parent, i32, tokens, at, "parent"))
 
 
 _current_device = None
@@ -461,7 +464,7 @@ def _stream_beside(stream, at) -> int:
     """The stream's handle (None: the current one) for a call on tensors of device `at`."""
     global _current_device
     if at < 0:
-        return _stream(stream)
+        raise ValueError("the cache has to lie on a GPU device")
     if stream is not None:
         on, handle = stream.device_index, stream.cuda_stream
     else:
@@ -476,7 +479,7 @@ def _stream_beside(stream, at) -> int:
     return handle
 
 
-def _rows(t, heads, head_dim, rows, bf16, what):
+def _rows(t, heads, head_dim, rows, at, bf16, what):
     """(pointer, elements between tokens) of a [tokens, heads, head_dim] bf16 tensor whose tokens may lie apart."""
     if t is None:
         return None, 0
@@ -485,10 +488,12 @@ def _rows(t, heads, head_dim, rows, bf16, what):
     apart, head, one = t.stride()                     # (ValueError for another number of dimensions)
     if t.shape != (rows, heads, head_dim) or one != 1 or (heads > 1 and head != head_dim):
         raise ValueError(f"{what}: [{rows}, {heads}, {head_dim}] with contiguous heads expected")
+    if t.get_device() != at:
+        raise ValueError(f"{what} lies on {t.device}, the cache does not")
     return t.data_ptr(), apart if rows > 1 else heads * head_dim
 
 
-def _quant_pools(k_pool, v_pool, k_scale, v_scale, f32, desc=None):
+def _quant_pools(k_pool, v_pool, k_scale, v_scale, at, f32, desc=None):
     """Pointers of an 8-bit cache: k_pool [num_pages, Hkv, D / 16, 16, 16] and v_pool [num_pages, Hkv, D, 16] of torch.float8_e4m3fn
     or torch.uint8, scales [num_pages, Hkv] float32."""
     if k_pool.element_size() != 1 or v_pool.element_size() != 1:
@@ -503,19 +508,21 @@ def _quant_pools(k_pool, v_pool, k_scale, v_scale, f32, desc=None):
         raise TypeError("k_scale, v_scale: torch.float32 expected")
     if not (k_pool.is_contiguous() and v_pool.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
         raise AssertionError("tensors handed to the library must be contiguous")
+    if not (v_pool.get_device() == at and k_scale.get_device() == at and v_scale.get_device() == at):
+        raise ValueError("the pools and scales of a cache have to lie on one device")
     return k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
 
 
 def _append(fn, desc, types, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream, at):
     i32, f32, bf16 = types
     Hq, D, total, Hkv = desc.num_q_heads, desc.head_dim, desc.total_q, desc.num_kv_heads
-    qp, qs = _rows(q, Hq, D, total, bf16, "q")
-    kp, ks = _rows(k, Hkv, D, total, bf16, "k")
-    vp, vs = _rows(v, Hkv, D, total, bf16, "v")
-    rc = fn(desc, qp, qs, kp, ks, vp, vs, _tensor(inv_freq, f32, desc.rotary_dim // 2, "inv_freq"),
-            _tensor(positions, i32, total, "positions"), *pools,
-            *_places(desc.batch, desc.max_pages_per_req, total, i32, block_table, ctx_len, q_offsets, parent),
-            _tensor(q_out, bf16, total * Hq * D, "q_out"), _stream_beside(stream, at))
+    qp, qs = _rows(q, Hq, D, total, at, bf16, "q")
+    kp, ks = _rows(k, Hkv, D, total, at, bf16, "k")
+    vp, vs = _rows(v, Hkv, D, total, at, bf16, "v")
+    rc = fn(desc, qp, qs, kp, ks, vp, vs, _tensor(inv_freq, f32, desc.rotary_dim // 2, at, "inv_freq"),
+            _tensor(positions, i32, total, at, "positions"), *pools,
+            *_places(desc.batch, desc.max_pages_per_req, total, at, i32, block_table, ctx_len, q_offsets, parent),
+            _tensor(q_out, bf16, total * Hq * D, at, "q_out"), _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError(fn.__name__, rc)
 
@@ -529,10 +536,10 @@ def spec_append_kv(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool, bloc
     if k_pool.shape != want or v_pool.shape != want:
         raise ValueError(f"pools of {want} expected, as in the descriptor")
     bf16, at = types[2], k_pool.get_device()
-    if (k_pool.dtype is bf16 and v_pool.dtype is bf16 and k_pool.is_contiguous() and v_pool.is_contiguous()):
+    if (k_pool.dtype is bf16 and v_pool.dtype is bf16 and k_pool.is_contiguous() and v_pool.is_contiguous() and v_pool.get_device() == at):
         pools = (k_pool.data_ptr(), v_pool.data_ptr())
     else:
-        pools = (_tensor(k_pool, bf16, 0, "k_pool"), _tensor(v_pool, bf16, 0, "v_pool"))
+        pools = (_tensor(k_pool, bf16, 0, at, "k_pool"), _tensor(v_pool, bf16, 0, at, "v_pool"))
     _append(lib().spec_append_kv, desc, types, q, k, v, inv_freq, pools, block_table, ctx_len, q_offsets, parent, q_out, positions, stream, at)
 
 
@@ -542,7 +549,7 @@ def spec_append_kv_quant(desc: SpecAppendDesc, q, k, v, inv_freq, k_pool, v_pool
     if k_pool.shape[0] != desc.num_pages:
         raise ValueError(f"pools of {desc.num_pages} pages expected, as in the descriptor")
     types, at = _tensor_types(), k_pool.get_device()
-    _append(lib().spec_append_kv_quant, desc, types, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale, types[1], desc),
+    _append(lib().spec_append_kv_quant, desc, types, q, k, v, inv_freq, _quant_pools(k_pool, v_pool, k_scale, v_scale, at, types[1], desc),
             block_table, ctx_len, q_offsets, parent, q_out, positions, stream, at)
 
 
@@ -560,11 +567,13 @@ def spec_verify_attn_quant(desc: SpecAttnDesc, q, k_pool, v_pool, k_scale, v_sca
     ws_bytes = 0
     if workspace is not None:
         ws_bytes = workspace.nbytes
-    rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _tensor(q, bf16, entries, "q"),
-                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, f32, desc),
-                                      *_places(desc.batch, desc.max_pages_per_req, total, i32, block_table, ctx_len, q_offsets, parent),
-                                      _tensor(out, f32 if desc.out_dtype == SPEC_F32 else bf16, entries, "out"),
-                                      _tensor(lse, f32, rows, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, at))
+        if workspace.get_device() != at:
+            raise ValueError(f"workspace lies on {workspace.device}, the cache does not")
+    rc = lib().spec_verify_attn_quant(desc, k_pool.shape[0], _tensor(q, bf16, entries, at, "q"),
+                                      *_quant_pools(k_pool, v_pool, k_scale, v_scale, at, f32, desc),
+                                      *_places(desc.batch, desc.max_pages_per_req, total, at, i32, block_table, ctx_len, q_offsets, parent),
+                                      _tensor(out, f32 if desc.out_dtype == SPEC_F32 else bf16, entries, at, "out"),
+                                      _tensor(lse, f32, rows, at, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError("spec_verify_attn_quant", rc)
 
@@ -582,12 +591,12 @@ def spec_compact_kv_quant(k_pool, v_pool, k_scale, v_scale, block_table, ctx_len
     """spec_compact_kv over an 8-bit cache (pools and scales modified in place); the rest int32 device tensors.  parent, if given, has an entry for
     every token up to the last of q_offsets, whose value only the device knows."""
     (i32, f32, _), at = _tensor_types(), k_pool.get_device()
-    pools = _quant_pools(k_pool, v_pool, k_scale, v_scale, f32)
+    pools = _quant_pools(k_pool, v_pool, k_scale, v_scale, at, f32)
     pages, heads, dim, page = v_pool.shape
     B, width = ctx_len.shape[0], block_table.shape[1]
     rc = lib().spec_compact_kv_quant(B, heads, dim, page, width, pages, *pools,
-                                     *_places(B, width, 0, i32, block_table, ctx_len, q_offsets, parent),
-                                     _tensor(stop_node, i32, B, "stop_node"), _tensor(new_len, i32, B, "new_len"),
+                                     *_places(B, width, 0, at, i32, block_table, ctx_len, q_offsets, parent),
+                                     _tensor(stop_node, i32, B, at, "stop_node"), _tensor(new_len, i32, B, at, "new_len"),
                                      _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError("spec_compact_kv_quant", rc)

@@ -1,9 +1,11 @@
-"""Tensors that the cache operators take as they come: larger than the batch, flat, of one request."""
+"""Tensors that the cache operators take as they come: larger than the batch, flat, of one request; and those in host
+memory, which they refuse."""
 import pytest
 
 torch = pytest.importorskip("torch")
 
 import cache_util as U
+import test_quant_sizes as S
 from paper_2503_10325_amd import binding as sv
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +65,27 @@ def test_one_request_of_a_wider_table():
 
     (want, want_len), (got, got_len) = step(c, pools), step(c, pools, change)
     assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(got_len, want_len)
+
+
+NAMES = dict(append_bf16=["q", "k", "v", "inv_freq", "k_pool", "v_pool", "block_table", "ctx_len", "q_offsets", "parent", "q_out", "positions"],
+             append_quant=["q", "k_pool", "v_pool", "k_scale", "v_scale", "block_table", "q_out"],
+             attend=["q", "k_pool", "v_pool", "k_scale", "v_scale", "block_table", "ctx_len", "q_offsets", "parent", "out", "lse", "workspace"],
+             compact=["k_pool", "v_pool", "k_scale", "v_scale", "block_table", "ctx_len", "q_offsets", "parent", "stop_node", "new_len"])
+
+
+@pytest.mark.parametrize("call,name", [(call, name) for call, names in NAMES.items() for name in names])
+def test_one_tensor_in_host_memory_is_refused(monkeypatch, call, name):
+    """On the host, before anything is launched."""
+    class Library:                                                        # nothing reaches the GPU, whatever the binding lets through
+        def __getattr__(self, entry):
+            return getattr(real, entry) if entry.endswith("size") else lambda *a: pytest.fail("launched")
+
+    real = sv.lib()
+    monkeypatch.setattr(sv, "_lib", Library())
+    for entry in ("spec_append_kv", "spec_append_kv_quant", "spec_verify_attn_quant", "spec_compact_kv_quant"):
+        def moved(*desc, stream=None, own=getattr(sv, entry), **tensors):
+            own(*desc, **{k: x if k == name else x.cuda() for k, x in tensors.items()})
+        monkeypatch.setattr(sv, entry, moved)
+    run = dict(append_bf16=lambda: S.append("bf16"), append_quant=lambda: S.append("quant"), attend=S.attend, compact=S.compact)[call]
+    with pytest.raises(ValueError, match="device|cache"):
+        run()
