@@ -448,8 +448,12 @@ int32_t spec_append_kv(
  * that sees no position at all gives zeros and lse = -infinity.  Slots behind the last
  * draft are read but take no part, whatever they hold; an entry of a draft that is NaN
  * reaches the rows that see that draft only.  Entries of v below 2^-35 of the largest
- * scale of v in the context may lose precision.  out is exact to about 2^-12 (fp32: 2^-20)
- * of its row's size before it is rounded.  The workspace need not be cleared.
+ * scale of v in the context may lose precision.  Accuracy, for a row that sees L positions
+ * with weights w, with A the largest scale sum_i |q_i k_i| of them and
+ * e = 2^-20 (1 + A) + 2^-24 sqrt(L): before it is rounded, out is within
+ * (2^-11 + e) sum w |v| (out_dtype SPEC_F32: e sum w |v|) and 2^-31 L times 448 times the largest
+ * scale of v of the exact result; lse is within e + 2^-22 |lse|.  Scores (scale <q, k>) are at
+ * most 2^23 in size.  The workspace need not be cleared.
  *
  * spec_compact_kv_quant is spec_compact_kv over it.  A page that entries move to gets the
  * largest of its own scale, if it holds tokens 0 .. ctx_len[b] - 1, and of the scales of

@@ -8,7 +8,8 @@
 //                 lane group g (lanes 16 g .. 16 g + 15, one query row each) ends up with 8 tokens of one page: its scale is one register, and
 //   O^T = V^T P^T takes those 8 weights as its operand without any exchange between lanes.
 // e4m3 is exact in bf16 and fp16.  K's scale rides on the softmax factor; V is fed in fp16, its page's scale on the conversion, relative to the
-// largest scale so far.  A weight is one fp16 term (2^-12 off, a sixteenth of the rounding of a bf16 result), or two for fp32 results.
+// largest scale so far.  A weight is one fp16 term (2^-11 off at most, an eighth of the rounding
+// of a bf16 result, and independent of its neighbours': results end up about 1 % further from the exact ones than with fp32 weights), or two for fp32 results.
 //
 // Work: a request's query rows of a KV head are taken in groups of up to 64 (a wave multiplies each unit with up to four 16-row blocks).
 // Per KV head the units of all requests and groups lie end to end and are cut into ranges of equal cost, one per workgroup, whatever the
