@@ -110,7 +110,7 @@ def _put(pool, scale, pg, h, keys, entries, kept, least):
     new = max(own, least) if kept else least
     view = pool[pg, h]
     if kept and new > own:
-        part = view[:, :kept] if keys else view[:, :kept]
+        part = view[:, :kept]                                     # (slots are the second axis of either layout)
         part[...] = encode_e4m3(E4M3[part] * (own / new))
     for t, x in entries.items():
         code = encode_e4m3(x / new)

@@ -5,7 +5,9 @@
 // is rotated as a linear context is), or the caller's own.  With pairs (x1, x2) of dimensions and a = position * inv_freq:
 //   x1' = s (x1 cos a - x2 sin a),  x2' = s (x2 cos a + x1 sin a).
 // The angle is reduced to a part of a turn in fp64 (at position 10^6 an fp32 angle is off by 0.03), sine and cosine are Taylor
-// polynomials on an eighth of a turn in fp32, and what is stored is rounded once.
+// polynomials on an eighth of a turn in fp32 (off by 2^-23.5 at most, a rounded fp32 value by 2^-25), and what is stored is rounded once.  Of a
+// long prompt's keys that moves 4 in 10^7 to a neighbouring e4m3 code (sine and cosine in fp64, rounded: 2 to 3), 2^-3 of their size at
+// most away: not worth polynomials in fp64.
 //
 // Work: a workgroup takes the (up to 16) new tokens of one page, for a share of the heads; the angles of those tokens are
 // worked out once, in LDS, for all of them.  Page slots are numbered without a scan: request b's start at q_offsets[b] / 16 + 2 b, which

@@ -17,9 +17,9 @@
 // leaves a partial result and its sum of weights; the workgroup that finishes the last piece merges them, in their order.  The four or
 // eight waves of a workgroup take units in turn and merge through LDS.
 //
-// Bound by memory up to 48 rows (64 requests x 8 KV heads x 2048 tokens, 8 to 32 rows: 54 to 58 us, 5.0 to 4.7 TB/s; 4096 tokens 5.2), by the
-// vector and matrix instructions of a SIMD's two waves beyond (64 rows 66 us; trees of 64 nodes, 256 rows, 4096 tokens: 800 TFLOP/s, vector issue
-// 55 %, matrix cores 31 %), by latency for few tokens: the launch, two dependent trips to memory before the first page, and the merge are 8 us.
+// Bound by memory up to 48 rows (64 requests x 8 KV heads x 2048 tokens, 8 to 32 rows: 55 to 60 us, 4.9 to 4.7 TB/s; 4096 tokens 5.15), by the
+// vector and matrix instructions of a SIMD's two waves beyond (64 rows 67 us; trees of 64 nodes, 256 rows, 4096 tokens: 84 to 91 us, 770 to 830
+// TFLOP/s, vector issue 54 %, matrix cores 33 %), by latency for few tokens: the launch, two dependent trips to memory before the first page, and the merge are 8 us.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -124,7 +124,7 @@ __device__ __forceinline__ RowGroups group_rows(int rows, int most, int halves) 
 }
 // What a unit costs its workgroup by the 16-row blocks it is multiplied with, and what a group of rows costs besides (its start, its end and its share
 // of merges: 10 to 15 us beside another workgroup's units, of which there are two in a microsecond).  300 + 60 blocks in place of it: 5 requests
-// of 1001 to 15999 tokens 25.8 -> 28.6 us, the serving batch of 64 alike.
+// of 1001 to 15999 tokens, fp32 results, 29.7 -> 32.6 us, the serving batch of 64 alike.
 __device__ __forceinline__ int unit_cost(int blocks) { return 24 + 4 * blocks; }
 // Units are counted in chunks of 2^shift (0 unless the block table has room for so many that the batch's cost would pass 31 bits).
 __device__ __forceinline__ int chunks_of(int units, int shift) { return (units + (1 << shift) - 1) >> shift; }
@@ -134,7 +134,7 @@ constexpr int kMostHead = 600 + 150 * kQaBlocks;
 constexpr int kWholeCost = 456;               // a group whose units cost at most this (16 of few rows) is not cut: its merge would take longer
 constexpr int kLeastRange = 256;              // ranges cost at least this, and
 constexpr float kRangeRoot = 7.5f;            // this times the root of what a group costs (or as much as a group): n pieces of a group take a time of group / n
-                                              // and their merge one of n (1 request of 16000 tokens x 8 KV heads: 25.8 -> 20.5 us)
+                                              // and their merge one of n (1 request of 16000 tokens x 8 KV heads: 27.1 -> 22.3 us)
 
 // The requests, 64 at a time: lane i holds request 64 k + i.
 struct Requests {
@@ -586,7 +586,6 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
   }
 
   for (int i = 0; i < mine; ++i, t += per_half) {
-    const unsigned at = 0;
     const int behind = mine - 1 - i;                            // units of this wave after this one
     // K of this unit is here: behind it the next one's K, and V
     wait_loads<kVLoads>();
@@ -596,13 +595,13 @@ __device__ __forceinline__ void quant_piece(Sh& S, const QuantPiece& J) {
     raw4 kr[kH][2], qr[2][NB];
 #pragma unroll
     for (int h = 0; h < kH; ++h) {
-      kr[h][0] = *lds_raw4(k_at + at + (0u ^ k_flip) + 1024 * h);
-      kr[h][1] = *lds_raw4(k_at + at + (64u ^ k_flip) + 1024 * h);
+      kr[h][0] = *lds_raw4(k_at + (0u ^ k_flip) + 1024 * h);
+      kr[h][1] = *lds_raw4(k_at + (64u ^ k_flip) + 1024 * h);
     }
 #pragma unroll
     for (int qi = 0; qi < kAhead; ++qi) qr[0][qi] = q_mine[qi * 2 * kH * kWave];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K has been read
-    if (behind > 0) issue_k(ring + at);
+    if (behind > 0) issue_k(ring);
     __builtin_amdgcn_s_setprio(1);                              // products before another wave's softmax
 #pragma unroll
     for (int step = 0; step < 2 * kH; ++step) {
@@ -921,8 +920,8 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.Hq / a.Hkv);
   const int blocks = static_cast<int>(std::max<int64_t>(1, (rows + 15) / 16));
   // Rows that are too many for a wave go to two halves of a workgroup where groups in workgroups of their own would be twice as many as those: they
-  // then read the same pages one after the other (64 requests x 8 KV heads x 2048 tokens, 128 rows: 128 us, in halves 103); with a workgroup for each
-  // group, side by side, halves gain nothing and cut more (16 requests x 8 KV heads x 4096 tokens, 256 rows: 104 us, 106).
+  // then read the same pages one after the other (64 requests x 8 KV heads x 2048 tokens, 128 rows: 119 us, in halves 97; 80 rows: 110, 79); with a
+  // workgroup for each group, side by side, halves gain nothing and cut more (16 requests x 8 KV heads x 4096 tokens, 256 rows: 89 us, 92).
   int most = most_blocks(a.D, a.out_dtype == kF32 ? 2 : 1);
   p.groups = (blocks + most - 1) / most;
   p.halves = p.groups > 1 && static_cast<int64_t>(a.Hkv) * a.B * p.groups >= 1024 ? 2 : 1;
@@ -930,8 +929,8 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a) {
   p.groups = (blocks + most - 1) / most;
   p.rows = 16 * std::min(blocks + p.halves - 1, most);
   // Two workgroups of four waves to a compute unit overlap the starts and ends of their pieces, where there are two pieces for it; else one of eight, whose
-  // waves share one (1 request of 16000 tokens x 8 KV heads: 52 us with four, 29 with eight; 16 of 2000: 24.8, 22.7; 64 of 2048: 55.2, 58.3;
-  // 256 of 512: 69, 89).
+  // waves share one (1 request of 16000 tokens x 8 KV heads, single tokens: 23.2 us with four, 21.6 with eight; 16 of 2000: 23.2, 24.0; 64 of 2048:
+  // 57, 61; 256 of 512: 68, 89).
   p.waves = static_cast<int64_t>(a.Hkv) * a.B * p.groups < 512 ? 8 : 4;
   p.ranges = std::max(1, (p.waves == 8 ? 256 : 512) / a.Hkv);
   // the cost of the batch stays below 2^31 (no chunk is long enough where there are millions of groups: shift is then 30 and the call is refused)
