@@ -16,7 +16,9 @@
  * Around them, what a paged cache needs: spec_append_kv writes the step's keys and values
  * (rotated by their positions) before the attention, spec_compact_kv tidies up after
  * acceptance; spec_append_kv_quant, spec_verify_attn_quant and spec_compact_kv_quant are
- * the same three over a cache of 8-bit values.
+ * the same three over a cache of 8-bit values.  spec_append_latent, spec_absorb_latent,
+ * spec_verify_attn_latent, spec_expand_latent and spec_compact_latent are the step of target
+ * models whose cache holds one latent vector per token, shared by all heads.
  *
  * Conventions common to every entry point
  *   - Pointers are DEVICE pointers unless the comment says "host".
@@ -489,6 +491,116 @@ int32_t spec_compact_kv_quant(
     int32_t B, int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t max_pages_per_req, int32_t num_pages,
     void* k_pool, void* v_pool, float* k_scale, float* v_scale, const int32_t* block_table,
     const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent, const int32_t* stop_node,
+    int32_t* new_len,            /* optional [B]                                       */
+    void* stream);
+
+/* ------------------------------------------------------------------------------
+ * The cache of latents: spec_append_latent, spec_absorb_latent, spec_verify_attn_latent,
+ * spec_expand_latent, spec_compact_latent
+ *
+ * Target models whose keys and values of all heads are products of one latent c of C =
+ * latent_dim elements per token, k_h = [W_k,h c | r] and v_h = W_v,h c, with R = rope_dim
+ * more elements r, rotated by position, that the keys of all heads share.  The cache holds
+ * [c | r] of a token as a row of W = C + R elements: pool [num_pages, page_size, W] bf16.
+ * The weights go to the other side of the attention (the absorbed form: for at most
+ * 128 drafts the cheaper one),
+ *   <q_h, k_h> = <[q_nope W_k,h | q_rope], [c | r]>,
+ *   sum_t p_t v_h,t = W_v,h sum_t p_t c_t,
+ * so that a step is: append, absorb, attention over the rows (the first C elements are
+ * the values), expand; compaction after acceptance.  One descriptor says what all of them
+ * need of the layer and of the batch.
+ *
+ * Rows of requests only: q_offsets[B] is the number of rows there are, rows of inputs and
+ * outputs from there on are neither read nor written.  Positions, draft trees, pages and
+ * slots are as for spec_append_kv and spec_verify_attn_quant.  Tensors are 16-byte aligned,
+ * strides multiples of 8 elements (SPEC_ERR_SHAPE otherwise), outputs overlap no input.
+ * total_q / 16 + 2 batch is at most 2^23, num_heads at most 1024 (SPEC_ERR_UNSUPPORTED).
+ * ---------------------------------------------------------------------------- */
+typedef struct {
+  int32_t batch;             /* B >= 0                                              */
+  int32_t num_heads;         /* H                                                   */
+  int32_t latent_dim;        /* C: 256 or 512                                       */
+  int32_t rope_dim;          /* R: 32 or 64                                         */
+  int32_t nope_dim;          /* elements of a query that are not rotated: 64 or 128 */
+  int32_t value_dim;         /* of a head: 64 or 128                                */
+  int32_t page_size;         /* tokens per cache page: 16                           */
+  int32_t total_q;           /* rows of the step's tensors; q_offsets[B] at most    */
+  int32_t max_q_per_req;     /* upper bound of the new tokens of a request          */
+  int32_t max_pages_per_req; /* row stride of block_table                           */
+  int32_t num_pages;         /* pages of the pool                                   */
+  int32_t interleaved;       /* rotated pairs: 0 = (i, i + R / 2), 1 = (2 i, 2 i + 1) */
+  int32_t out_dtype;         /* spec_dtype of the attention's `out`                 */
+  float rotary_scale;        /* of rotated elements; 0 selects 1                    */
+  float norm_eps;            /* >= 0                                                */
+  float scale;               /* of the scores; 0 selects 1 / sqrt(nope_dim + rope_dim) */
+} spec_latent_desc;
+
+/* New tokens into the cache: row q_offsets[b] + i to slot ctx_len[b] + i, prompts (any
+ * length, parent == NULL) and drafts alike.  With norm_weight g the latent x is normalised
+ * on the way, c = x g / sqrt(mean(x^2) + norm_eps), else copied; the shared key is rotated.
+ * Results are rounded once.  What spec_append_kv says of slots without a page holds here. */
+int32_t spec_append_latent(
+    const spec_latent_desc* desc, /* host                                             */
+    const void* latent, int64_t latent_stride, /* [total_q] rows of C bf16            */
+    const void* key, int64_t key_stride,       /* [total_q] rows of R bf16            */
+    const void* norm_weight,     /* optional [C] bf16                                  */
+    const float* inv_freq,       /* [R / 2]                                            */
+    const int32_t* positions,    /* optional [total_q] rotation positions              */
+    void* pool,                  /* [num_pages, page_size, C + R] bf16, modified       */
+    const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent, void* stream);
+
+/* Queries into the latent space: q_out[t, h] = [q[t, h, :nope_dim] w_key[h] | the rest
+ * rotated], fp32 accumulation, rounded once. */
+int32_t spec_absorb_latent(
+    const spec_latent_desc* desc,
+    const void* q, int64_t q_stride,     /* [total_q] rows of [H, nope_dim + R] bf16   */
+    const void* w_key, int64_t w_stride, /* [nope_dim, C] bf16 per head, w_stride elements
+                                            apart (a slice of [H, nope_dim + value_dim, C]) */
+    const float* inv_freq, const int32_t* positions, const int32_t* ctx_len, const int32_t* q_offsets,
+    const int32_t* parent,
+    void* q_out,                 /* [total_q, H, C + R] bf16                           */
+    void* stream);
+
+/* Bytes of workspace spec_verify_attn_latent uses for this descriptor (host call). */
+size_t spec_verify_attn_latent_workspace_size(const spec_latent_desc* desc);
+
+/* spec_verify_attn over the cache of latents: out[i, h] = sum_t softmax_t(scale <q[i, h], row t>)
+ * row t[:C], the same masks (at most 128 nodes per request, one for plain decoding).
+ * Positions whose page is outside [0, num_pages), or behind max_pages_per_req pages, count as
+ * not there; a row that sees no position at all gives zeros and lse = -infinity.  Slots
+ * behind the last draft are read but take no part, whatever they hold; an entry of a draft
+ * that is not finite reaches only the rows that see that draft.  Accuracy, for a row that
+ * sees L positions with weights w, with A the largest scale sum_i |q_i k_i| of them and
+ * e = 2^-19 (1 + A) + 2^-28 L: before it is rounded, out is within (2^-8 + e)
+ * sum w |c| (out_dtype SPEC_F32: e sum w |c|) of the exact result; lse is within
+ * e + 2^-22 |lse|.  The workspace need not be cleared. */
+int32_t spec_verify_attn_latent(
+    const spec_latent_desc* desc,
+    const void* q,               /* [total_q, H, C + R] bf16                           */
+    const void* pool, const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent,
+    void* out,                   /* [total_q, H, C] of out_dtype                       */
+    float* lse,                  /* optional [total_q, H]                              */
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/* One-line description of the kernel and the cut spec_verify_attn_latent takes (host). */
+int32_t spec_describe_attn_latent_plan(const spec_latent_desc* desc, char* buf, size_t buf_bytes);
+
+/* Results out of the latent space: out[t, h] = w_value[h] x[t, h], fp32 accumulation, rounded once. */
+int32_t spec_expand_latent(
+    const spec_latent_desc* desc,
+    const void* x,               /* [total_q, H, C] bf16                               */
+    const void* w_value, int64_t w_stride, /* [value_dim, C] bf16 per head, w_stride elements apart */
+    const int32_t* q_offsets,
+    void* out,                   /* [total_q, H, value_dim] bf16                       */
+    void* stream);
+
+/* spec_compact_kv over the cache of latents: rows of `width` elements (a multiple of 8, at
+ * most 576).  Rows whose page (of origin or of destination) is outside the pool stay
+ * where they are; a draft tree has at most 128 nodes, a linear request any number. */
+int32_t spec_compact_latent(
+    int32_t B, int32_t width, int32_t page_size, int32_t max_pages_per_req, int32_t num_pages,
+    void* pool, const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent,
+    const int32_t* stop_node,
     int32_t* new_len,            /* optional [B]                                       */
     void* stream);
 

@@ -30,6 +30,8 @@ EXPORTS = [
     "spec_describe_lm_head_plan",
     "spec_append_kv", "spec_append_kv_quant", "spec_verify_attn_quant_workspace_size", "spec_verify_attn_quant",
     "spec_describe_attn_quant_plan", "spec_compact_kv_quant",
+    "spec_append_latent", "spec_absorb_latent", "spec_verify_attn_latent_workspace_size", "spec_verify_attn_latent",
+    "spec_describe_attn_latent_plan", "spec_expand_latent", "spec_compact_latent",
     "spec_strerror", "spec_abi_version",
 ]
 
@@ -50,6 +52,12 @@ class SpecAppendDesc(ctypes.Structure):
         ("max_q_per_req", ctypes.c_int32), ("max_pages_per_req", ctypes.c_int32), ("num_pages", ctypes.c_int32),
         ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("rotary_scale", ctypes.c_float),
     ]
+
+
+class SpecLatentDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in (
+        "batch", "num_heads", "latent_dim", "rope_dim", "nope_dim", "value_dim", "page_size", "total_q", "max_q_per_req", "max_pages_per_req",
+        "num_pages", "interleaved", "out_dtype")] + [("rotary_scale", ctypes.c_float), ("norm_eps", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
 class SpecAcceptTuning(ctypes.Structure):
@@ -140,6 +148,21 @@ def lib() -> ctypes.CDLL:
         L.spec_describe_attn_quant_plan.argtypes = [ctypes.POINTER(SpecAttnDesc), ctypes.c_char_p, sz]
         L.spec_compact_kv_quant.restype = i32
         L.spec_compact_kv_quant.argtypes = [i32] * 6 + [vp] * 11
+        latent = ctypes.POINTER(SpecLatentDesc)
+        L.spec_append_latent.restype = i32
+        L.spec_append_latent.argtypes = [latent, vp, i64, vp, i64] + [vp] * 9
+        L.spec_absorb_latent.restype = i32
+        L.spec_absorb_latent.argtypes = [latent, vp, i64, vp, i64] + [vp] * 7
+        L.spec_verify_attn_latent_workspace_size.restype = sz
+        L.spec_verify_attn_latent_workspace_size.argtypes = [latent]
+        L.spec_verify_attn_latent.restype = i32
+        L.spec_verify_attn_latent.argtypes = [latent] + [vp] * 9 + [sz, vp]
+        L.spec_describe_attn_latent_plan.restype = i32
+        L.spec_describe_attn_latent_plan.argtypes = [latent, ctypes.c_char_p, sz]
+        L.spec_expand_latent.restype = i32
+        L.spec_expand_latent.argtypes = [latent, vp, vp, i64] + [vp] * 3
+        L.spec_compact_latent.restype = i32
+        L.spec_compact_latent.argtypes = [i32] * 5 + [vp] * 8
         _lib = L
     return _lib
 
@@ -600,3 +623,133 @@ def spec_compact_kv_quant(k_pool, v_pool, k_scale, v_scale, block_table, ctx_len
                                      _stream_beside(stream, at))
     if rc != SPEC_OK:
         raise SpecError("spec_compact_kv_quant", rc)
+
+
+# ---- the cache of latents ----
+def make_latent_desc(batch, num_heads, latent_dim, rope_dim, nope_dim, value_dim, total_q, max_q_per_req, max_pages_per_req, num_pages,
+                     interleaved=False, rotary_scale=0.0, norm_eps=0.0, scale=0.0, out_dtype=SPEC_BF16, page_size=16) -> SpecLatentDesc:
+    return SpecLatentDesc(batch, num_heads, latent_dim, rope_dim, nope_dim, value_dim, page_size, total_q, max_q_per_req, max_pages_per_req,
+                          num_pages, int(interleaved), out_dtype, rotary_scale, norm_eps, scale)
+
+
+def _flat_rows(t, width, rows, at, bf16, what):
+    """(pointer, elements between rows) of a [rows, width] bf16 tensor whose rows may lie apart."""
+    if t is None:
+        return None, 0
+    if t.dtype is not bf16:
+        raise TypeError(f"{what}: torch.bfloat16 expected, not {t.dtype}")
+    apart, one = t.stride()                           # (ValueError for another number of dimensions)
+    if t.shape != (rows, width) or one != 1:
+        raise ValueError(f"{what}: [{rows}, {width}] with contiguous rows expected")
+    if t.get_device() != at:
+        raise ValueError(f"{what} lies on {t.device}, the call's other tensors do not")
+    return t.data_ptr(), apart if rows > 1 else width
+
+
+def _head_weight(t, heads, rows, width, at, bf16, what):
+    """(pointer, elements between heads) of a [heads, rows, width] bf16 weight whose heads may lie apart."""
+    if t is None:
+        return None, 0
+    if t.dtype is not bf16:
+        raise TypeError(f"{what}: torch.bfloat16 expected, not {t.dtype}")
+    apart, row, one = t.stride()
+    if t.shape != (heads, rows, width) or one != 1 or row != width:
+        raise ValueError(f"{what}: [{heads}, {rows}, {width}] with contiguous heads expected")
+    if t.get_device() != at:
+        raise ValueError(f"{what} lies on {t.device}, the call's other tensors do not")
+    return t.data_ptr(), apart if heads > 1 else rows * width
+
+
+def _latent_pool(desc, pool, bf16):
+    """(pointer, device) of a cache of latents [num_pages, 16, latent_dim + rope_dim] bf16."""
+    want = (desc.num_pages, desc.page_size, desc.latent_dim + desc.rope_dim)
+    if pool.shape != want:
+        raise ValueError(f"a pool of {want} expected, as in the descriptor")
+    at = pool.get_device()
+    return _tensor(pool, bf16, 0, at, "pool"), at
+
+
+def spec_append_latent(desc: SpecLatentDesc, latent, key, norm_weight, inv_freq, pool, block_table, ctx_len, q_offsets, parent, positions=None,
+                       stream=None) -> None:
+    """Device tensors: latent [total_q, latent_dim] and key [total_q, rope_dim] bf16 (rows may lie apart, as slices of one projection do), norm_weight
+    [latent_dim] bf16 or None, inv_freq [rope_dim / 2] float32, pool [num_pages, 16, latent_dim + rope_dim] bf16 (modified), the rest int32."""
+    i32, f32, bf16 = _tensor_types()
+    C, R, total = desc.latent_dim, desc.rope_dim, desc.total_q
+    to, at = _latent_pool(desc, pool, bf16)
+    rc = lib().spec_append_latent(desc, *_flat_rows(latent, C, total, at, bf16, "latent"), *_flat_rows(key, R, total, at, bf16, "key"),
+                                  _tensor(norm_weight, bf16, C, at, "norm_weight"), _tensor(inv_freq, f32, R // 2, at, "inv_freq"),
+                                  _tensor(positions, i32, total, at, "positions"), to,
+                                  *_places(desc.batch, desc.max_pages_per_req, total, at, i32, block_table, ctx_len, q_offsets, parent),
+                                  _stream_beside(stream, at))
+    if rc != SPEC_OK:
+        raise SpecError("spec_append_latent", rc)
+
+
+def spec_absorb_latent(desc: SpecLatentDesc, q, w_key, inv_freq, ctx_len, q_offsets, parent, q_out, positions=None, stream=None) -> None:
+    """q [total_q, num_heads, nope_dim + rope_dim] bf16 (tokens may lie apart), w_key [num_heads, nope_dim, latent_dim] bf16 (heads may lie apart, as the
+    slice of one weight's do); q_out [total_q, num_heads, latent_dim + rope_dim] bf16."""
+    i32, f32, bf16 = _tensor_types()
+    H, C, R, N, total, at = desc.num_heads, desc.latent_dim, desc.rope_dim, desc.nope_dim, desc.total_q, q_out.get_device()
+    rc = lib().spec_absorb_latent(desc, *_rows(q, H, N + R, total, at, bf16, "q"), *_head_weight(w_key, H, N, C, at, bf16, "w_key"),
+                                  _tensor(inv_freq, f32, R // 2, at, "inv_freq"), _tensor(positions, i32, total, at, "positions"),
+                                  _tensor(ctx_len, i32, desc.batch, at, "ctx_len"), _tensor(q_offsets, i32, desc.batch and desc.batch + 1, at, "q_offsets"),
+                                  _tensor(parent, i32, total, at, "parent"), _tensor(q_out, bf16, total * H * (C + R), at, "q_out"),
+                                  _stream_beside(stream, at))
+    if rc != SPEC_OK:
+        raise SpecError("spec_absorb_latent", rc)
+
+
+def spec_verify_attn_latent_workspace_size(desc: SpecLatentDesc) -> int:
+    return int(lib().spec_verify_attn_latent_workspace_size(ctypes.byref(desc)))
+
+
+def spec_verify_attn_latent(desc: SpecLatentDesc, q, pool, block_table, ctx_len, q_offsets, parent, out, lse=None, workspace=None, stream=None) -> None:
+    """q [total_q, num_heads, latent_dim + rope_dim] bf16, pool [num_pages, 16, latent_dim + rope_dim] bf16, out [total_q, num_heads, latent_dim] of the
+    descriptor's type, lse [total_q, num_heads] float32 or None; workspace of at least spec_verify_attn_latent_workspace_size(desc) bytes."""
+    i32, f32, bf16 = _tensor_types()
+    held, at = _latent_pool(desc, pool, bf16)
+    rows = desc.total_q * desc.num_heads
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.nbytes
+        if workspace.get_device() != at:
+            raise ValueError(f"workspace lies on {workspace.device}, the cache does not")
+    rc = lib().spec_verify_attn_latent(desc, _tensor(q, bf16, rows * (desc.latent_dim + desc.rope_dim), at, "q"), held,
+                                       *_places(desc.batch, desc.max_pages_per_req, desc.total_q, at, i32, block_table, ctx_len, q_offsets, parent),
+                                       _tensor(out, f32 if desc.out_dtype == SPEC_F32 else bf16, rows * desc.latent_dim, at, "out"),
+                                       _tensor(lse, f32, rows, at, "lse"), _ptr(workspace), ws_bytes, _stream_beside(stream, at))
+    if rc != SPEC_OK:
+        raise SpecError("spec_verify_attn_latent", rc)
+
+
+def spec_describe_attn_latent_plan(desc: SpecLatentDesc) -> str:
+    buf = ctypes.create_string_buffer(256)
+    rc = lib().spec_describe_attn_latent_plan(ctypes.byref(desc), buf, 256)
+    if rc != SPEC_OK:
+        raise SpecError("spec_describe_attn_latent_plan", rc)
+    return buf.value.decode()
+
+
+def spec_expand_latent(desc: SpecLatentDesc, x, w_value, q_offsets, out, stream=None) -> None:
+    """x [total_q, num_heads, latent_dim] bf16, w_value [num_heads, value_dim, latent_dim] bf16 (heads may lie apart); out [total_q, num_heads, value_dim]
+    bf16."""
+    i32, _, bf16 = _tensor_types()
+    H, C, V, total, at = desc.num_heads, desc.latent_dim, desc.value_dim, desc.total_q, out.get_device()
+    rc = lib().spec_expand_latent(desc, _tensor(x, bf16, total * H * C, at, "x"), *_head_weight(w_value, H, V, C, at, bf16, "w_value"),
+                                  _tensor(q_offsets, i32, desc.batch and desc.batch + 1, at, "q_offsets"), _tensor(out, bf16, total * H * V, at, "out"),
+                                  _stream_beside(stream, at))
+    if rc != SPEC_OK:
+        raise SpecError("spec_expand_latent", rc)
+
+
+def spec_compact_latent(pool, block_table, ctx_len, q_offsets, parent, stop_node, new_len=None, stream=None) -> None:
+    """spec_compact_kv over a cache of latents [num_pages, 16, width] bf16 (modified in place); the rest int32 device tensors.  parent, if given, has an
+    entry for every token up to the last of q_offsets, whose value only the device knows."""
+    (i32, _, bf16), at = _tensor_types(), pool.get_device()
+    pages, page, wide = pool.shape
+    B, width = ctx_len.shape[0], block_table.shape[1]
+    rc = lib().spec_compact_latent(B, wide, page, width, pages, _tensor(pool, bf16, 0, at, "pool"),
+                                   *_places(B, width, 0, at, i32, block_table, ctx_len, q_offsets, parent),
+                                   _tensor(stop_node, i32, B, at, "stop_node"), _tensor(new_len, i32, B, at, "new_len"), _stream_beside(stream, at))
+    if rc != SPEC_OK:
+        raise SpecError("spec_compact_latent", rc)

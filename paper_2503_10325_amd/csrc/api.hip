@@ -24,6 +24,9 @@ static void* noalloc_scratch_ptr() {
   return p;
 }
 
+template <typename... Ptr>
+static bool misaligned(Ptr... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 15u) != 0; }
+
 extern "C" {
 
 const char* spec_strerror(int32_t status) {
@@ -509,6 +512,134 @@ int32_t spec_compact_kv_quant(int32_t B, int32_t num_kv_heads, int32_t head_dim,
   a.k_scale = k_scale; a.v_scale = v_scale; a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets;
   a.parent = parent; a.stop_node = stop_node; a.new_len = new_len;
   launch_compact_kv_quant(a, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+static int check_latent_desc(const spec_latent_desc* d) {
+  if (!d) return SPEC_ERR_NULL;
+  if (d->batch < 0 || d->num_heads <= 0 || d->total_q < 0 || d->max_q_per_req < 0 || d->max_pages_per_req < 0 || d->num_pages < 0)
+    return SPEC_ERR_SHAPE;
+  if (!(d->rotary_scale >= 0.f) || !(d->norm_eps >= 0.f) || !(d->scale >= 0.f)) return SPEC_ERR_SHAPE;
+  if ((d->latent_dim != 256 && d->latent_dim != 512) || (d->rope_dim != 32 && d->rope_dim != 64) || (d->nope_dim != 64 && d->nope_dim != 128) ||
+      (d->value_dim != 64 && d->value_dim != 128) || d->page_size != 16)
+    return SPEC_ERR_UNSUPPORTED;
+  if (d->interleaved != 0 && d->interleaved != 1) return SPEC_ERR_UNSUPPORTED;
+  if (d->out_dtype != SPEC_BF16 && d->out_dtype != SPEC_F32) return SPEC_ERR_UNSUPPORTED;
+  if (d->num_heads > 1024 || d->batch > 65535) return SPEC_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->total_q) / 16 + 2 * static_cast<int64_t>(d->batch) > (1 << 23)) return SPEC_ERR_UNSUPPORTED;
+  return SPEC_OK;
+}
+
+static LatentArgs latent_args_from(const spec_latent_desc* d) {
+  LatentArgs a{};
+  a.B = d->batch; a.H = d->num_heads; a.C = d->latent_dim; a.R = d->rope_dim; a.nope = d->nope_dim; a.value = d->value_dim;
+  a.total_q = d->total_q; a.max_q = d->max_q_per_req; a.max_pages = d->max_pages_per_req; a.num_pages = d->num_pages;
+  a.interleaved = d->interleaved; a.out_dtype = d->out_dtype; a.eps = d->norm_eps;
+  a.rotary_scale = d->rotary_scale == 0.f ? 1.f : d->rotary_scale;
+  a.scale = d->scale == 0.f ? 1.0f / sqrtf(static_cast<float>(d->nope_dim + d->rope_dim)) : d->scale;
+  return a;
+}
+
+int32_t spec_append_latent(const spec_latent_desc* desc, const void* latent, int64_t latent_stride, const void* key, int64_t key_stride,
+                           const void* norm_weight, const float* inv_freq, const int32_t* positions, void* pool, const int32_t* block_table,
+                           const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent, void* stream) {
+  const int rc = check_latent_desc(desc);
+  if (rc != SPEC_OK) return rc;
+  if (parent && desc->max_q_per_req > 128) return SPEC_ERR_UNSUPPORTED;
+  if (desc->batch == 0 || desc->total_q == 0) return SPEC_OK;
+  if (!latent || !key || !inv_freq || !pool || !block_table || !ctx_len || !q_offsets) return SPEC_ERR_NULL;
+  if (desc->max_pages_per_req == 0 || desc->num_pages == 0 || desc->max_q_per_req == 0) return SPEC_ERR_SHAPE;
+  if (latent_stride < desc->latent_dim || latent_stride % 8 || key_stride < desc->rope_dim || key_stride % 8) return SPEC_ERR_SHAPE;
+  if (misaligned(latent, key, norm_weight, pool)) return SPEC_ERR_SHAPE;
+  LatentArgs a = latent_args_from(desc);
+  a.inv_freq = inv_freq; a.positions = positions; a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets; a.parent = parent;
+  launch_append_latent(a, latent, latent_stride, key, key_stride, norm_weight, pool, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+int32_t spec_absorb_latent(const spec_latent_desc* desc, const void* q, int64_t q_stride, const void* w_key, int64_t w_stride, const float* inv_freq,
+                           const int32_t* positions, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent, void* q_out, void* stream) {
+  const int rc = check_latent_desc(desc);
+  if (rc != SPEC_OK) return rc;
+  if (parent && desc->max_q_per_req > 128) return SPEC_ERR_UNSUPPORTED;
+  if (desc->batch == 0 || desc->total_q == 0) return SPEC_OK;
+  if (!q || !w_key || !inv_freq || !ctx_len || !q_offsets || !q_out) return SPEC_ERR_NULL;
+  if (desc->max_q_per_req == 0) return SPEC_ERR_SHAPE;
+  if (q_stride < static_cast<int64_t>(desc->num_heads) * (desc->nope_dim + desc->rope_dim) || q_stride % 8) return SPEC_ERR_SHAPE;
+  if (w_stride < static_cast<int64_t>(desc->nope_dim) * desc->latent_dim || w_stride % 8) return SPEC_ERR_SHAPE;
+  if (misaligned(q, w_key, q_out)) return SPEC_ERR_SHAPE;
+  LatentArgs a = latent_args_from(desc);
+  a.inv_freq = inv_freq; a.positions = positions; a.ctx_len = ctx_len; a.q_offsets = q_offsets; a.parent = parent;
+  launch_absorb_latent(a, q, q_stride, w_key, w_stride, q_out, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+static int check_latent_attn(const spec_latent_desc* d) {
+  const int rc = check_latent_desc(d);
+  if (rc != SPEC_OK) return rc;
+  return d->max_q_per_req > 128 ? SPEC_ERR_UNSUPPORTED : SPEC_OK;
+}
+
+size_t spec_verify_attn_latent_workspace_size(const spec_latent_desc* desc) {
+  if (check_latent_attn(desc) != SPEC_OK) return 0;
+  const LatentArgs a = latent_args_from(desc);
+  return latent_attn_workspace_bytes(a, make_latent_attn_plan(a));
+}
+
+int32_t spec_verify_attn_latent(const spec_latent_desc* desc, const void* q, const void* pool, const int32_t* block_table, const int32_t* ctx_len,
+                                const int32_t* q_offsets, const int32_t* parent, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  const int rc = check_latent_attn(desc);
+  if (rc != SPEC_OK) return rc;
+  if (desc->batch == 0 || desc->total_q == 0) return SPEC_OK;
+  if (!q || !pool || !block_table || !ctx_len || !q_offsets || !out) return SPEC_ERR_NULL;
+  if (desc->max_pages_per_req == 0 || desc->num_pages == 0 || desc->max_q_per_req == 0) return SPEC_ERR_SHAPE;
+  if (misaligned(q, pool, out, workspace)) return SPEC_ERR_SHAPE;
+  LatentArgs a = latent_args_from(desc);
+  const LatentAttnPlan plan = make_latent_attn_plan(a);
+  if (!workspace || workspace_bytes < latent_attn_workspace_bytes(a, plan)) return SPEC_ERR_WORKSPACE;
+  a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets; a.parent = parent;
+  if (launch_attn_latent(a, q, pool, out, lse, workspace, plan, static_cast<hipStream_t>(stream)) != 0) return SPEC_ERR_LAUNCH;
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+int32_t spec_describe_attn_latent_plan(const spec_latent_desc* desc, char* buf, size_t buf_bytes) {
+  const int rc = check_latent_attn(desc);
+  if (rc != SPEC_OK) return rc;
+  if (!buf || buf_bytes == 0) return SPEC_ERR_NULL;
+  const LatentArgs a = latent_args_from(desc);
+  const LatentAttnPlan p = make_latent_attn_plan(a);
+  snprintf(buf, buf_bytes, "attn_latent_kernel<%d, %d, %d>: %d query rows at a time, at most %d group(s) of them per request, %d range(s) of the tokens", a.C, a.R,
+           a.out_dtype == SPEC_F32 ? 3 : 1, p.rows, p.groups, p.ranges);
+  return SPEC_OK;
+}
+
+int32_t spec_expand_latent(const spec_latent_desc* desc, const void* x, const void* w_value, int64_t w_stride, const int32_t* q_offsets, void* out,
+                           void* stream) {
+  const int rc = check_latent_desc(desc);
+  if (rc != SPEC_OK) return rc;
+  if (desc->batch == 0 || desc->total_q == 0) return SPEC_OK;
+  if (!x || !w_value || !q_offsets || !out) return SPEC_ERR_NULL;
+  if (w_stride < static_cast<int64_t>(desc->value_dim) * desc->latent_dim || w_stride % 8) return SPEC_ERR_SHAPE;
+  if (misaligned(x, w_value, out)) return SPEC_ERR_SHAPE;
+  LatentArgs a = latent_args_from(desc);
+  a.q_offsets = q_offsets;
+  if (launch_expand_latent(a, x, w_value, w_stride, out, static_cast<hipStream_t>(stream)) != 0) return SPEC_ERR_LAUNCH;
+  return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
+}
+
+int32_t spec_compact_latent(int32_t B, int32_t width, int32_t page_size, int32_t max_pages_per_req, int32_t num_pages, void* pool,
+                            const int32_t* block_table, const int32_t* ctx_len, const int32_t* q_offsets, const int32_t* parent,
+                            const int32_t* stop_node, int32_t* new_len, void* stream) {
+  if (B < 0 || width <= 0 || width % 8 != 0 || max_pages_per_req < 0 || num_pages < 0) return SPEC_ERR_SHAPE;
+  if (width > 576 || page_size != 16 || B > 65535) return SPEC_ERR_UNSUPPORTED;
+  if (B == 0) return SPEC_OK;
+  if (!pool || !block_table || !ctx_len || !q_offsets || !stop_node) return SPEC_ERR_NULL;
+  if (misaligned(pool)) return SPEC_ERR_SHAPE;
+  LatentCompactArgs a{};
+  a.B = B; a.width = width; a.max_pages = max_pages_per_req; a.num_pages = num_pages; a.pool = static_cast<uint16_t*>(pool);
+  a.block_table = block_table; a.ctx_len = ctx_len; a.q_offsets = q_offsets; a.parent = parent; a.stop_node = stop_node; a.new_len = new_len;
+  launch_compact_latent(a, static_cast<hipStream_t>(stream));
   return hipGetLastError() == hipSuccess ? SPEC_OK : SPEC_ERR_LAUNCH;
 }
 

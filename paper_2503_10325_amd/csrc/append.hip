@@ -22,13 +22,13 @@
 #include "common.h"
 #include "kernels.h"
 #include "quant.h"
+#include "rotary.h"
 
 namespace specv {
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = kRotaryThreads;
 constexpr int kAppendWaves = kAppendThreads / kWave;
-constexpr int kAppendMaxTree = 128;
-constexpr int kAngleStride = 64 + 2;           // pairs: 16 tokens' rows start 4 banks apart
+static_assert(kRunTokens == kQuantPage, "the tokens of a page are a run");
 
 struct AppendParams {
   const uint16_t* q;
@@ -55,66 +55,6 @@ struct AppendParams {
 struct PageRun {
   int b, row0, slot0, count, page, ctx, first, n;
 };
-
-// sine and cosine of `turns` * 2 pi
-__device__ __forceinline__ float2 cos_sin_turns(double turns) {
-  const double part = turns - rint(turns);                    // [-1/2, 1/2]
-  const double quarter = rint(4.0 * part);
-  const float x = static_cast<float>((part - 0.25 * quarter) * 6.283185307179586);
-  const float z = x * x;
-  const float s = x * (1.f + z * (-1.f / 6 + z * (1.f / 120 + z * (-1.f / 5040 + z * (1.f / 362880)))));
-  const float c = 1.f + z * (-0.5f + z * (1.f / 24 + z * (-1.f / 720 + z * (1.f / 40320 + z * (-1.f / 3628800)))));
-  const int k = static_cast<int>(quarter) & 3;
-  const float cc = k & 1 ? s : c, ss = k & 1 ? c : s;
-  return make_float2(k == 1 || k == 2 ? -cc : cc, k >= 2 ? -ss : ss);
-}
-
-// Which request page slot u belongs to: the last b with q_offsets[b] / 16 + 2 b <= u, by 64 comparisons a step.
-__device__ __forceinline__ int request_of_slot(const int32_t* q_offsets, int B, int u, int lane) {
-  int lo = 0, count = B;
-  while (count > 1) {
-    const int step = (count + kWave - 1) / kWave;
-    const int b = lo + lane * step;
-    const bool le = lane * step < count && (q_offsets[b] >> 4) + 2 * b <= u;
-    const int k = max(__popcll(__ballot(le)) - 1, 0);
-    lo += k * step;
-    count = min(step, count - k * step);
-  }
-  return lo;
-}
-
-// 8 dimensions (unit `u` of a head) rotated.  own, other: the unit and the one that holds its partners (halves); cs: the token's
-// angles.
-__device__ __forceinline__ void rotate_halves(const float (&own)[8], const float (&other)[8], const float2* cs, int u, int half_units,
-                                              float (&x)[8]) {
-  const bool first = u < half_units;
-  const float2* c = cs + 8 * (first ? u : u - half_units);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float2 w = c[j];
-    x[j] = own[j] * w.x + other[j] * (first ? -w.y : w.y);
-  }
-}
-__device__ __forceinline__ void rotate_neighbours(const float (&own)[8], const float2* cs, int u, float (&x)[8]) {
-  const float2* c = cs + 4 * u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float2 w = c[j];
-    x[2 * j] = own[2 * j] * w.x - own[2 * j + 1] * w.y;
-    x[2 * j + 1] = own[2 * j + 1] * w.x + own[2 * j] * w.y;
-  }
-}
-
-typedef __bf16 abf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ raw4 round_bf16(const float (&x)[8]) {
-  raw4 w;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const abf16x2 p = {static_cast<__bf16>(x[2 * j]), static_cast<__bf16>(x[2 * j + 1])};
-    w[j] = __builtin_bit_cast(uint32_t, p);
-  }
-  return w;
-}
 
 // ---- 8-bit cache: the keys of one (page, head) --------------------------------------------------------------
 // Lane: slot t = lane % 16, chunks of 16 dimensions lane / 16 and, for D = 128, 4 + lane / 16.
@@ -276,28 +216,13 @@ __device__ __forceinline__ void store_values(const AppendParams& P, const PageRu
 template <int D, bool QUANT>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P) {
   constexpr int kPairUnits = D / 16;                            // items of a head: two units of 8 dimensions each
-  __shared__ __align__(16) float2 sh_cs[kQuantPage][kAngleStride];
-  __shared__ int sh_parent[kAppendMaxTree];
-  __shared__ int sh_pos[kQuantPage];
-  __shared__ float sh_freq[64];
+  __shared__ RunAngles angles;
+  auto& sh_cs = angles.cs;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const RunRequest Q = find_request(P, blockIdx.x, lane);
   PageRun R;
-  if (P.B <= kWave) {                                           // one load for which request it is and what there is to know of it
-    const int b = min(lane, P.B - 1), off = P.q_offsets[b], next = P.q_offsets[b + 1], ctx = P.ctx_len[b];
-    const bool le = lane < P.B && (off >> 4) + 2 * lane <= static_cast<int>(blockIdx.x);
-    R.b = max(__popcll(__builtin_amdgcn_ballot_w64(le)) - 1, 0);
-    R.first = __builtin_amdgcn_readlane(off, R.b);
-    R.n = __builtin_amdgcn_readlane(next, R.b);
-    R.ctx = __builtin_amdgcn_readlane(ctx, R.b);
-  } else {
-    R.b = __builtin_amdgcn_readfirstlane(request_of_slot(P.q_offsets, P.B, blockIdx.x, lane));
-    R.first = P.q_offsets[R.b];
-    R.n = P.q_offsets[R.b + 1];
-    R.ctx = P.ctx_len[R.b];
-  }
-  R.n = min(R.n, P.total_q) - R.first;
-  if (P.parent) R.n = min(R.n, kAppendMaxTree);
+  R.b = Q.b; R.first = Q.first; R.n = Q.n; R.ctx = Q.ctx;
   if (R.ctx < 0 || R.first < 0) return;
   const int64_t lp64 = static_cast<int64_t>(R.ctx >> 4) + (static_cast<int>(blockIdx.x) - (R.first >> 4) - 2 * R.b);
   const int64_t from = max(static_cast<int64_t>(R.ctx), 16 * lp64), to = min(static_cast<int64_t>(R.ctx) + R.n, 16 * lp64 + 16);
@@ -307,39 +232,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams P) 
   R.row0 = R.first + static_cast<int>(from - R.ctx);
   R.page = lp64 < P.max_pages ? P.block_table[static_cast<int64_t>(R.b) * P.max_pages + lp64] : -1;
 
-  // ---- angles of the page's tokens: what they take is asked for at once ----
-  const int half = P.rotary >> 1;
-  const bool tree = half > 0 && P.positions == nullptr && P.parent;
-  const int up = tree && tid < R.n ? P.parent[R.first + tid] : -1;
-  const int given = half > 0 && P.positions && tid < R.count ? P.positions[R.row0 + tid] : 0;
-  const float freq = tid < half ? P.inv_freq[tid] : 0.f;
-  if (half > 0) {
-    if (tid < half) sh_freq[tid] = freq;
-    const int i = R.row0 - R.first + tid;
-    if (tree) {
-      if (tid < R.n) sh_parent[tid] = up;
-      lds_sync();
-      if (tid < R.count) {
-        int depth = 0;
-        for (int a = i; depth < kAppendMaxTree; ++depth) {
-          const int p = sh_parent[a];
-          if (p < 0 || p >= a) break;                           // (a malformed entry is a root)
-          a = p;
-        }
-        sh_pos[tid] = R.ctx + depth;
-      }
-    } else if (tid < R.count) {
-      sh_pos[tid] = P.positions ? given : R.ctx + i;
-    }
-    lds_sync();
-    for (int at = tid; at < R.count * half; at += kAppendThreads) {
-      const int t = at / half, p = at - t * half;
-      const double turns = static_cast<double>(sh_pos[t]) * static_cast<double>(sh_freq[p]) * 0.15915494309189535;
-      const float2 w = cos_sin_turns(turns);
-      sh_cs[t][p] = make_float2(w.x * P.rotary_scale, w.y * P.rotary_scale);
-    }
-    lds_sync();
-  }
+  run_angles(P, angles, R.first, R.n, R.ctx, R.row0, R.count);
 
   if (R.page < 0 || R.page >= P.num_pages) R.page = -1;
 

@@ -231,4 +231,76 @@ void launch_compact_kv_quant(const QuantCompactArgs& a, hipStream_t stream) {
                      a.k_scale, a.v_scale, a.block_table, a.ctx_len, a.q_offsets, a.parent, a.stop_node, a.new_len);
 }
 
+// ----------------------------------------------------------------------------------
+// The same for the cache of latents: one row of `width` elements per token.  One workgroup per request; a row of up to 576 elements is 72 items of 16
+// bytes, and every source row is read before any is written.
+// ----------------------------------------------------------------------------------
+constexpr int kLatentMost = 576 / 8;                                          // items of a row, at most
+
+__global__ __launch_bounds__(1024) void compact_latent_kernel(
+    int width, int max_pages, int num_pages, uint16_t* __restrict__ pool, const int32_t* __restrict__ block_table,
+    const int32_t* __restrict__ ctx_len, const int32_t* __restrict__ q_offsets, const int32_t* __restrict__ parent,
+    const int32_t* __restrict__ stop_node, int32_t* __restrict__ new_len) {
+  constexpr int kPerThread = (kCompactMaxNodes * kLatentMost + 1023) / 1024;
+  constexpr int kPage = 16;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  __shared__ int sh_parent[kCompactMaxNodes], sh_path[kCompactMaxNodes];      // path: leaf -> root
+  __shared__ int sh_depth;
+  __shared__ int64_t sh_from[kCompactMaxNodes], sh_to[kCompactMaxNodes];      // rows of the pool; -1: none
+  const int o = q_offsets[b], behind = q_offsets[b + 1];
+  const int tokens = o < 0 ? 0 : max(behind, o) - o;
+  const int ctx = ctx_len[b], stop = stop_node[b];
+  if (ctx < 0) {                                                             // no request: nothing of it moves, its length stays
+    if (tid == 0 && new_len) new_len[b] = ctx;
+    return;
+  }
+  if (parent == nullptr) {                                                   // linear drafts, however many, lie where they belong
+    if (tid == 0 && new_len)
+      new_len[b] = static_cast<int>(min(static_cast<unsigned>(ctx) + (stop >= 0 && stop < tokens ? stop + 1 : 0), 0x7fffffffu));
+    return;
+  }
+  const int n = min(tokens, kCompactMaxNodes);
+  if (tid < n) sh_parent[tid] = parent[o + tid];
+  __syncthreads();
+  if (tid == 0) {
+    int depth = 0;
+    for (int a = stop; a >= 0 && a < n && depth < kCompactMaxNodes;) {
+      sh_path[depth++] = a;
+      const int p = sh_parent[a];
+      a = p < a ? p : -1;                                                    // a malformed parent entry ends the path
+    }
+    sh_depth = depth;
+    if (new_len) new_len[b] = static_cast<int>(min(static_cast<unsigned>(ctx) + depth, 0x7fffffffu));
+  }
+  __syncthreads();
+  const int depth = sh_depth;
+  if (depth == 0) return;
+  if (tid < 2 * depth) {
+    const int d = tid >> 1;
+    const int64_t pos = static_cast<int64_t>(ctx) + (tid & 1 ? d : sh_path[depth - 1 - d]), lp = pos / kPage;
+    const int id = lp < max_pages ? block_table[static_cast<int64_t>(b) * max_pages + lp] : -1;
+    (tid & 1 ? sh_to : sh_from)[d] = id >= 0 && id < num_pages ? static_cast<int64_t>(id) * kPage + pos % kPage : -1;
+  }
+  __syncthreads();
+  const int row = width / 8, items = depth * row;
+  raw4 held[kPerThread];
+#pragma unroll
+  for (int r = 0; r < kPerThread; ++r) {
+    const int it = r * 1024 + tid, d = it / row;
+    if (it < items && sh_from[d] >= 0) held[r] = reinterpret_cast<const raw4*>(pool + sh_from[d] * width)[it - d * row];
+  }
+  __syncthreads();                                                           // everything that is read has been
+#pragma unroll
+  for (int r = 0; r < kPerThread; ++r) {
+    const int it = r * 1024 + tid, d = it / row;
+    if (it < items && sh_from[d] >= 0 && sh_to[d] >= 0) reinterpret_cast<raw4*>(pool + sh_to[d] * width)[it - d * row] = held[r];
+  }
+}
+
+void launch_compact_latent(const LatentCompactArgs& a, hipStream_t stream) {
+  if (a.B <= 0) return;
+  hipLaunchKernelGGL(compact_latent_kernel, dim3(a.B), dim3(1024), 0, stream, a.width, a.max_pages, a.num_pages, a.pool, a.block_table, a.ctx_len, a.q_offsets,
+                     a.parent, a.stop_node, a.new_len);
+}
+
 }  // namespace specv

@@ -148,6 +148,17 @@ struct QuantCompactArgs {
   int32_t* new_len;
 };
 void launch_compact_kv_quant(const QuantCompactArgs& a, hipStream_t stream);
+struct LatentCompactArgs {
+  int B, width, max_pages, num_pages;
+  uint16_t* pool;
+  const int32_t* block_table;
+  const int32_t* ctx_len;
+  const int32_t* q_offsets;
+  const int32_t* parent;
+  const int32_t* stop_node;
+  int32_t* new_len;
+};
+void launch_compact_latent(const LatentCompactArgs& a, hipStream_t stream);
 
 // ---- append.hip -------------------------------------------------------------------
 struct AppendArgs {
@@ -244,6 +255,32 @@ QuantAttnPlan make_quant_attn_plan(const AttnArgs& a);
 size_t quant_attn_workspace_bytes(const AttnArgs& a, const QuantAttnPlan& plan);
 int launch_attn_quant(const AttnArgs& a, const float* k_scale, const float* v_scale, int num_pages, const QuantAttnPlan& plan,
                       hipStream_t stream);      // 0 or a negative spec_status
+
+// ---- latent.hip, attn_latent.hip --------------------------------------------------
+struct LatentArgs {
+  int B, H, C, R, nope, value, total_q, max_q, max_pages, num_pages, interleaved, out_dtype;
+  float rotary_scale, eps, scale;
+  const float* inv_freq;
+  const int32_t* positions;
+  const int32_t* block_table;
+  const int32_t* ctx_len;
+  const int32_t* q_offsets;
+  const int32_t* parent;
+};
+void launch_append_latent(const LatentArgs& a, const void* latent, int64_t latent_stride, const void* key, int64_t key_stride, const void* norm, void* pool,
+                          hipStream_t stream);
+void launch_absorb_latent(const LatentArgs& a, const void* q, int64_t q_stride, const void* w, int64_t w_stride, void* out, hipStream_t stream);
+int launch_expand_latent(const LatentArgs& a, const void* x, const void* w, int64_t w_stride, void* out, hipStream_t stream);
+// A pure function of the descriptor, as AttnPlan.
+struct LatentAttnPlan {
+  int rows;           // query rows a workgroup takes at a time: 16, 32, 64 or 128
+  int groups;         // ... groups of so many that cover a request's rows
+  int ranges;         // workgroups: ranges of the batch's tokens and groups of equal cost
+};
+LatentAttnPlan make_latent_attn_plan(const LatentArgs& a);
+size_t latent_attn_workspace_bytes(const LatentArgs& a, const LatentAttnPlan& plan);
+int launch_attn_latent(const LatentArgs& a, const void* q, const void* pool, void* out, float* lse, void* workspace, const LatentAttnPlan& plan,
+                       hipStream_t stream);     // 0 or a negative spec_status
 
 // Vector (16-byte) accesses need 16-byte aligned base pointers; the launchers pick the scalar
 // variants of their kernels when a caller's pointer is not.
