@@ -1,17 +1,20 @@
 // Verify-attention over the cache of latents: the draft queries of each request, of all heads, attend over its committed context and their draft ancestors.
 // A cache row is a latent of C elements, key and value at once, and R more that only keys have; all heads read the same rows.
 //
-//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16: 16 tokens x 16 query rows a block.  A lane ends up with 4 consecutive tokens of one row.
-//   O^T = V^T P^T the weights of two blocks of 16 tokens are an operand as they are (token 4 g + i of block s is element 4 s + i of lane group g);
-//                 V^T, the same bytes as K, is read from LDS by columns.
-// Query rows of a request (node x head, consecutive in memory) are taken in groups of up to M, the tokens in tiles of T, which four waves bring to LDS
-// and share.  The scores are split over the waves as WR groups of rows x WK groups of tokens, the weights go through LDS, and of the second
-// product every wave takes C / 4 columns for all rows: a tile is read WR times from LDS for the scores and once for the results.
+//   S^T = K Q^T     matrix instructions leave a lane with consecutive tokens of one query row, 4 (16x16x32) or 8 (32x32x16: 4 and 4) at a time
+//   O^T = V^T P^T   so its weights, in bf16, are operands as they are; V^T, the same bytes as K, is read from LDS by columns
+// fp32 results take the weights in three terms of bf16, which hold all of fp32.
+// Query rows of a request (node x head, consecutive in memory) are taken in groups of 16, 32 or 128, the tokens in tiles, which four waves bring to LDS and
+// share: LatentNarrow and LatentWide below.  Of the second product every wave takes C / 4 columns for all rows; the weights go through LDS.
+//
+// Bound: up to 32 rows by memory (64 tokens' rows in one, 2048 x 64 of 16 heads: 39 us, 5.6 TB/s, and 6 for the merge), with 128 by the matrix instructions
+// (batch 64, 8192 tokens, 4 x 128 rows: 1160 TFLOP/s of the 1520 that a large matrix product reaches).
 //
 // Work: the tiles of all requests and groups lie end to end and are cut into ranges of equal cost, one per workgroup, whatever the lengths; every
 // workgroup works out from ctx_len and q_offsets which pieces its range holds.  Groups that are cut leave partial results, which a second launch
 // merges in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -24,9 +27,7 @@ constexpr int kLaPage = 16;
 constexpr int kLaMaxNodes = 128;
 constexpr int kLaRanges = 256;                 // workgroups: one per compute unit
 constexpr float kLaNoScore = -3.0e38f;         // the reference before the first position: finite, so that -infinity stays ahead of nothing
-constexpr float kLaSlack = 8.f;                // a row's reference follows its maximum when that is 2^8 ahead (bf16 weights have the range of fp32)
-constexpr int kLaHead = 3;                     // what the start and the end of a group cost, in tiles
-constexpr int kLaLeast = 3;                    // tiles of a range at least
+constexpr float kLaSlack = 40.f;               // a row's reference follows its maximum when that is 2^40 ahead: weights in bf16, and their sums, have the range of fp32
 
 struct LatentAttnParams {
   const uint16_t* q;
@@ -74,39 +75,24 @@ template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
 // ---- the cut of the batch: costs are whole numbers in fp64 (exact up to 2^53) --------------------------------------
-struct LaRequests {                            // 64 at a time, lane i: request 64 k + i
-  int ctx, first, n;
-  double upto, sum;                            // cost up to the end of this lane's request, of these 64
-};
 template <int T>
 __device__ __forceinline__ int tiles_of(const LatentAttnParams& P, int ctx, int n) {
   constexpr int kPages = T / kLaPage;
   return n > 0 ? min(static_cast<int>((static_cast<unsigned>(ctx) + n + T - 1) / T), static_cast<int>((static_cast<unsigned>(P.max_pages) + kPages - 1) / kPages)) : 0;
 }
-template <int M, int T>
-__device__ __forceinline__ LaRequests load_requests(const LatentAttnParams& P, int k, int lane) {
-  LaRequests r;
-  const int b = 64 * k + lane;
-  r.ctx = r.first = r.n = 0;
-  if (b < P.B) {
-    r.ctx = min(max(P.ctx_len[b], 0), 0x7fffff00);              // (the end of the drafts still fits)
-    r.first = P.q_offsets[b];
-    r.n = r.first < 0 ? 0 : max(min(min(P.q_offsets[b + 1], P.total_q) - r.first, P.max_q), 0);
-  }
-  const int groups = (r.n * P.H + M - 1) / M;
-  r.upto = wave_scan(static_cast<double>(groups) * (kLaHead + tiles_of<T>(P, r.ctx, r.n)));
-  r.sum = lane_f64(r.upto, 63);
-  return r;
-}
+// A number that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ double uniform(double x) { return lane_f64(x, 0); }
+// The groups of all requests end to end, each its kHead (what its start and end cost, in tiles) and its tiles, in `used` ranges of equal length, whole numbers apart,
+// at least kLeast long.  A border that would leave a piece of a group with fewer than kSnap tiles goes to the group's end.
 struct LaCut {
   int used;
   double each, total;
 };
-__device__ __forceinline__ LaCut cut_ranges(int most, double total) {
+__device__ __forceinline__ LaCut cut_ranges(int most, int least, double total) {
   LaCut c;
   c.total = total;
-  c.used = __builtin_amdgcn_readfirstlane(static_cast<int>(fmin(fmax(total / kLaLeast, 1.0), static_cast<double>(most))));
-  c.each = total / c.used;
+  c.used = __builtin_amdgcn_readfirstlane(static_cast<int>(fmin(fmax(total / least, 1.0), static_cast<double>(most))));
+  c.each = uniform(total / c.used);
   return c;
 }
 __device__ __forceinline__ double range_start(const LaCut& c, int s) { return s >= c.used ? c.total : floor(s * c.each); }
@@ -115,12 +101,22 @@ __device__ __forceinline__ int range_of(const LaCut& c, double at) {
   while (s + 1 < c.used && range_start(c, s + 1) <= at) ++s;
   return s;
 }
+// Where a border at `at` goes by the group [start, end) that it lies in (another: where it is).
+template <typename K>
+__device__ __forceinline__ double border(double at, double start, double end) {
+  if (at <= start || at >= end) return at;
+  if (at < start + K::kHead + K::kSnap) return start;
+  return at > end - K::kSnap ? end : at;
+}
 
-template <int C_, int R_, int NB_, int WR_, int KB_, int TERMS_>
-struct LatentConfig {
-  static constexpr int C = C_, R = R_, NB = NB_, WR = WR_, WK = kLaWaves / WR_, KB = KB_, TERMS = TERMS_;
+// Up to 16 NB rows: every wave takes a quarter of a tile's tokens for the scores.
+template <int C_, int R_, int NB_, int TERMS_>
+struct LatentNarrow {
+  static constexpr bool kWide = false;
+  static constexpr int C = C_, R = R_, NB = NB_, TERMS = TERMS_;
   static constexpr int W = C + R;
-  static constexpr int M = 16 * NB * WR, T = 16 * KB * WK;
+  static constexpr int kHead = 3, kSnap = 1, kLeast = 2;      // see Cut
+  static constexpr int M = 16 * NB, T = 64, WK = kLaWaves;
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;            // 16-byte units of a row in LDS
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
   static constexpr int kPages = T / kLaPage;
@@ -128,23 +124,72 @@ struct LatentConfig {
   static constexpr int kSteps = W / 32;
   static constexpr int kLoads = kTile / kLaWaves / 1024;        // of a wave for a tile
   static constexpr int kOffsets = 8 * kRow / 1024;              // loads that bring 8 rows
-  static constexpr int kWeights = T / 32 * RB * 1024;           // bytes of a term of a tile's weights
-  static constexpr int kSmall = TERMS * kWeights + kLaMaxNodes * 20 + 64 + 4 * M * (2 * WK + 2);
+  static constexpr int kWeights = TERMS * (T / 32) * RB * 1024, kBuffers = 1;
+  static constexpr int kSmall = kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 + 4 + 80;
   static constexpr int kStages = std::min(4, (160 * 1024 - kSmall) / kTile);
   static_assert(kStages >= 2 && kRow % 256 == 128, "");
+};
+// Up to 128 rows: every wave takes 32 of them for the scores.
+template <int C_, int R_, int TERMS_>
+struct LatentWide {
+  static constexpr bool kWide = true;
+  static constexpr int C = C_, R = R_, TERMS = TERMS_;
+  static constexpr int W = C + R;
+  static constexpr int kHead = 12, kSnap = 4, kLeast = 4;      // see Cut
+  static constexpr int M = 128, T = 32, WK = 1;
+  static constexpr int kUnits = (W / 8 + 7) / 8 * 8;
+  static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
+  static constexpr int kPages = T / kLaPage;
+  static constexpr int RB = M / 32, CB = C / 4 / 32;            // 32-row blocks; 32-column blocks of a wave
+  static constexpr int kSteps = W / 16;
+  static constexpr int kLoads = kTile / kLaWaves / 1024;
+  static constexpr int kOffsets = 8 * kRow / 1024;
+  static constexpr int kInTile = T * 128 / 1024;                // of a tile's 8 TERMS operands of 1 KB: those that lie in the tile itself, where
+  static constexpr int kWeights = (TERMS * 2 * RB - kInTile) * 1024, kBuffers = 2;      // the shared part of the keys was; the others' bytes
+  static constexpr int kSmall = kBuffers * kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 +
+                                2 * kOffsets * kWave * 4 + 80;
+  static constexpr int kStages = std::min(4, (160 * 1024 - kSmall) / kTile);
+  static_assert(kStages >= 3 && kRow % 256 == 128 && kLoads == kOffsets, "");
 };
 
 template <typename K>
 struct LatentShared {
   __align__(1024) unsigned char ring[K::kStages][K::kTile];
-  __align__(16) unsigned char p[K::TERMS][K::kWeights];
+  __align__(16) unsigned char p[K::kBuffers][K::kWeights];
   unsigned long long anc[kLaMaxNodes][2];
-  int parent[kLaMaxNodes];
   int node[K::M];
-  float top[K::WK][K::M], sum[K::WK][K::M], by[K::M];
-  unsigned ahead[kLaWaves];
+  union {
+    int parent[kLaMaxNodes];                                    // (until the ancestors are known)
+    float top[K::WK][K::M];
+  };
+  float sum[K::WK][K::M], by[2][K::M];
+  __align__(16) unsigned ahead[2][kLaWaves];
+  double each, total;                                           // of the cut
+  double upto[kWave];                                           // 64 requests: the cost up to the end of each, ...
+  int ctx[kWave], first[kWave], n[kWave];
+  unsigned off[K::kWide ? 2 : 1][K::kWide ? K::kOffsets : 1][kWave];      // where the bytes of a tile's load come from, in either half of a page
 };
 
+// Requests 64 k .. + 63 into LDS, and what they cost together; by all threads.
+template <typename K>
+__device__ __forceinline__ double load_requests(const LatentAttnParams& P, LatentShared<K>& S, int k) {
+  const int tid = threadIdx.x + opaque_zero(), lane = tid & 63, b = 64 * k + lane;      // (nothing of this is kept across a piece)
+  int ctx = 0, first = 0, n = 0;
+  if (b < P.B) {
+    ctx = min(max(P.ctx_len[b], 0), 0x7fffff00);                // (the end of the drafts still fits)
+    first = P.q_offsets[b];
+    n = first < 0 ? 0 : max(min(min(P.q_offsets[b + 1], P.total_q) - first, P.max_q), 0);
+  }
+  const int groups = (n * P.H + K::M - 1) / K::M;
+  const double upto = wave_scan(static_cast<double>(groups) * (K::kHead + tiles_of<K::T>(P, ctx, n)));
+  lds_sync();                                                   // (what was there has been read)
+  if (tid < kWave) {
+    S.upto[lane] = upto;
+    S.ctx[lane] = ctx; S.first[lane] = first; S.n[lane] = n;
+  }
+  lds_sync();
+  return lane_f64(upto, 63);
+}
 struct LatentPiece {
   int b, first, n, ctx, t0, t1, rows;
   int row_base;
@@ -152,27 +197,599 @@ struct LatentPiece {
   int64_t part;               // first row of its partial result
 };
 
+// Row r of a tile, 16-byte unit u lies at u ^ fold(r): 16 rows' units of one place take 16 places of 16 bytes modulo the banks' 256 (rows are 128 bytes apart
+// modulo 256, so r % 2 is told apart by itself).
+__device__ __forceinline__ int fold(int r) { return 4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1) + ((r >> 3) & 1); }
+// Where the bytes of a load come from, in the first 8 rows of a page; in the other 8 rows at ^ 16.  Units past the row's last repeat one.
+template <typename K>
+__device__ __forceinline__ void tile_offsets(unsigned (&off)[K::kOffsets], int lane) {
+#pragma unroll
+  for (int j = 0; j < K::kOffsets; ++j) {
+    const int u = 64 * j + lane, r = u / K::kUnits, p = u % K::kUnits;
+    int unit = p ^ fold(r);
+    if constexpr (K::kUnits * 8 != K::W) unit = unit < K::W / 8 ? unit : unit & 3 | K::W / 8 - 4;
+    off[j] = r * (K::W * 2) + unit * 16;
+  }
+}
+
+// The rows' nodes, and the nodes' ancestors.
+template <typename K>
+__device__ __forceinline__ void find_lineage(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J, int tid, int parent) {
+  if (tid < kLaMaxNodes) S.parent[tid] = parent;
+  int heads = P.H;
+  asm volatile("" : "+s"(heads));                               // (or its reciprocal is kept across pieces)
+  if (tid < K::M) S.node[tid] = (J.row_base + min(tid, J.rows - 1)) / heads;
+  lds_sync();
+  if (tid < kLaMaxNodes) {
+    unsigned long long w[2] = {0ull, 0ull};
+    if (tid < J.n) {
+      if (P.parent) {
+        int a = tid;
+        for (int k = 0; k < kLaMaxNodes && a >= 0; ++k) {
+          if (a < 64) w[0] |= 1ull << a; else w[1] |= 1ull << (a - 64);
+          const int p = S.parent[a];
+          a = (p >= a || p < 0) ? -1 : p;                       // (a malformed entry is a root)
+        }
+      } else {
+        w[0] = tid < 63 ? (2ull << tid) - 1ull : ~0ull;
+        w[1] = tid < 64 ? 0ull : (tid < 127 ? (2ull << (tid - 64)) - 1ull : ~0ull);
+      }
+    }
+    S.anc[tid][0] = w[0];
+    S.anc[tid][1] = w[1];
+  }
+}
+
+// A weight of zero times what is not finite would be NaN: where rows differ in what they see, such values are taken out of V.  (A row that sees one has met it in
+// its scores.)  By all threads, of a tile that all have read for the scores.
+template <typename K>
+__device__ __forceinline__ void take_out(unsigned tile, int tid) {
+  constexpr int kUnits = K::C / 8;
+  for (int u = tid; u < K::T * kUnits; u += kLaThreads) {
+    const unsigned at = tile + u / kUnits * K::kRow + u % kUnits * 16;
+    raw4 w = read_lds16(at);
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool l = (w[i] & 0x7f80u) == 0x7f80u, h = (w[i] & 0x7f800000u) == 0x7f800000u;
+      any |= l | h;
+      w[i] = (l ? 0u : w[i] & 0xffffu) | (h ? 0u : w[i] & 0xffff0000u);
+    }
+    if (any) *lds_pointer<raw4>(at) = w;
+  }
+}
+
+template <typename K>
+__device__ __forceinline__ void write_results(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J, lf32x4 (&o)[K::CB][K::RB],
+                                              const float (&ref)[K::NB], const float (&sum)[K::NB], int wave, int lane) {
+  constexpr int NB = K::NB, WK = K::WK, RB = K::RB, CB = K::CB;
+  const int tid = threadIdx.x, rn = lane & 15, g = lane >> 4;
+  lds_sync();                                                   // (S.by has been read)
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const float z = groups_sum(sum[nb]);
+    if (lane < 16) {
+      S.sum[wave][16 * nb + lane] = z;
+      if (wave == 0) S.by[0][16 * nb + lane] = ref[nb];
+    }
+  }
+  lds_sync();
+  auto row_sum = [&](int row) __attribute__((always_inline)) {
+    float z = S.sum[0][row];
+#pragma unroll
+    for (int k = 1; k < WK; ++k) z += S.sum[k][row];
+    return z;
+  };
+  const int64_t row0 = static_cast<int64_t>(J.first) * P.H + J.row_base;
+  if (tid < J.rows) {
+    const float z = row_sum(tid), m = z == 0.f ? -INFINITY : S.by[0][tid];
+    if (!J.whole) P.ws_ml[J.part + tid] = make_float2(m, z);
+    else if (P.lse) P.lse[row0 + tid] = (m + log2f(z)) * static_cast<float>(kLn2);
+  }
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = 16 * rb + rn;
+    if (row >= J.rows) continue;
+    const float z = row_sum(row), f = z == 0.f ? 0.f : 1.f / z;
+#pragma unroll
+    for (int cb = 0; cb < CB; cb += 2) {
+      const lf32x4 a = o[cb][rb] * f, b = o[cb + 1][rb] * f;
+      const int col = wave * (K::C / 4) + 16 * cb + 8 * g;
+      if (!J.whole || P.out_f32) {
+        float* to = J.whole ? static_cast<float*>(P.out) + (row0 + row) * K::C + col : P.ws_o + (J.part + row) * K::C + col;
+        *reinterpret_cast<float4*>(to) = make_float4(a[0], a[1], a[2], a[3]);
+        *reinterpret_cast<float4*>(to + 4) = make_float4(b[0], b[1], b[2], b[3]);
+      } else {
+        const uint2 lo = pack4(a), hi = pack4(b);
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(P.out) + (row0 + row) * K::C + col) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      }
+    }
+  }
+}
+
+// An accumulation in registers of their own kind (the compiler, left to choose, keeps results in vector registers and copies the queries' operands for
+// every product).  Nothing that the compiler knows of may read or write x within a few instructions: see settle().
+__device__ __forceinline__ void accumulate(lf32x16& x, lbf16x8 a, lbf16x8 b) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void clear(lf32x16& x) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float a;
+    asm volatile("v_accvgpr_write_b32 %0, 0" : "=a"(a));
+    x[i] = a;
+  }
+}
+// x *= by, likewise, four at a time.
+__device__ __forceinline__ void rescale(lf32x16& x, float by) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) {
+    float a = x[i], b = x[i + 1], c = x[i + 2], d = x[i + 3], t0, t1, t2, t3;
+    asm volatile(
+        "v_accvgpr_read_b32 %4, %0\n\tv_accvgpr_read_b32 %5, %1\n\tv_accvgpr_read_b32 %6, %2\n\tv_accvgpr_read_b32 %7, %3\n\t"
+        "v_mul_f32 %4, %4, %8\n\tv_mul_f32 %5, %5, %8\n\tv_mul_f32 %6, %6, %8\n\tv_mul_f32 %7, %7, %8\n\t"
+        "v_accvgpr_write_b32 %0, %4\n\tv_accvgpr_write_b32 %1, %5\n\tv_accvgpr_write_b32 %2, %6\n\tv_accvgpr_write_b32 %3, %7"
+        : "+a"(a), "+a"(b), "+a"(c), "+a"(d), "=&v"(t0), "=&v"(t1), "=&v"(t2), "=&v"(t3) : "v"(by));
+    x[i] = a; x[i + 1] = b; x[i + 2] = c; x[i + 3] = d;
+  }
+}
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+// max and sum over a lane and the one 32 away.
+__device__ __forceinline__ float halves_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// What a piece leaves, from the sums and references in LDS.
+template <typename K>
+__device__ __forceinline__ void write_results_wide(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J, lf32x16 (&o)[K::CB][K::RB]) {
+  constexpr int RB = K::RB, CB = K::CB, NS = K::kStages, TERMS = K::TERMS;
+  const int tid = static_cast<int>(threadIdx.x) + opaque_zero(), lane = tid & 63, rn = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned ring = lds_address(&S.ring[0][0]);
+  const int64_t row0 = static_cast<int64_t>(J.first) * P.H + J.row_base;
+  if (tid < J.rows) {
+    const float l = S.sum[0][tid], m = l == 0.f ? -INFINITY : S.by[0][tid];
+    if (!J.whole) P.ws_ml[J.part + tid] = make_float2(m, l);
+    else if (P.lse) P.lse[row0 + tid] = (m + log2f(l)) * static_cast<float>(kLn2);
+  }
+  // Through LDS, so that a store takes consecutive bytes of rows (straight from the registers: 16 bytes of 64 rows, and 40000 cycles for a piece of fp32 results).
+  auto put = [&](auto f32, auto row_blocks) __attribute__((always_inline)) {
+    constexpr bool kF32 = decltype(f32)::value;
+    constexpr int kTogether = decltype(row_blocks)::value, kBytes = K::C * (kF32 ? 4 : 2), kApart = kBytes + 16, kLanes = kBytes / 16;
+    static_assert(kTogether * 32 * kApart <= NS * K::kTile, "");
+    unsigned char* const to = kF32 && !J.whole ? reinterpret_cast<unsigned char*>(P.ws_o + J.part * K::C)
+                                               : static_cast<unsigned char*>(P.out) + row0 * kBytes;
+#pragma unroll
+    for (int rb0 = 0; rb0 < RB; rb0 += kTogether) {
+      if (rb0 > 0) lds_sync();
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+        const int rb = rb0 + j;
+        const float l = S.sum[0][32 * rb + rn], f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const unsigned at = ring + (32 * j + rn) * kApart + (wave * (K::C / 4) + 32 * cb + 16 * h) * (kF32 ? 4 : 2);
+          const lf32x16 x = o[cb][rb] * f;
+          if constexpr (kF32) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *lds_pointer<lf32x4>(at + 4 * i) = lf32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; i += 8)
+              *lds_pointer<raw4>(at + 2 * i) = raw4{pack2(x[i], x[i + 1]), pack2(x[i + 2], x[i + 3]), pack2(x[i + 4], x[i + 5]), pack2(x[i + 6], x[i + 7])};
+          }
+        }
+      }
+      lds_sync();
+      for (int u = tid; u < kTogether * 32 * kLanes; u += kLaThreads) {
+        const int r = u / kLanes, c = u % kLanes;
+        if (32 * rb0 + r >= J.rows) break;
+        *reinterpret_cast<raw4*>(to + static_cast<int64_t>(32 * rb0 + r) * kBytes + 16 * c) = read_lds16(ring + r * kApart + 16 * c);
+      }
+    }
+  };
+  constexpr int kF32Blocks = 2 * 32 * (K::C * 4 + 16) <= NS * K::kTile ? 2 : 1;
+  if (TERMS > 1 || !J.whole) put(std::true_type(), std::integral_constant<int, kF32Blocks>());
+  else if constexpr (TERMS == 1) put(std::false_type(), std::integral_constant<int, 128 * (K::C * 2 + 16) <= NS * K::kTile ? 4 : 2>());
+}
+
+// Up to 128 query rows: matrix instructions bound it, and one wave per SIMD has to keep them busy by itself, at one instruction in 5 cycles.  32x32x16
+// products: a lane has 16 of a tile's 32 scores of one query row (lane % 32; score i: token 8 (i / 4) + 4 (lane / 32) + i % 4), so that a wave works out the
+// weights and the references of its 32 rows by itself.  In turn:
+//   scores of tile t + 1 (36 products, a read of LDS each), at whose middle lies the barrier behind which all waves' weights of tile t are there, then
+//   O^T += V^T P^T of tile t (32 products), between which the weights of tile t + 1 are worked out.
+template <typename K>
+__device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J) {
+  constexpr int W = K::W, T = K::T, RB = K::RB, CB = K::CB, kPages = K::kPages, NS = K::kStages, kSteps = K::kSteps, TERMS = K::TERMS;
+  static_assert(T == 32 && NS >= 3 && kPages == 2 && RB == kLaWaves, "");
+  const int tid = static_cast<int>(threadIdx.x) + opaque_zero(), lane = tid & 63;
+  __builtin_assume(tid >= 0 && tid < kLaThreads);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rn = lane & 31, h = lane >> 5;                      // query row of the block (matrix column), half
+  const int L = J.ctx + J.n;
+
+  constexpr int64_t kPageBytes = kLaPage * W * 2;
+  const int32_t* bt = P.block_table + static_cast<int64_t>(J.b) * P.max_pages;
+  const int last_page = min((L - 1) / kLaPage, P.max_pages - 1), num_pages = P.num_pages, max_pages = P.max_pages;
+  const unsigned char* const pool = reinterpret_cast<const unsigned char*>(P.pool) + (wave & 1) * 8 * W * 2;      // this wave's half of its page
+  const unsigned ring = lds_address(&S.ring[0][0]);
+  // page ids of 32 tiles at a time, a lane each: through the scalar cache they would have every read of LDS waited for alike.  -1: none
+  int ids = -1;
+  auto fetch_ids = [&](int t) __attribute__((always_inline)) {
+    const int lp = kPages * t + lane, id = bt[min(lp, last_page)];
+    ids = id >= 0 && id < num_pages && lp < max_pages ? id : -1;
+  };
+  unsigned bad = 0u;                                            // pages that are none: 2 bits a tile, the present one's lowest
+  // A tile's loads, of which a wave has kLoads: issued one by one among the products (all at once they wait for each other, 700 cycles a tile).
+  const unsigned char* page = pool;
+  unsigned to = 0;
+  auto aim = [&](int t, int slot, int ahead) __attribute__((always_inline)) {
+    const int at = (kPages * (t - J.t0)) & 63;
+    const int a = __builtin_amdgcn_readlane(ids, at), b = __builtin_amdgcn_readlane(ids, at + 1);
+    bad |= ((a < 0 ? 1u : 0u) | (b < 0 ? 2u : 0u)) << (kPages * ahead);
+    page = pool + max(wave < 2 ? a : b, 0) * kPageBytes;        // (one that is none of the pool's: page 0 in its place)
+    to = ring + slot * K::kTile + wave * (K::kTile / kLaWaves);
+  };
+  const unsigned off_at = lds_address(reinterpret_cast<unsigned char*>(&S.off[0][0][0])) + ((wave & 1) * K::kOffsets * kWave + lane) * 4;
+  unsigned off = 0;                                             // of the next load, read well ahead
+  auto read_off = [&](int j) __attribute__((always_inline)) {
+    unsigned at = off_at;
+    asm volatile("" : "+v"(at));
+    off = *lds_pointer<unsigned>(at + j * kWave * 4);
+  };
+  auto issue = [&](int j) __attribute__((always_inline)) {
+    load_to_lds(page, off, to + 1024 * j, 0);
+    if (j + 1 < K::kLoads) read_off(j + 1);
+  };
+
+  const bool touches_drafts = J.t1 * static_cast<int64_t>(T) > J.ctx;
+  int parent = -1;
+  if (touches_drafts && P.parent && tid < J.n) parent = P.parent[J.first + tid];
+  fetch_ids(J.t0);
+  lds_sync();                                                   // the LDS of the piece before is free
+
+  // The queries' operands, each wave's 32 rows in two times 16, laid out as a tile's are in the last two slots, while the first tiles come into the others (each lane
+  // 16 bytes of a row of its own, straight from memory: 64 lines a load, and twice the time).  Rows past the last, which nobody looks at, have bytes of the last.
+  lbf16x8 qf[kSteps];
+  {
+    unsigned off[K::kOffsets];
+    tile_offsets<K>(off, lane);
+    if (wave < 2) {                                             // (the same for every piece)
+#pragma unroll
+      for (int j = 0; j < K::kOffsets; ++j) S.off[wave][j][lane] = off[j] ^ (16 * wave);
+    }
+    const unsigned char* const q = reinterpret_cast<const unsigned char*>(P.q) + (static_cast<int64_t>(J.first) * P.H + J.row_base) * (W * 2);
+    const unsigned mine = ring + (NS - 2) * K::kTile + wave * (16 * K::kRow);
+    auto bring = [&](int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int eight = 0; eight < 2; ++eight) {
+        const int row = min(32 * wave + 16 * half + 8 * eight, J.rows - 1);
+        const unsigned last = (J.rows - row) * (W * 2) - 16;
+#pragma unroll
+        for (int j = 0; j < K::kOffsets; ++j) load_to_lds(q + row * (W * 2), min(off[j] ^ (16 * eight), last), mine + eight * (8 * K::kRow) + 1024 * j, 0);
+      }
+    };
+    auto take = [&](int half) __attribute__((always_inline)) {
+      const unsigned at = mine + (rn & 15) * K::kRow + (h ^ fold(rn)) * 16;
+      if (rn >> 4 == half) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) qf[s] = operand(read_lds16((at ^ (32 * (s & 3))) + 128 * (s >> 2)));
+      }
+    };
+    bring(0);
+    lds_sync();                                                 // (S.off)
+#pragma unroll
+    for (int i = 0; i < NS - 2; ++i) {
+      if (J.t0 + i >= J.t1) break;
+      aim(J.t0 + i, i, i);
+      read_off(0);
+#pragma unroll
+      for (int j = 0; j < K::kLoads; ++j) issue(j);
+    }
+    wait_loads<0>();
+    take(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (what was there has been read)
+    bring(1);
+    if (touches_drafts) find_lineage<K>(P, S, J, tid, parent);
+    wait_loads<0>();
+    take(1);
+    lds_sync();
+    if (J.t0 + NS - 2 < J.t1) {
+      aim(J.t0 + NS - 2, NS - 2, NS - 2);
+      read_off(0);
+#pragma unroll
+      for (int j = 0; j < K::kLoads; ++j) issue(j);
+    }
+  }
+
+  // Operand reads.  K: token rn, unit 2 s + h.  V by columns: lane i of 16 (group G of two in a half) points at token 4 h + i / 4 (and 8 more), column
+  // 16 (i % 2) + 8 G + 4 (i / 2 % 2): column 16 h + 4 a + e of the wave's 32 is row 8 a + 4 h + e of the block, so that a lane ends up with 16 consecutive ones.
+  const unsigned k_at = rn * K::kRow + (h ^ fold(rn)) * 16;     // step s at ^ 32 (s % 4), 128 (s / 4) more
+  const int vi = lane & 15, vt = 4 * h + (vi >> 2);
+  const unsigned v_at = vt * K::kRow + ((2 * (vi & 1) + ((lane >> 4) & 1)) ^ fold(vt)) * 16 + 8 * ((vi >> 1) & 1) + wave * (K::C / 4 * 2);   // block cb at ^ 64 (cb % 2)
+  // weights: the first kInTile operands lie in the tile's rows behind the latents, 8 lanes to a row
+  static_assert(K::kInTile == RB, "the operands in the tile are those of one term and half of the tokens");
+  const unsigned in_tile = (lane >> 3) * K::kRow + K::C * 2 + (lane & 7) * 16, apart = lds_address(&S.p[0][0]) + 16 * lane;
+  // (bases that the compiler knows no parts of, so that it does not keep one for every constant behind them)
+  auto opaque = [&](unsigned at) __attribute__((always_inline)) { asm volatile("" : "+v"(at)); return at; };
+  auto read_p = [&](unsigned inside, unsigned outside, int f) __attribute__((always_inline)) {
+    return operand(read_lds16(f < K::kInTile ? inside + f * 8 * K::kRow : outside + (f - K::kInTile) * 1024));
+  };
+
+  float ref = kLaNoScore, sum = 0.f, z = 0.f;
+  lf32x16 o[CB][RB];
+  lf32x16 s;
+  constexpr int kDeep = 7;                                      // K is read six steps ahead
+  lbf16x8 k[kDeep];
+  // (the shared part of the keys first: weights go where it lies, behind a barrier after these steps)
+  auto place = [](int step) { return step < K::R / 16 ? K::C / 16 + step : step - K::R / 16; };
+  auto read_k = [&](unsigned tile, int step) __attribute__((always_inline)) {
+    const int at = place(step);
+    k[step % kDeep] = operand(read_lds16(((tile + k_at) ^ (32 * (at & 3))) + 128 * (at >> 2)));
+  };
+  auto score = [&](unsigned tile, int step) __attribute__((always_inline)) {
+    if (step + kDeep - 1 < kSteps) read_k(tile, step + kDeep - 1);
+    lf32x16 zero;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[step % kDeep], qf[place(step)], step == 0 ? zero : s, 0, 0, 0);
+  };
+  // From this tile on rows differ in what they see (or, behind the last tile, see nothing).
+  const int drafts_from = min(J.ctx / T, J.t1);
+  // of tile t, whose pages' bits are `none`: scores that a row does not see; behind the last tile, all
+  auto mask = [&](int t, unsigned none) __attribute__((always_inline)) {
+    const int node = touches_drafts ? S.node[32 * wave + rn] : 0;
+#pragma unroll
+    for (int page = 0; page < 2; ++page) {
+      const int64_t past = static_cast<int64_t>(t) * T + 16 * page - J.ctx;
+      uint32_t seen = 0xffffu;
+      if (past > -16 && t < J.t1) seen = page_mask(S.anc[node][0], S.anc[node][1], static_cast<int>(past));
+      seen = ((none >> page) & 1u) != 0u || t >= J.t1 ? 0u : seen >> (4 * h);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[8 * page + i] = (seen >> (8 * (i >> 2) + (i & 3))) & 1u ? s[8 * page + i] : -INFINITY;
+    }
+  };
+  // A row's reference follows its maximum where that has come far ahead (each row by itself: its result has the same bits whatever the others are); what the
+  // results of the tiles before have to be scaled by is left for all waves, which look at the flags behind the next barrier.
+  float top = 0.f;
+  auto find_top = [&](int part) __attribute__((always_inline)) {
+    if (part == 0) top = max3(s[0], s[1], s[2]);
+#pragma unroll
+    for (int i = part == 0 ? 3 : 9; i < (part == 0 ? 9 : 15); i += 2) top = max3(top, s[i], s[i + 1]);
+    if (part == 1) top = __builtin_elementwise_maximum(top, s[15]) * P.c;
+  };
+  auto refer = [&](int t) __attribute__((always_inline)) {
+    const unsigned flag = any_lane(top > ref + kLaSlack) ? 1u : 0u;
+    S.ahead[t & 1][wave] = flag;
+    if (__builtin_expect(flag != 0u, 0)) {
+      const float now = halves_max(top), next = now > ref + kLaSlack ? now : ref, by = fast_exp2(ref - next);
+      ref = next;
+      sum *= by;
+      S.by[t & 1][32 * wave + rn] = by;
+    }
+  };
+  // weights of pair i of a lane's 8 pairs of scores; four pairs make an operand
+  uint32_t w[TERMS][4];
+  float p0 = 0.f, p1 = 0.f;
+  auto weigh_pair = [&](unsigned inside, unsigned outside, int i, int part) __attribute__((always_inline)) {
+    if (part == 0) p0 = fast_exp2(fmaf(s[2 * i], P.c, -ref));
+    if (part == 1) p1 = fast_exp2(fmaf(s[2 * i + 1], P.c, -ref));
+    if (part < 2) return;
+    z = i == 0 ? p0 + p1 : z + (p0 + p1);
+    asm volatile("" : "+v"(z));                                 // (here, and not where the sum is first needed)
+    float r0 = p0, r1 = p1;
+#pragma unroll
+    for (int term = 0; term < TERMS; ++term) {
+      w[term][i & 3] = pack2(r0, r1);
+      r0 -= bf16_lo(w[term][i & 3]);
+      r1 -= bf16_hi(w[term][i & 3]);
+    }
+    if ((i & 3) == 3) {
+#pragma unroll
+      for (int term = 0; term < TERMS; ++term) {
+        const int f = 2 * RB * term + RB * (i >> 2);            // operand f + wave
+        *lds_pointer<raw4>(f < K::kInTile ? inside + wave * (8 * K::kRow) : outside + (f - K::kInTile + wave) * 1024) =
+            raw4{w[term][0], w[term][1], w[term][2], w[term][3]};
+      }
+    }
+  };
+
+  constexpr int kBarrier = 8, kCheck = kBarrier + (kSteps - kBarrier) / 3, kRead = kCheck + (kSteps - kCheck) / 3;
+  static_assert(kBarrier >= K::R / 16, "the shared part of the keys has been read");
+  auto issue_at = [&](int step) __attribute__((always_inline)) {
+    constexpr int kEvery = (kSteps - kBarrier) / K::kLoads;
+    static_assert(kEvery >= 2, "");
+    const int at = step - kBarrier;
+    if (at % kEvery == 1 && at / kEvery < K::kLoads) issue(at / kEvery);
+  };
+  // The first scores of the tile behind t (past the last one: of whatever is there), up to where the flags of tile t are known.  Not 0: there is something to be
+  // done before tile t is added: results are to be scaled, or rows differ in what they see.
+  auto first_half = [&](int t, int slot) __attribute__((always_inline)) {
+    const unsigned tile1 = ring + (slot + 1 == NS ? 0 : slot + 1) * K::kTile;
+#pragma unroll
+    for (int step = 0; step < kBarrier; ++step) {
+      score(tile1, step);
+      if (step == 1) {
+        const int ahead = min(t + NS - 1, J.t1 - 1);            // (behind the last tile that one again, which nobody looks at)
+        if (__builtin_expect(ahead == t + NS - 1 && ((kPages * (ahead - J.t0)) & 63) == 0, 0)) fetch_ids(ahead);
+        aim(ahead, slot == 0 ? NS - 1 : slot - 1, NS - 1);
+      }
+      if (step == kBarrier - 1) read_off(0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (NS == 4) wait_loads<0>();                               // the tile after next is here
+    lds_sync();
+    const raw4 flags = *reinterpret_cast<const raw4*>(S.ahead[t & 1]);
+    unsigned special = 0u;
+#pragma unroll
+    for (int step = kBarrier; step < kCheck; ++step) {
+      score(tile1, step);
+      issue_at(step);
+      if (step == kCheck - 2) special = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) | (bad & 3u) | (t >= drafts_from ? 1u : 0u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return special;
+  };
+  // The rest of the scores; O^T += V^T P^T of tile t, and the weights of the tile behind it.
+  auto second_half = [&](int t, int slot) __attribute__((always_inline)) {
+    const int slot1 = slot + 1 == NS ? 0 : slot + 1;
+    const unsigned tile = ring + slot * K::kTile, tile1 = ring + slot1 * K::kTile, tile2 = ring + (slot1 + 1 == NS ? 0 : slot1 + 1) * K::kTile;
+#pragma unroll
+    for (int step = kCheck; step < kRead; ++step) {
+      score(tile1, step);
+      issue_at(step);
+      if (step == kCheck) sum += z;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const unsigned inside = opaque(tile + in_tile), outside = opaque(apart + (t & 1) * K::kWeights), v_base = opaque(tile + v_at), v_other = v_base ^ 16;
+    const unsigned inside1 = opaque(tile1 + in_tile), outside1 = opaque(apart + ((t + 1) & 1) * K::kWeights);
+    lbf16x8 p[2][RB];
+    ls16x4 v[3][2];
+    auto read_v = [&](int i, int part) __attribute__((always_inline)) {                     // block i % CB, tokens 16 (i / CB) ..
+      const unsigned at = part == 0 ? v_base : v_other;
+      v[i % 3][part] = read_columns((at ^ (64 * (i % CB & 1))) + 128 * (i % CB >> 1) + (i / CB * 16 + part * 8) * K::kRow);
+    };
+#pragma unroll
+    for (int step = kRead; step < kSteps; ++step) {
+      score(tile1, step);
+      issue_at(step);
+      constexpr int kReads = RB + 4, kAt = (kReads + kSteps - kRead - 1) / (kSteps - kRead);
+#pragma unroll
+      for (int at = (step - kRead) * kAt; at < (step - kRead + 1) * kAt && at < kReads; ++at) {      // operands of the first products
+        if (at < RB) p[0][at] = read_p(inside, outside, at);
+        else read_v((at - RB) >> 1, (at - RB) & 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__builtin_expect(t + 1 >= drafts_from || (bad & (3u << kPages)) != 0u, 0)) mask(t + 1, (bad >> kPages) & 3u);
+    // one product, and what a lane has for it of the next tile's weights and of operand reads: what the products' 32 cycles hold
+    constexpr int kBlocks = 2 * CB * TERMS, kProducts = kBlocks * RB;
+    auto beside = [&](int at) __attribute__((always_inline)) {
+      if (at < 2) find_top(at);
+      if (at == 2) refer(t + 1);
+      constexpr int kPer = kProducts >= 28 ? 3 : 1;             // products for a pair
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int part = 0; part < 3; ++part)
+          if (at == 3 + i * kPer + (kPer > 1 ? part : 0)) weigh_pair(inside1, outside1, i, part);
+      const int late = at - (kProducts - (kDeep - 1));
+      if (NS == 4 && late >= 0) read_k(tile2, late);
+    };
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      const int term = b / (2 * CB), i = b % (2 * CB);
+      if (term > 0 && i == 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) read_v(j >> 1, j & 1);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) p[0][rb] = read_p(inside, outside, 2 * RB * term + rb);
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        if (rb < 2 && i + 2 < 2 * CB) read_v(i + 2, rb);
+        if (i == CB - 1) p[1][rb] = read_p(inside, outside, 2 * RB * term + RB + rb);
+        accumulate(o[i % CB][rb], join(v[i % 3][0], v[i % 3][1]), p[i / CB][rb]);
+        beside(b * RB + rb);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    bad >>= kPages;
+    if (NS == 3) {
+      wait_loads<0>();
+      lds_sync();
+#pragma unroll
+      for (int step = 0; step < kDeep - 1; ++step) read_k(tile2, step);
+    }
+  };
+
+  // ---- the first tile's scores and weights ----
+#pragma unroll
+  for (int step = 0; step < kDeep - 1; ++step) read_k(ring, step);
+#pragma unroll
+  for (int step = 0; step < kSteps; ++step) {
+    score(ring, step);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (J.t0 >= drafts_from || (bad & 3u) != 0u) mask(J.t0, bad & 3u);
+  if (NS == 3) wait_loads<0>();                                 // the second tile
+  lds_sync();                                                   // all have read the shared part of the keys
+  find_top(0);
+  find_top(1);
+  refer(J.t0);
+  {
+    const unsigned inside = opaque(ring + in_tile), outside = opaque(apart + (J.t0 & 1) * K::kWeights);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int part = 0; part < 3; ++part) weigh_pair(inside, outside, i, part);
+    }
+  }
+#pragma unroll
+  for (int step = 0; step < kDeep - 1; ++step) read_k(ring + K::kTile, step);
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) clear(o[cb][rb]);
+  int slot = 0, t = J.t0;
+  unsigned special = first_half(t, slot);
+  // (Two loops: results are scaled in the outer one alone, which keeps their registers where the products have them.)
+  for (;;) {
+    if (special) {
+      settle();
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        if (__builtin_amdgcn_readfirstlane(S.ahead[t & 1][rb]) == 0u) continue;
+        const float by = S.by[t & 1][32 * rb + rn];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) rescale(o[cb][rb], by);
+      }
+      settle();
+      if (t >= drafts_from || (bad & 3u) != 0u) {
+        take_out<K>(ring + slot * K::kTile, tid);
+        lds_sync();
+      }
+    }
+    bool more;
+    do {
+      second_half(t, slot);
+      slot = slot + 1 == NS ? 0 : slot + 1;
+      more = ++t < J.t1;
+      if (!more) break;
+      special = first_half(t, slot);
+    } while (__builtin_expect(special == 0u, 1));
+    if (!more) break;
+  }
+  settle();
+  wait_loads<0>();
+
+  // ---- results ----
+  lds_sync();                                                   // (S.by has been read)
+  sum = halves_sum(sum);
+  if (h == 0) {
+    S.sum[0][32 * wave + rn] = sum;
+    S.by[0][32 * wave + rn] = ref;
+  }
+  lds_sync();
+  write_results_wide<K>(P, S, J, o);
+}
+
 template <typename K>
 __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J) {
-  constexpr int W = K::W, T = K::T, M = K::M, NB = K::NB, KB = K::KB, WK = K::WK, RB = K::RB, CB = K::CB, kPages = K::kPages, NS = K::kStages;
+  constexpr int W = K::W, T = K::T, NB = K::NB, WK = K::WK, RB = K::RB, CB = K::CB, kPages = K::kPages, NS = K::kStages;
   const int tid = static_cast<int>(threadIdx.x) + opaque_zero(), lane = tid & 63;
   __builtin_assume(tid >= 0 && tid < kLaThreads);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rn = lane & 15, g = lane >> 4;
-  const int wr = wave / WK, wk = wave % WK;                     // of the scores: this wave's rows 16 NB wr .., tokens 16 KB wk .. of a tile
   const int L = J.ctx + J.n;
 
-  // ---- a tile's loads ----
-  // Row r of a tile, 16-byte unit u lies at u ^ f(r), f = 4 (r / 2 % 2) + 2 (r / 4 % 2): 8 lanes that read a unit of 8 rows, and 16 lanes that read 4 rows
-  // by columns, take 128 bytes from as many banks (rows are 128 bytes apart modulo the banks' 256).  Units past the row's last repeat one.
   unsigned off[K::kOffsets];
-#pragma unroll
-  for (int j = 0; j < K::kOffsets; ++j) {
-    const int u = 64 * j + lane, r = u / K::kUnits, p = u % K::kUnits;
-    int unit = p ^ (4 * ((r >> 1) & 1) + 2 * ((r >> 2) & 1));
-    if constexpr (K::kUnits * 8 != W) unit = min(unit, W / 8 - 1);
-    off[j] = r * (W * 2) + unit * 16;
-  }
+  tile_offsets<K>(off, lane);
   constexpr int64_t kPageBytes = kLaPage * W * 2;
   const const_i32* bt = (const const_i32*)(P.block_table + static_cast<int64_t>(J.b) * P.max_pages);
   const int last_page = min((L - 1) / kLaPage, P.max_pages - 1);
@@ -201,7 +818,7 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     const unsigned to = ring + slot * K::kTile + wave * (K::kTile / kLaWaves);
     const unsigned char* page = reinterpret_cast<const unsigned char*>(P.pool) + __builtin_amdgcn_readfirstlane(my_id) * kPageBytes + (kPages == 4 ? 0 : (wave & 1) * 8 * W * 2);
 #pragma unroll
-    for (int j = 0; j < K::kLoads; ++j) load_to_lds(page + j / K::kOffsets * 8 * W * 2, off[j % K::kOffsets], to + 1024 * j, 0);
+    for (int j = 0; j < K::kLoads; ++j) load_to_lds(page + j / K::kOffsets * 8 * W * 2, j < K::kOffsets ? off[j] : off[j - K::kOffsets] ^ 16, to + 1024 * j, 0);
   };
   unsigned long long bad = 0ull;                                // pages that are none: kPages bits a tile, the present one's lowest
 
@@ -211,7 +828,7 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     const uint16_t* q = P.q + (static_cast<int64_t>(J.first) * P.H + J.row_base) * W + 8 * g;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const uint16_t* row = q + static_cast<int64_t>(min(16 * (NB * wr + nb) + rn, J.rows - 1)) * W;
+      const uint16_t* row = q + static_cast<int64_t>(min(16 * nb + rn, J.rows - 1)) * W;
 #pragma unroll
       for (int s = 0; s < K::kSteps; ++s) qf[nb][s] = operand(*reinterpret_cast<const raw4*>(row + 32 * s));
     }
@@ -229,36 +846,13 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
       fetch_ids(J.t0 + i + 1);
     }
   }
-  if (touches_drafts) {
-    if (tid < kLaMaxNodes) S.parent[tid] = parent;
-    if (tid < M) S.node[tid] = (J.row_base + min(tid, J.rows - 1)) / P.H;
-    lds_sync();
-    if (tid < kLaMaxNodes) {
-      unsigned long long w[2] = {0ull, 0ull};
-      if (tid < J.n) {
-        if (P.parent) {
-          int a = tid;
-          for (int k = 0; k < kLaMaxNodes && a >= 0; ++k) {
-            if (a < 64) w[0] |= 1ull << a; else w[1] |= 1ull << (a - 64);
-            const int p = S.parent[a];
-            a = (p >= a || p < 0) ? -1 : p;                     // (a malformed entry is a root)
-          }
-        } else {
-          w[0] = tid < 63 ? (2ull << tid) - 1ull : ~0ull;
-          w[1] = tid < 64 ? 0ull : (tid < 127 ? (2ull << (tid - 64)) - 1ull : ~0ull);
-        }
-      }
-      S.anc[tid][0] = w[0];
-      S.anc[tid][1] = w[1];
-    }
-  }
+  if (touches_drafts) find_lineage<K>(P, S, J, tid, parent);
 
-  // Operand reads: K, token 16 (KB wk + kb) + rn, unit 4 s + g; V by columns, token 4 g + rn / 4 (and 16 more), unit 4 (cb / 2) + rn % 4, half cb % 2: column
+  // Operand reads: K, token 16 wave + rn, unit 4 s + g; V by columns, token 4 g + rn / 4 (and 16 more), unit 4 (cb / 2) + rn % 4, half cb % 2: column
   // 32 p + 8 g + 4 s + i of the wave's is row 4 g + i of block 2 p + s, so that a lane ends up with 8 consecutive ones
-  const int kf = 4 * ((rn >> 1) & 1) + 2 * ((rn >> 2) & 1);
-  const unsigned k_at = (16 * KB * wk + rn) * K::kRow + (g ^ kf) * 16;              // even steps; odd ones at ^ 64; 128 more every two
-  const int vt = 4 * g + (rn >> 2), vf = 4 * ((vt >> 1) & 1) + 2 * ((vt >> 2) & 1);
-  const unsigned v_at = vt * K::kRow + ((rn & 3) ^ vf) * 16 + wave * (K::C / 4 * 2);   // even pairs of blocks; odd ones at ^ 64; 128 more every two
+  const unsigned k_at = (16 * wave + rn) * K::kRow + (g ^ fold(rn)) * 16;             // even steps; odd ones at ^ 64; 128 more every two
+  const int vt = 4 * g + (rn >> 2);
+  const unsigned v_at = vt * K::kRow + ((rn & 3) ^ fold(vt)) * 16 + wave * (K::C / 4 * 2);   // even pairs of blocks; odd ones at ^ 64; 128 more every two
   const unsigned p_at = lds_address(&S.p[0][0]);
 
   float ref[NB], sum[NB];
@@ -293,37 +887,29 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     const unsigned tile = ring + slot * K::kTile;
 
     // ---- scores ----
-    lf32x4 s[KB][NB];
+    lf32x4 s[NB];
 #pragma unroll
     for (int step = 0; step < K::kSteps; ++step) {
-      lbf16x8 k[KB];
+      const lbf16x8 k = operand(read_lds16(((tile + k_at) ^ (64 * (step & 1))) + 128 * (step >> 1)));
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) k[kb] = operand(read_lds16(((tile + k_at) ^ (64 * (step & 1))) + 128 * (step >> 1) + kb * 16 * K::kRow));
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[kb][nb] = multiply(k[kb], qf[nb][step], step == 0 ? lf32x4{0.f, 0.f, 0.f, 0.f} : s[kb][nb]);
+      for (int nb = 0; nb < NB; ++nb) s[nb] = multiply(k, qf[nb][step], step == 0 ? lf32x4{0.f, 0.f, 0.f, 0.f} : s[nb]);
       if (step % 4 == 3) __builtin_amdgcn_sched_barrier(0);     // (else all of K is read first, into registers there are none of)
     }
 
     // ---- masks: only where the tile reaches the drafts, or a page is none ----
     const bool special = (t + 1) * static_cast<int64_t>(T) > J.ctx || (bad & ((1u << kPages) - 1u)) != 0ull;
     if (special) {
+      const int64_t past = static_cast<int64_t>(t) * T + 16 * wave - J.ctx;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const int page = KB * wk + kb;
-        const int64_t past = static_cast<int64_t>(t) * T + 16 * page - J.ctx;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          uint32_t seen = 0xffffu;
-          if (past > -16) {
-            const int node = S.node[16 * (NB * wr + nb) + rn];
-            seen = page_mask(S.anc[node][0], S.anc[node][1], static_cast<int>(past));
-          }
-          seen = (bad >> page) & 1ull ? 0u : seen >> (4 * g);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[kb][nb][i] = (seen >> i) & 1u ? s[kb][nb][i] : -INFINITY;
+      for (int nb = 0; nb < NB; ++nb) {
+        uint32_t seen = 0xffffu;
+        if (past > -16) {
+          const int node = S.node[16 * nb + rn];
+          seen = page_mask(S.anc[node][0], S.anc[node][1], static_cast<int>(past));
         }
+        seen = (bad >> wave) & 1ull ? 0u : seen >> (4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[nb][i] = (seen >> i) & 1u ? s[nb][i] : -INFINITY;
       }
     }
 
@@ -332,61 +918,50 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     bool ahead = false;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      top[nb] = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) top[nb] = max3(top[nb], max3(s[kb][nb][0], s[kb][nb][1], s[kb][nb][2]), s[kb][nb][3]);
-      top[nb] *= P.c;
+      top[nb] = __builtin_elementwise_maximum(max3(s[nb][0], s[nb][1], s[nb][2]), s[nb][3]) * P.c;
       ahead |= top[nb] > ref[nb] + kLaSlack;
     }
     auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         z[nb] = 0.f;
-        uint32_t w[K::TERMS][KB][2];
+        uint32_t w[K::TERMS][2];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int i = 0; i < 2; ++i) {
+          const float p0 = fast_exp2(fmaf(s[nb][2 * i], P.c, -ref[nb])), p1 = fast_exp2(fmaf(s[nb][2 * i + 1], P.c, -ref[nb]));
+          z[nb] += p0 + p1;
+          float r0 = p0, r1 = p1;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float p0 = fast_exp2(fmaf(s[kb][nb][2 * i], P.c, -ref[nb])), p1 = fast_exp2(fmaf(s[kb][nb][2 * i + 1], P.c, -ref[nb]));
-            z[nb] += p0 + p1;
-            float r0 = p0, r1 = p1;
-#pragma unroll
-            for (int term = 0; term < K::TERMS; ++term) {
-              w[term][kb][i] = pack2(r0, r1);
-              r0 -= bf16_lo(w[term][kb][i]);
-              r1 -= bf16_hi(w[term][kb][i]);
-            }
+          for (int term = 0; term < K::TERMS; ++term) {
+            w[term][i] = pack2(r0, r1);
+            r0 -= bf16_lo(w[term][i]);
+            r1 -= bf16_hi(w[term][i]);
           }
+        }
         // blocks of 16 tokens 2 m and 2 m + 1 are the halves of a lane's 16 bytes
 #pragma unroll
         for (int term = 0; term < K::TERMS; ++term) {
-          const unsigned at = p_at + term * K::kWeights + 16 * lane + (NB * wr + nb) * 1024;
-          if constexpr (KB == 1) {
-            *lds_pointer<unsigned long long>(at + (wk >> 1) * RB * 1024 + 8 * (wk & 1)) = static_cast<unsigned long long>(w[term][0][1]) << 32 | w[term][0][0];
-          } else {
-#pragma unroll
-            for (int m = 0; m < KB / 2; ++m)
-              *lds_pointer<raw4>(at + (wk * (KB / 2) + m) * RB * 1024) = raw4{w[term][2 * m][0], w[term][2 * m][1], w[term][2 * m + 1][0], w[term][2 * m + 1][1]};
-          }
+          const unsigned at = p_at + (term * (T / 32) * RB + nb) * 1024 + 16 * lane;
+          *lds_pointer<unsigned long long>(at + (wave >> 1) * RB * 1024 + 8 * (wave & 1)) = static_cast<unsigned long long>(w[term][1]) << 32 | w[term][0];
         }
       }
     };
     weigh();
     const unsigned flag = any_lane(ahead) ? 1u : 0u;
-    if (lane == 0) S.ahead[wave] = flag;
+    if (lane == 0) S.ahead[0][wave] = flag;
     lds_sync();
-    const raw4 flags = *reinterpret_cast<const raw4*>(S.ahead);
+    const raw4 flags = *reinterpret_cast<const raw4*>(S.ahead[0]);
     if (__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3])) {
       // ---- a row's reference follows its maximum where that has come far ahead (in all waves, or in none) ----
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float m = groups_max(top[nb]);
-        if (lane < 16) S.top[wk][16 * (NB * wr + nb) + lane] = m;
+        if (lane < 16) S.top[wave][16 * nb + lane] = m;
       }
       lds_sync();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const int row = 16 * (NB * wr + nb) + rn;
+        const int row = 16 * nb + rn;
         float now = S.top[0][row];
 #pragma unroll
         for (int k = 1; k < WK; ++k) now = fmaxf(now, S.top[k][row]);
@@ -394,13 +969,13 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
         const float by = fast_exp2(ref[nb] - now);
         ref[nb] = now;
         sum[nb] *= by;
-        if (wk == 0 && lane < 16) S.by[row] = by;
+        if (wave == 0 && lane < 16) S.by[0][row] = by;
       }
       weigh();
       lds_sync();
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const float by = S.by[16 * rb + rn];
+        const float by = S.by[0][16 * rb + rn];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) o[cb][rb] *= by;
       }
@@ -408,20 +983,8 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) sum[nb] += z[nb];
 
-    // A weight of zero times what is not finite would be NaN: where rows differ in what they see, such values are taken out of V.  (A row that
-    // sees one has met it in its scores.)
     if (special) {
-      for (int at = 16 * tid; at < K::kTile; at += 16 * kLaThreads) {
-        raw4 w = read_lds16(tile + at);
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool l = (w[i] & 0x7f80u) == 0x7f80u, h = (w[i] & 0x7f800000u) == 0x7f800000u;
-          any |= l | h;
-          w[i] = (l ? 0u : w[i] & 0xffffu) | (h ? 0u : w[i] & 0xffff0000u);
-        }
-        if (any) *lds_pointer<raw4>(tile + at) = w;
-      }
+      take_out<K>(tile, tid);
       lds_sync();
     }
 
@@ -432,7 +995,7 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
 #pragma unroll
       for (int term = 0; term < K::TERMS; ++term)
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) p[term][rb] = operand(read_lds16(p_at + term * K::kWeights + (m * RB + rb) * 1024 + 16 * lane));
+        for (int rb = 0; rb < RB; ++rb) p[term][rb] = operand(read_lds16(p_at + ((term * (T / 32) + m) * RB + rb) * 1024 + 16 * lane));
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
         const unsigned at = ((tile + v_at) ^ (64 * ((cb >> 1) & 1))) + 128 * (cb >> 2) + 8 * (cb & 1) + m * 32 * K::kRow;
@@ -449,48 +1012,7 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     slot = slot + 1 == NS ? 0 : slot + 1;
   }
 
-  // ---- results ----
-  lds_sync();                                                   // (S.by has been read)
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const float z = groups_sum(sum[nb]);
-    if (lane < 16) {
-      S.sum[wk][16 * (NB * wr + nb) + lane] = z;
-      if (wk == 0) S.by[16 * (NB * wr + nb) + lane] = ref[nb];
-    }
-  }
-  lds_sync();
-  auto row_sum = [&](int row) __attribute__((always_inline)) {
-    float z = S.sum[0][row];
-#pragma unroll
-    for (int k = 1; k < WK; ++k) z += S.sum[k][row];
-    return z;
-  };
-  const int64_t row0 = static_cast<int64_t>(J.first) * P.H + J.row_base;
-  if (tid < J.rows) {
-    const float z = row_sum(tid), m = z == 0.f ? -INFINITY : S.by[tid];
-    if (!J.whole) P.ws_ml[J.part + tid] = make_float2(m, z);
-    else if (P.lse) P.lse[row0 + tid] = (m + log2f(z)) * static_cast<float>(kLn2);
-  }
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = 16 * rb + rn;
-    if (row >= J.rows) continue;
-    const float z = row_sum(row), f = z == 0.f ? 0.f : 1.f / z;
-#pragma unroll
-    for (int cb = 0; cb < CB; cb += 2) {
-      const lf32x4 a = o[cb][rb] * f, b = o[cb + 1][rb] * f;
-      const int col = wave * (K::C / 4) + 16 * cb + 8 * g;
-      if (!J.whole || P.out_f32) {
-        float* to = J.whole ? static_cast<float*>(P.out) + (row0 + row) * K::C + col : P.ws_o + (J.part + row) * K::C + col;
-        *reinterpret_cast<float4*>(to) = make_float4(a[0], a[1], a[2], a[3]);
-        *reinterpret_cast<float4*>(to + 4) = make_float4(b[0], b[1], b[2], b[3]);
-      } else {
-        const uint2 lo = pack4(a), hi = pack4(b);
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(P.out) + (row0 + row) * K::C + col) = make_uint4(lo.x, lo.y, hi.x, hi.y);
-      }
-    }
-  }
+  write_results<K>(P, S, J, o, ref, sum, wave, lane);
 }
 
 template <typename K>
@@ -498,108 +1020,174 @@ __global__ __launch_bounds__(kLaThreads, 1) void attn_latent_kernel(LatentAttnPa
   extern __shared__ __align__(1024) unsigned char smem[];
   auto& S = *reinterpret_cast<LatentShared<K>*>(smem);
   constexpr int M = K::M, T = K::T;
-  const int lane = threadIdx.x & 63;
   const int batches = (P.B + 63) / 64;
+  if (threadIdx.x == 0) P.cut[blockIdx.x] = make_int4(0, 0, 0, 0);
   double total = 0.0;
-  LaRequests r;
-  for (int k = batches - 1; k >= 0; --k) {                      // (down: the first 64 requests stay in registers)
-    r = load_requests<M, T>(P, k, lane);
-    total += r.sum;
-  }
-  const LaCut cut = cut_ranges(P.ranges, total);
+  for (int k = batches - 1; k >= 0; --k) total += load_requests<K>(P, S, k);        // (down: the first 64 requests stay)
+  total = uniform(total);
+  const LaCut cut = cut_ranges(P.ranges, K::kLeast, total);
   // Workgroups go to the 8 XCDs in turn: renumbered so that neighbouring ranges, which may hold groups of rows of one request, share an L2
   const int each = (cut.used + 7) >> 3, range = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
-  int4 record = make_int4(0, 0, 0, 0);
-  if (any_lane(total > 0.0) && static_cast<int>(blockIdx.x >> 3) < each && range < cut.used) {
-    const double from = range_start(cut, range), end = range_start(cut, range + 1);
-    double base = 0.0;                                          // cost before these 64 requests
-    double at = from;
-    for (int k = 0; any_lane(at < end);) {                      // (uniform, as the compiler has to know)
-      const unsigned long long later = __builtin_amdgcn_ballot_w64(base + r.upto > at);
-      if (later == 0ull) {
-        base += r.sum;
-        if (++k >= batches) break;
-        r = load_requests<M, T>(P, k, lane);
-        continue;
-      }
-      const int i = __ffsll(later) - 1;
-      LatentPiece J;
-      J.b = 64 * k + i;
-      J.ctx = __builtin_amdgcn_readlane(r.ctx, i);
-      J.first = __builtin_amdgcn_readlane(r.first, i);
-      J.n = __builtin_amdgcn_readlane(r.n, i);
-      const int rows = J.n * P.H, groups = (rows + M - 1) / M, tiles = tiles_of<T>(P, J.ctx, J.n);
-      const double behind = base + lane_f64(r.upto, i);
-      double start = behind - static_cast<double>(groups) * (kLaHead + tiles);
-      for (int grp = 0; grp < groups && any_lane(start < end); ++grp, start += kLaHead + tiles) {
-        // tile k is at start + kLaHead + k and belongs to the range that this is in
-        J.t0 = static_cast<int>(fmin(fmax(from - start - kLaHead, 0.0), static_cast<double>(tiles)));
-        J.t1 = static_cast<int>(fmin(fmax(end - start - kLaHead, 0.0), static_cast<double>(tiles)));
-        J.t0 = __builtin_amdgcn_readfirstlane(J.t0);
-        J.t1 = __builtin_amdgcn_readfirstlane(J.t1);
-        if (J.t0 >= J.t1) continue;
-        J.row_base = M * grp;
-        J.rows = min(rows - J.row_base, M);
-        J.whole = J.t0 == 0 && J.t1 == tiles;
-        J.part = (static_cast<int64_t>(range) * 2 + (J.t0 == 0 ? 1 : 0)) * M;
-        latent_piece<K>(P, S, J);
-        if (!J.whole && J.t0 == 0) {
-          const int last = range_of(cut, start + kLaHead + tiles - 1);
-          const int64_t row0 = static_cast<int64_t>(J.first) * P.H + J.row_base;
-          record = make_int4(static_cast<int>(row0 & 0xffffffff), static_cast<int>(row0 >> 32), J.rows << 16 | (last - range + 1), range);
-        }
-      }
-      at = behind;
-    }
+  if (!any_lane(total > 0.0) || static_cast<int>(blockIdx.x >> 3) >= each || range >= cut.used) return;
+  if (threadIdx.x == 0) {
+    S.each = cut.each;
+    S.total = cut.total;
   }
-  if (P.cut && threadIdx.x == 0) P.cut[blockIdx.x] = record;
+  const double end = uniform(range_start(cut, range + 1));
+  double at = uniform(range_start(cut, range)), base = 0.0;     // cost before these 64 requests
+  const int used = cut.used;
+  // (Nothing but these and the requests in LDS is kept across a piece: it has use for all registers.)
+  for (int k = 0; any_lane(at < end);) {
+    const int lane = (threadIdx.x + opaque_zero()) & 63;
+    const unsigned long long later = __builtin_amdgcn_ballot_w64(base + S.upto[lane] > at);
+    if (later == 0ull) {
+      base = uniform(base + S.upto[63]);
+      if (++k >= batches) break;
+      load_requests<K>(P, S, k);
+      continue;
+    }
+    const int i = __ffsll(later) - 1;
+    LatentPiece J;
+    J.b = 64 * k + i;
+    J.ctx = __builtin_amdgcn_readfirstlane(S.ctx[i]);
+    J.first = __builtin_amdgcn_readfirstlane(S.first[i]);
+    J.n = __builtin_amdgcn_readfirstlane(S.n[i]);
+    const int rows = J.n * P.H, groups = (rows + M - 1) / M, tiles = tiles_of<T>(P, J.ctx, J.n);
+    const double cost = K::kHead + tiles, start0 = base + S.upto[i] - groups * cost;
+    int grp = 0;                                                // the group that `at` lies in
+    if (groups > 1) {
+      grp = min(max(static_cast<int>((at - start0) / cost), 0), groups - 1);
+      if (start0 + grp * cost > at) --grp;
+      else if (start0 + (grp + 1) * cost <= at) ++grp;
+    }
+    const double start = start0 + grp * cost;
+    // tile k is at start + kHead + k and belongs to the range that this is in
+    auto tile_at = [&](double x) { return static_cast<int>(fmin(fmax(border<K>(x, start, start + cost) - start - K::kHead, 0.0), static_cast<double>(tiles))); };
+    J.t0 = __builtin_amdgcn_readfirstlane(tile_at(at));
+    J.t1 = __builtin_amdgcn_readfirstlane(tile_at(end));
+    at = uniform(start + cost);
+    if (J.t0 >= J.t1) continue;
+    J.row_base = __builtin_amdgcn_readfirstlane(M * grp);
+    J.rows = min(rows - J.row_base, M);
+    J.whole = J.t0 == 0 && J.t1 == tiles;
+    J.part = (static_cast<int64_t>(range) * 2 + (J.t0 == 0 ? 1 : 0)) * M;
+    if (!J.whole && J.t0 == 0 && threadIdx.x == 0) {
+      const LaCut again = {used, S.each, S.total};
+      int last = range_of(again, start + cost - 1);
+      while (border<K>(range_start(again, last), start, start + cost) == start + cost) --last;
+      const int64_t row0 = static_cast<int64_t>(J.first) * P.H + J.row_base;
+      P.cut[blockIdx.x] = make_int4(static_cast<int>(row0 & 0xffffffff), static_cast<int>(row0 >> 32), J.rows << 16 | (last - range + 1), range);
+    }
+    if constexpr (K::kWide) latent_piece_wide<K>(P, S, J);
+    else latent_piece<K>(P, S, J);
+  }
 }
 
-// Merges the partial results of the groups that were cut: a wave takes a row.
+// Merges the partial results of the groups that were cut, piece by piece in their order.  Every workgroup works out which rows there are, and takes its share: four
+// rows at a time, a wave each, or, of many pieces, one, whose pieces the waves share.
+constexpr int kLaMergers = 2048;               // workgroups
+constexpr int kLaFew = 8;                      // pieces
 template <int C>
 __global__ __launch_bounds__(kLaThreads) void merge_latent_kernel(LatentAttnParams P, int M) {
-  const int4 record = P.cut[blockIdx.x];
-  const int pieces = record.z & 0xffff, rows = record.z >> 16;
-  const int lane = threadIdx.x & 63, r = __builtin_amdgcn_readfirstlane(blockIdx.y * kLaWaves + (threadIdx.x >> 6));
-  if (r >= rows || pieces == 0) return;
-  const int64_t row = (static_cast<int64_t>(record.y) << 32 | static_cast<unsigned>(record.x)) + r;
-  auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
-  float m = -INFINITY;
-  for (int i = 0; i < pieces; ++i) m = fmaxf(m, P.ws_ml[part(i)].x);
-  constexpr int E = C / kWave;
-  float sum[E], Z = 0.f;
+  constexpr int E = C / kWave, kFly = 8;
+  __shared__ int upto[kLaRanges];
+  __shared__ int4 records[kLaRanges];
+  __shared__ float shared_sum[kLaWaves - 1][C], shared_z[kLaWaves - 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  static_assert(kLaRanges == kLaThreads, "a thread for each record");
+  auto units_of = [](const int4& r) { const int rows = r.z >> 16, pieces = r.z & 0xffff; return pieces == 0 ? 0 : pieces <= kLaFew ? (rows + kLaWaves - 1) / kLaWaves : rows; };
+  {
+    const int4 r = tid < P.ranges ? P.cut[tid] : make_int4(0, 0, 0, 0);
+    records[tid] = r;
+    const double sum = wave_scan(static_cast<double>(units_of(r)));
+    upto[tid] = static_cast<int>(sum);
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < wave; ++w) before += upto[64 * w + 63];
+    __syncthreads();
+    upto[tid] += before;
+    __syncthreads();
+  }
+  const int total = upto[kLaRanges - 1];
+  for (int u = blockIdx.x; u < total; u += gridDim.x) {
+    int k = 0;                                                  // the record that unit u is of
 #pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] = 0.f;
-  for (int i = 0; i < pieces; ++i) {
-    const float2 ml = P.ws_ml[part(i)];
-    const float share = ml.x == -INFINITY ? 0.f : ml.y * fast_exp2(ml.x - m);
-    Z += share;
+    for (int w = 0; w < kLaRanges / kWave; ++w) k += __popcll(__builtin_amdgcn_ballot_w64(upto[64 * w + lane] <= u));
+    const int4 record = records[k];
+    const int pieces = record.z & 0xffff, rows = record.z >> 16, unit = u - (k > 0 ? upto[k - 1] : 0);
+    const bool few = pieces <= kLaFew;
+    const int r = few ? unit * kLaWaves + wave : unit;
+    auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
+    float m = -INFINITY, sum[E], Z = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = 0.f;
+    if (r < rows) {
+      for (int i = lane; i < pieces; i += kWave) m = fmaxf(m, P.ws_ml[part(i)].x);
+      m = wave_max(m);
+      const int step = few ? 1 : kLaWaves;
+      for (int i0 = few ? 0 : wave; i0 < pieces; i0 += kFly * step) {
+        float2 ml[kFly];
+        float4 x[kFly][E / 4];
+#pragma unroll
+        for (int f = 0; f < kFly; ++f) {
+          const int64_t at = part(min(i0 + f * step, pieces - 1));
+          ml[f] = P.ws_ml[at];
+#pragma unroll
+          for (int e = 0; e < E / 4; ++e) x[f][e] = *reinterpret_cast<const float4*>(P.ws_o + at * C + e * 4 * kWave + 4 * lane);
+        }
+#pragma unroll
+        for (int f = 0; f < kFly; ++f) {
+          const float share = i0 + f * step >= pieces || ml[f].x == -INFINITY ? 0.f : ml[f].y * fast_exp2(ml[f].x - m);
+          Z += share;
+#pragma unroll
+          for (int e = 0; e < E / 4; ++e) {
+            sum[4 * e] = fmaf(x[f][e].x, share, sum[4 * e]); sum[4 * e + 1] = fmaf(x[f][e].y, share, sum[4 * e + 1]);
+            sum[4 * e + 2] = fmaf(x[f][e].z, share, sum[4 * e + 2]); sum[4 * e + 3] = fmaf(x[f][e].w, share, sum[4 * e + 3]);
+          }
+        }
+      }
+    }
+    if (!few) {
+      __syncthreads();                                          // (what was there has been read)
+      if (wave > 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) shared_sum[wave - 1][e * kWave + lane] = sum[e];
+        if (lane == 0) shared_z[wave - 1] = Z;
+      }
+      __syncthreads();
+      if (wave > 0) continue;
+#pragma unroll
+      for (int w = 0; w < kLaWaves - 1; ++w) {
+        Z += shared_z[w];
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += shared_sum[w][e * kWave + lane];
+      }
+    }
+    if (r >= rows) continue;
+    const int64_t row = (static_cast<int64_t>(record.y) << 32 | static_cast<unsigned>(record.x)) + r;
+    const float f = Z == 0.f ? 0.f : 1.f / Z;
 #pragma unroll
     for (int e = 0; e < E; e += 4) {
-      const float4 x = *reinterpret_cast<const float4*>(P.ws_o + part(i) * C + e * kWave + 4 * lane);
-      sum[e] += x.x * share; sum[e + 1] += x.y * share; sum[e + 2] += x.z * share; sum[e + 3] += x.w * share;
+      const lf32x4 x = {sum[e] * f, sum[e + 1] * f, sum[e + 2] * f, sum[e + 3] * f};
+      const int64_t to = row * C + e * kWave + 4 * lane;
+      if (P.out_f32) *reinterpret_cast<float4*>(static_cast<float*>(P.out) + to) = make_float4(x[0], x[1], x[2], x[3]);
+      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + to) = pack4(x);
     }
+    if (P.lse && lane == 0) P.lse[row] = (m + log2f(Z)) * static_cast<float>(kLn2);
   }
-  const float f = Z == 0.f ? 0.f : 1.f / Z;
-#pragma unroll
-  for (int e = 0; e < E; e += 4) {
-    const lf32x4 x = {sum[e] * f, sum[e + 1] * f, sum[e + 2] * f, sum[e + 3] * f};
-    const int64_t to = row * C + e * kWave + 4 * lane;
-    if (P.out_f32) *reinterpret_cast<float4*>(static_cast<float*>(P.out) + to) = make_float4(x[0], x[1], x[2], x[3]);
-    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + to) = pack4(x);
-  }
-  if (P.lse && lane == 0) P.lse[row] = (m + log2f(Z)) * static_cast<float>(kLn2);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
 LatentAttnPlan make_latent_attn_plan(const LatentArgs& a) {
   LatentAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * a.H;
-  const int most = a.out_dtype == kF32 ? 64 : 128;
-  p.rows = 16;
-  while (p.rows < most && p.rows < rows) p.rows *= 2;
+  // 128 rows: the least to do for all together, but 30 us for the smallest batch.  Fewer, in as many more groups, where there is little to do, by the number of
+  // groups of 16 rows x 64 tokens if all requests had all their pages (bf16, C = 512; 16, 32, 128 rows): 64: 17, 22, 31 us; 2048: 32, 33, 41 us; 4096: 48, 42, 51 us;
+  // 8192: 73, 60, 62 us; 16384: 127, 102, 87 us.  (Three terms of 32 rows' weights, for tiles of 64 tokens, are too much for LDS: no fp32 there.)
+  const int64_t small = static_cast<int64_t>(a.B) * ((rows + 15) / 16) * ((static_cast<int64_t>(a.max_pages) + 3) / 4);
+  p.rows = rows <= 16 || small <= 2048 ? 16 : a.out_dtype == kBF16 && (rows <= 32 || small <= 6144) ? 32 : 128;
   p.groups = static_cast<int>((rows + p.rows - 1) / p.rows);
-  const int64_t tiles = static_cast<int64_t>(a.B) * p.groups * (static_cast<int64_t>(a.max_pages) + kLaHead);
+  const int64_t tiles = static_cast<int64_t>(a.B) * p.groups * static_cast<int64_t>(a.max_pages);
   p.ranges = static_cast<int>(std::min<int64_t>(kLaRanges, (tiles + 7) / 8 * 8));
   return p;
 }
@@ -616,24 +1204,18 @@ static int launch_latent(const LatentAttnParams& P, const LatentAttnPlan& p, hip
   static_assert(lds <= 160 * 1024, "");
   if (lds > 65536 && set_lds_once(attn_latent_kernel<K>, lds, lds_set) != 0) return -6;
   hipLaunchKernelGGL(attn_latent_kernel<K>, dim3(p.ranges), dim3(kLaThreads), lds, stream, P);
-  hipLaunchKernelGGL(merge_latent_kernel<K::C>, dim3(p.ranges, (p.rows + kLaWaves - 1) / kLaWaves), dim3(kLaThreads), 0, stream, P, p.rows);
+  hipLaunchKernelGGL(merge_latent_kernel<K::C>, dim3(static_cast<unsigned>(std::min<int64_t>(kLaMergers, static_cast<int64_t>(p.ranges) * p.rows / 2))), dim3(kLaThreads), 0, stream, P, p.rows);
   return 0;
 }
 template <int C, int R>
 static int launch_latent_rows(const LatentAttnParams& P, const LatentAttnPlan& p, hipStream_t stream) {
   if (P.out_f32) {
-    switch (p.rows) {
-      case 16: return launch_latent<LatentConfig<C, R, 1, 1, 1, 3>>(P, p, stream);
-      case 32: return launch_latent<LatentConfig<C, R, 2, 1, 1, 3>>(P, p, stream);
-      default: return launch_latent<LatentConfig<C, R, 2, 2, 1, 3>>(P, p, stream);
-    }
+    if (p.rows == 16) return launch_latent<LatentNarrow<C, R, 1, 3>>(P, p, stream);
+    return launch_latent<LatentWide<C, R, 3>>(P, p, stream);
   }
-  switch (p.rows) {
-    case 16: return launch_latent<LatentConfig<C, R, 1, 1, 1, 1>>(P, p, stream);
-    case 32: return launch_latent<LatentConfig<C, R, 2, 1, 1, 1>>(P, p, stream);
-    case 64: return launch_latent<LatentConfig<C, R, 2, 2, 1, 1>>(P, p, stream);
-    default: return launch_latent<LatentConfig<C, R, 2, 4, 2, 1>>(P, p, stream);
-  }
+  if (p.rows == 16) return launch_latent<LatentNarrow<C, R, 1, 1>>(P, p, stream);
+  if (p.rows == 32) return launch_latent<LatentNarrow<C, R, 2, 1>>(P, p, stream);
+  return launch_latent<LatentWide<C, R, 1>>(P, p, stream);
 }
 
 int launch_attn_latent(const LatentArgs& a, const void* q, const void* pool, void* out, float* lse, void* workspace, const LatentAttnPlan& p,

@@ -11,6 +11,7 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 lbf16x8;
 typedef __bf16 lbf16x2 __attribute__((ext_vector_type(2)));
 typedef short ls16x4 __attribute__((ext_vector_type(4)));
 typedef float lf32x4 __attribute__((ext_vector_type(4)));
+typedef float lf32x16 __attribute__((ext_vector_type(16)));
 
 template <typename T>
 __device__ __forceinline__ __attribute__((address_space(3))) T* lds_pointer(unsigned at) {

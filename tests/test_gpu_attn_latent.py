@@ -28,9 +28,26 @@ def lib():
     binding.lib()
 
 
+class Device(U.Device):
+    """With the block table widened, by columns that hold no pages, until there is more to be done for every request than `least` groups of 16 rows x 64
+    tokens: the kernels of 16, 32 and 128 rows."""
+    least = 0
+
+    def __init__(self, c, **more):
+        groups = len(c["ctx"]) * -(-int(c["n"].max()) * c["H"] // 16)
+        columns = 4 * (self.least // groups + 1) if self.least else 0
+        spare = np.full((len(c["ctx"]), max(0, columns - c["table"].shape[1])), -1, dtype=np.int32)
+        super().__init__(dict(c, table=np.concatenate([c["table"], spare], 1)), **more)
+
+
+@pytest.fixture(params=[0, 2048, 6144], ids=lambda least: f"above{least}", autouse=True)
+def least(request, monkeypatch):
+    monkeypatch.setattr(Device, "least", request.param)
+
+
 def ratio(c, f32=False, softmax=0.0, pool=None):
     """The largest error by its bound, of results and of log-sum-exp; rows that see nothing and rows behind are checked for what they have to be."""
-    d = U.Device(c, f32=f32, softmax=softmax)
+    d = Device(c, f32=f32, softmax=softmax)
     out, lse = (U.host(x) for x in d.attend())
     ref, ref_lse, size, A, L = R.attend(c, c["ql"], c["pool"] if pool is None else pool, c["C"], softmax or c["softmax"])
     m = c["total"]
@@ -148,10 +165,10 @@ def test_a_draft_that_is_not_finite(bad, H):
     _, sees = R.visible(c, 0, c["held"])
     hit = sees[:, at]
     assert hit[node] and not hit[:node].any()
-    d = U.Device(c)
+    d = Device(c)
     out, lse = (U.host(x) for x in d.attend())
     assert np.all(np.isnan(out[hit])) and not np.isnan(out[~hit]).any() and not np.isnan(lse[~hit]).any()
-    e = U.Device(dict(c, pool=clean))
+    e = Device(dict(c, pool=clean))
     want, want_lse = (U.host(x) for x in e.attend())
     assert np.array_equal(out[~hit], want[~hit]) and np.array_equal(lse[~hit], want_lse[~hit])
 
@@ -159,7 +176,7 @@ def test_a_draft_that_is_not_finite(bad, H):
 def test_a_query_that_is_not_finite_stays_alone():
     c = U.batch(32, ctx=[100], n=[3], H=50)
     c["ql"][1, 7, 3], c["ql"][2, 0, 570] = np.nan, np.inf
-    out = U.host(U.Device(c).attend()[0])
+    out = U.host(Device(c).attend()[0])
     bad = np.isnan(out).any(-1)
     assert bad[1, 7] and bad[2, 0] and bad.sum() == 2
 
@@ -167,12 +184,12 @@ def test_a_query_that_is_not_finite_stays_alone():
 def test_a_context_entry_that_is_not_finite():
     c = U.batch(33, ctx=[100], n=[2], H=3)
     c["pool"][c["table"][0, 1], 3, 7] = np.nan
-    assert np.all(np.isnan(U.host(U.Device(c).attend()[0])))
+    assert np.all(np.isnan(U.host(Device(c).attend()[0])))
 
 
 def test_without_lse_and_twice_the_same():
     c = U.batch(34, ctx=[3000, 64, 900], n=[3, 1, 2], H=16)
-    d = U.Device(c)
+    d = Device(c)
     a = d.attend()[0].clone()
     d.lse.fill_(7.0)
     d.workspace.fill_(0x3c)
