@@ -109,25 +109,25 @@ __device__ __forceinline__ double border(double at, double start, double end) {
   return at > end - K::kSnap ? end : at;
 }
 
-// Up to 16 NB rows: every wave takes a quarter of a tile's tokens for the scores.
+// Up to 16 NB rows, NB 1, 2 or 4.  Of the scores a wave takes 16 rows, by half of a tile's tokens (NB 1: two waves have none) or, NB 4, by all.
 template <int C_, int R_, int NB_, int TERMS_>
 struct LatentNarrow {
   static constexpr bool kWide = false;
   static constexpr int C = C_, R = R_, NB = NB_, TERMS = TERMS_;
   static constexpr int W = C + R;
-  static constexpr int kHead = 3, kSnap = 1, kLeast = 2;      // see Cut
-  static constexpr int M = 16 * NB, T = 64, WK = kLaWaves;
+  static constexpr int kHead = 6, kSnap = 2, kLeast = 4;       // see LaCut
+  static constexpr int M = 16 * NB, T = 32, KB = NB == 4 ? 2 : 1, WK = 2 / KB;      // blocks of 16 tokens of a wave; waves that share a row
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;            // 16-byte units of a row in LDS
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
   static constexpr int kPages = T / kLaPage;
-  static constexpr int RB = M / 16, CB = C / 4 / 16;            // 16-row blocks; 16-column blocks of a wave
+  static constexpr int RB = NB, CB = C / 4 / 16;                // 16-row blocks; 16-column blocks of a wave
   static constexpr int kSteps = W / 32;
   static constexpr int kLoads = kTile / kLaWaves / 1024;        // of a wave for a tile
   static constexpr int kOffsets = 8 * kRow / 1024;              // loads that bring 8 rows
-  static constexpr int kWeights = TERMS * (T / 32) * RB * 1024, kBuffers = 1;
+  static constexpr int kWeights = TERMS * RB * 1024, kBuffers = 1;
   static constexpr int kSmall = kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 + 4 + 80;
-  static constexpr int kStages = std::min(4, (160 * 1024 - kSmall) / kTile);
-  static_assert(kStages >= 2 && kRow % 256 == 128, "");
+  static constexpr int kStages = std::min(6, (160 * 1024 - kSmall) / kTile);
+  static_assert(kStages >= 3 && kRow % 256 == 128 && kLoads == kOffsets, "");
 };
 // Up to 128 rows: every wave takes 32 of them for the scores.
 template <int C_, int R_, int TERMS_>
@@ -135,7 +135,7 @@ struct LatentWide {
   static constexpr bool kWide = true;
   static constexpr int C = C_, R = R_, TERMS = TERMS_;
   static constexpr int W = C + R;
-  static constexpr int kHead = 12, kSnap = 4, kLeast = 4;      // see Cut
+  static constexpr int kHead = 12, kSnap = 4, kLeast = 4;      // see LaCut
   static constexpr int M = 128, T = 32, WK = 1;
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
@@ -261,17 +261,15 @@ __device__ __forceinline__ void take_out(unsigned tile, int tid) {
 
 template <typename K>
 __device__ __forceinline__ void write_results(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J, lf32x4 (&o)[K::CB][K::RB],
-                                              const float (&ref)[K::NB], const float (&sum)[K::NB], int wave, int lane) {
-  constexpr int NB = K::NB, WK = K::WK, RB = K::RB, CB = K::CB;
+                                              float ref, float sum, int wave, int lane) {
+  constexpr int WK = K::WK, RB = K::RB, CB = K::CB;
   const int tid = threadIdx.x, rn = lane & 15, g = lane >> 4;
   lds_sync();                                                   // (S.by has been read)
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const float z = groups_sum(sum[nb]);
-    if (lane < 16) {
-      S.sum[wave][16 * nb + lane] = z;
-      if (wave == 0) S.by[0][16 * nb + lane] = ref[nb];
-    }
+  const float z = groups_sum(sum);
+  const int block = K::NB == 4 ? wave : wave >> 1, part = K::NB == 4 ? 0 : wave & 1;
+  if (block < K::NB && lane < 16) {
+    S.sum[part][16 * block + lane] = z;
+    if (part == 0) S.by[0][16 * block + lane] = ref;
   }
   lds_sync();
   auto row_sum = [&](int row) __attribute__((always_inline)) {
@@ -779,89 +777,75 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
   write_results_wide<K>(P, S, J, o);
 }
 
+// Up to 64 query rows: memory bounds it.  Three tiles or more are on their way while one is worked on, in turn: scores, weights to LDS, results.
 template <typename K>
 __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J) {
-  constexpr int W = K::W, T = K::T, NB = K::NB, WK = K::WK, RB = K::RB, CB = K::CB, kPages = K::kPages, NS = K::kStages;
+  constexpr int W = K::W, T = K::T, KB = K::KB, WK = K::WK, RB = K::RB, CB = K::CB, kPages = K::kPages, NS = K::kStages, TERMS = K::TERMS;
   const int tid = static_cast<int>(threadIdx.x) + opaque_zero(), lane = tid & 63;
   __builtin_assume(tid >= 0 && tid < kLaThreads);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rn = lane & 15, g = lane >> 4;
+  const int block = K::NB == 4 ? wave : wave >> 1, part = K::NB == 4 ? 0 : wave & 1;      // of the scores: this wave's rows 16 block .., tokens 16 part ..
+  const bool scores = block < K::NB;
   const int L = J.ctx + J.n;
 
   unsigned off[K::kOffsets];
   tile_offsets<K>(off, lane);
+#pragma unroll
+  for (int j = 0; j < K::kOffsets; ++j) off[j] ^= 16 * (wave & 1);
   constexpr int64_t kPageBytes = kLaPage * W * 2;
-  const const_i32* bt = (const const_i32*)(P.block_table + static_cast<int64_t>(J.b) * P.max_pages);
+  const int32_t* bt = P.block_table + static_cast<int64_t>(J.b) * P.max_pages;
   const int last_page = min((L - 1) / kLaPage, P.max_pages - 1);
   const unsigned ring = lds_address(&S.ring[0][0]);
-  const int my_page = kPages == 4 ? wave : wave >> 1;           // of a tile's pages: the one that this wave brings (half of)
-  int ids[kPages], my_id = 0;
+  const unsigned char* const pool = reinterpret_cast<const unsigned char*>(P.pool) + (wave & 1) * 8 * W * 2;      // this wave's half of its page
+  // page ids of 32 tiles at a time, a lane each (through the scalar cache they would have every read of LDS waited for alike).  -1: none
+  int ids = -1;
   auto fetch_ids = [&](int t) __attribute__((always_inline)) {
-    if (t < J.t1) {
-#pragma unroll
-      for (int i = 0; i < kPages; ++i) {
-        const int lp = kPages * t + i, id = bt[min(lp, last_page)];
-        ids[i] = id >= 0 && id < P.num_pages && lp < P.max_pages ? id : -1;
-      }
-      my_id = bt[min(kPages * t + my_page, last_page)];
-      my_id = my_id >= 0 && my_id < P.num_pages ? my_id : 0;
-    }
+    const int lp = kPages * t + lane, id = bt[min(lp, last_page)];
+    ids = id >= 0 && id < P.num_pages && lp < P.max_pages ? id : -1;
   };
-  auto bad_pages = [&]() __attribute__((always_inline)) {
-    unsigned bad = 0u;
-#pragma unroll
-    for (int i = 0; i < kPages; ++i) bad |= ids[i] < 0 ? 1u << i : 0u;
-    return bad;
+  unsigned bad = 0u;                                            // pages that are none: 2 bits a tile, the present one's lowest
+  const unsigned char* page = pool;
+  unsigned to = 0;
+  auto aim = [&](int t, int slot, int ahead) __attribute__((always_inline)) {
+    const int at = (kPages * (t - J.t0)) & 63;
+    if (at == 0) fetch_ids(t);
+    const int a = __builtin_amdgcn_readlane(ids, at), b = __builtin_amdgcn_readlane(ids, at + 1);
+    bad |= ((a < 0 ? 1u : 0u) | (b < 0 ? 2u : 0u)) << (kPages * ahead);
+    page = pool + max(wave < 2 ? a : b, 0) * kPageBytes;        // (one that is none of the pool's: page 0 in its place)
+    to = ring + slot * K::kTile + wave * (K::kTile / kLaWaves);
   };
-  // (a page that is none of the pool's: page 0 in its place)
-  auto issue = [&](int slot) __attribute__((always_inline)) {
-    const unsigned to = ring + slot * K::kTile + wave * (K::kTile / kLaWaves);
-    const unsigned char* page = reinterpret_cast<const unsigned char*>(P.pool) + __builtin_amdgcn_readfirstlane(my_id) * kPageBytes + (kPages == 4 ? 0 : (wave & 1) * 8 * W * 2);
-#pragma unroll
-    for (int j = 0; j < K::kLoads; ++j) load_to_lds(page + j / K::kOffsets * 8 * W * 2, j < K::kOffsets ? off[j] : off[j - K::kOffsets] ^ 16, to + 1024 * j, 0);
-  };
-  unsigned long long bad = 0ull;                                // pages that are none: kPages bits a tile, the present one's lowest
+  auto issue = [&](int j) __attribute__((always_inline)) { load_to_lds(page, off[j], to + 1024 * j, 0); };
 
   // ---- the queries' operands: rows past the last repeat it ----
-  lbf16x8 qf[NB][K::kSteps];
+  lbf16x8 qf[K::kSteps];
   {
-    const uint16_t* q = P.q + (static_cast<int64_t>(J.first) * P.H + J.row_base) * W + 8 * g;
+    const uint16_t* row = P.q + (static_cast<int64_t>(J.first) * P.H + J.row_base + min(16 * block + rn, J.rows - 1)) * W + 8 * g;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const uint16_t* row = q + static_cast<int64_t>(min(16 * nb + rn, J.rows - 1)) * W;
-#pragma unroll
-      for (int s = 0; s < K::kSteps; ++s) qf[nb][s] = operand(*reinterpret_cast<const raw4*>(row + 32 * s));
-    }
+    for (int s = 0; s < K::kSteps; ++s) qf[s] = operand(*reinterpret_cast<const raw4*>(row + 32 * s));
   }
   const bool touches_drafts = J.t1 * static_cast<int64_t>(T) > J.ctx;
   int parent = -1;
   if (touches_drafts && P.parent && tid < J.n) parent = P.parent[J.first + tid];
   lds_sync();                                                   // the LDS of the piece before is free
-  fetch_ids(J.t0);
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i) {
-    if (J.t0 + i < J.t1) {
-      bad |= static_cast<unsigned long long>(bad_pages()) << (kPages * i);
-      issue(i);
-      fetch_ids(J.t0 + i + 1);
-    }
+    if (J.t0 + i >= J.t1) break;
+    aim(J.t0 + i, i, i);
+#pragma unroll
+    for (int j = 0; j < K::kLoads; ++j) issue(j);
   }
   if (touches_drafts) find_lineage<K>(P, S, J, tid, parent);
 
-  // Operand reads: K, token 16 wave + rn, unit 4 s + g; V by columns, token 4 g + rn / 4 (and 16 more), unit 4 (cb / 2) + rn % 4, half cb % 2: column
+  // Operand reads: K, token 16 part + rn, unit 4 s + g; V by columns, token 4 g + rn / 4 (and 16 more), unit 4 (cb / 2) + rn % 4, half cb % 2: column
   // 32 p + 8 g + 4 s + i of the wave's is row 4 g + i of block 2 p + s, so that a lane ends up with 8 consecutive ones
-  const unsigned k_at = (16 * wave + rn) * K::kRow + (g ^ fold(rn)) * 16;             // even steps; odd ones at ^ 64; 128 more every two
+  const unsigned k_at = (16 * part + rn) * K::kRow + (g ^ fold(rn)) * 16;           // even steps; odd ones at ^ 64; 128 more every two
   const int vt = 4 * g + (rn >> 2);
   const unsigned v_at = vt * K::kRow + ((rn & 3) ^ fold(vt)) * 16 + wave * (K::C / 4 * 2);   // even pairs of blocks; odd ones at ^ 64; 128 more every two
-  const unsigned p_at = lds_address(&S.p[0][0]);
+  const unsigned p_at = lds_address(&S.p[0][0]) + 16 * lane;
 
-  float ref[NB], sum[NB];
+  float ref = kLaNoScore, sum = 0.f;
   lf32x4 o[CB][RB];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    ref[nb] = kLaNoScore;
-    sum[nb] = 0.f;
-  }
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -871,107 +855,108 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
   for (int t = J.t0; t < J.t1; ++t) {
     // ---- the tile is here, and all waves are done with the one before ----
     const int more = J.t1 - 1 - t;
-    if constexpr (NS >= 4) {
-      if (more >= 2) wait_loads<2 * K::kLoads>();
-    }
-    if constexpr (NS >= 3) {
-      if (more == 1 || (NS == 3 && more > 1)) wait_loads<K::kLoads>();
-    }
-    if (NS == 2 || more == 0) wait_loads<0>();
+    if (more >= NS - 2) wait_loads<(NS - 2) * K::kLoads>();
+    else if (NS >= 5 && more == 2) wait_loads<2 * K::kLoads>();
+    else if (NS >= 6 && more == 3) wait_loads<3 * K::kLoads>();
+    else if (NS >= 4 && more == 1) wait_loads<K::kLoads>();
+    else wait_loads<0>();
     lds_sync();
-    if (t + NS - 1 < J.t1) {
-      bad |= static_cast<unsigned long long>(bad_pages()) << (kPages * (NS - 1));
-      issue(slot == 0 ? NS - 1 : slot - 1);
-      fetch_ids(t + NS);
-    }
+    const bool another = t + NS - 1 < J.t1;
+    if (another) aim(t + NS - 1, slot == 0 ? NS - 1 : slot - 1, NS - 1);
     const unsigned tile = ring + slot * K::kTile;
+    const bool special = (t + 1) * static_cast<int64_t>(T) > J.ctx || (bad & 3u) != 0u;
 
     // ---- scores ----
-    lf32x4 s[NB];
-#pragma unroll
-    for (int step = 0; step < K::kSteps; ++step) {
-      const lbf16x8 k = operand(read_lds16(((tile + k_at) ^ (64 * (step & 1))) + 128 * (step >> 1)));
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) s[nb] = multiply(k, qf[nb][step], step == 0 ? lf32x4{0.f, 0.f, 0.f, 0.f} : s[nb]);
-      if (step % 4 == 3) __builtin_amdgcn_sched_barrier(0);     // (else all of K is read first, into registers there are none of)
-    }
-
-    // ---- masks: only where the tile reaches the drafts, or a page is none ----
-    const bool special = (t + 1) * static_cast<int64_t>(T) > J.ctx || (bad & ((1u << kPages) - 1u)) != 0ull;
-    if (special) {
-      const int64_t past = static_cast<int64_t>(t) * T + 16 * wave - J.ctx;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        uint32_t seen = 0xffffu;
-        if (past > -16) {
-          const int node = S.node[16 * nb + rn];
-          seen = page_mask(S.anc[node][0], S.anc[node][1], static_cast<int>(past));
-        }
-        seen = (bad >> wave) & 1ull ? 0u : seen >> (4 * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[nb][i] = (seen >> i) & 1u ? s[nb][i] : -INFINITY;
-      }
-    }
-
-    // ---- weights ----
-    float top[NB], z[NB];
-    bool ahead = false;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      top[nb] = __builtin_elementwise_maximum(max3(s[nb][0], s[nb][1], s[nb][2]), s[nb][3]) * P.c;
-      ahead |= top[nb] > ref[nb] + kLaSlack;
-    }
+    lf32x4 s[KB];
+    float top = -INFINITY, z = 0.f;
     auto weigh = [&]() __attribute__((always_inline)) {
+      uint32_t w[TERMS][KB][2];
+      z = 0.f;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        z[nb] = 0.f;
-        uint32_t w[K::TERMS][2];
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float p0 = fast_exp2(fmaf(s[nb][2 * i], P.c, -ref[nb])), p1 = fast_exp2(fmaf(s[nb][2 * i + 1], P.c, -ref[nb]));
-          z[nb] += p0 + p1;
+          const float p0 = fast_exp2(fmaf(s[kb][2 * i], P.c, -ref)), p1 = fast_exp2(fmaf(s[kb][2 * i + 1], P.c, -ref));
+          z += p0 + p1;
           float r0 = p0, r1 = p1;
 #pragma unroll
-          for (int term = 0; term < K::TERMS; ++term) {
-            w[term][i] = pack2(r0, r1);
-            r0 -= bf16_lo(w[term][i]);
-            r1 -= bf16_hi(w[term][i]);
+          for (int term = 0; term < TERMS; ++term) {
+            w[term][kb][i] = pack2(r0, r1);
+            r0 -= bf16_lo(w[term][kb][i]);
+            r1 -= bf16_hi(w[term][kb][i]);
           }
         }
-        // blocks of 16 tokens 2 m and 2 m + 1 are the halves of a lane's 16 bytes
+      // the two blocks of 16 tokens are the halves of a lane's 16 bytes
 #pragma unroll
-        for (int term = 0; term < K::TERMS; ++term) {
-          const unsigned at = p_at + (term * (T / 32) * RB + nb) * 1024 + 16 * lane;
-          *lds_pointer<unsigned long long>(at + (wave >> 1) * RB * 1024 + 8 * (wave & 1)) = static_cast<unsigned long long>(w[term][1]) << 32 | w[term][0];
-        }
+      for (int term = 0; term < TERMS; ++term) {
+        const unsigned at = p_at + (term * RB + block) * 1024;
+        if constexpr (KB == 1) *lds_pointer<unsigned long long>(at + 8 * part) = static_cast<unsigned long long>(w[term][0][1]) << 32 | w[term][0][0];
+        else *lds_pointer<raw4>(at) = raw4{w[term][0][0], w[term][0][1], w[term][1][0], w[term][1][1]};
       }
     };
-    weigh();
-    const unsigned flag = any_lane(ahead) ? 1u : 0u;
+    if (scores) {
+      // (K is read ahead, and the loads of a tile lie between the products: all at once they wait for each other)
+      constexpr int kDeep = 8;
+      lbf16x8 k[kDeep][KB];
+      auto read_k = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) k[step % kDeep][kb] = operand(read_lds16(((tile + k_at) ^ (64 * (step & 1))) + 128 * (step >> 1) + kb * 16 * K::kRow));
+      };
+#pragma unroll
+      for (int step = 0; step < kDeep - 1; ++step) read_k(step);
+#pragma unroll
+      for (int step = 0; step < K::kSteps; ++step) {
+        if (step + kDeep - 1 < K::kSteps) read_k(step + kDeep - 1);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s[kb] = multiply(k[step % kDeep][kb], qf[step], step == 0 ? lf32x4{0.f, 0.f, 0.f, 0.f} : s[kb]);
+        if (another && step % 2 == 0 && step / 2 < K::kLoads) issue(step / 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // masks: only where the tile reaches the drafts, or a page is none
+      if (special) {
+        const int node = S.node[16 * block + rn];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const int page = part + kb;
+          const int64_t past = static_cast<int64_t>(t) * T + 16 * page - J.ctx;
+          uint32_t seen = 0xffffu;
+          if (past > -16) seen = page_mask(S.anc[node][0], S.anc[node][1], static_cast<int>(past));
+          seen = (bad >> page) & 1u ? 0u : seen >> (4 * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[kb][i] = (seen >> i) & 1u ? s[kb][i] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) top = max3(top, max3(s[kb][0], s[kb][1], s[kb][2]), s[kb][3]);
+      top *= P.c;
+      weigh();
+    } else if (another) {
+#pragma unroll
+      for (int j = 0; j < K::kLoads; ++j) issue(j);
+    }
+    const unsigned flag = any_lane(top > ref + kLaSlack) ? 1u : 0u;
     if (lane == 0) S.ahead[0][wave] = flag;
     lds_sync();
     const raw4 flags = *reinterpret_cast<const raw4*>(S.ahead[0]);
     if (__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3])) {
       // ---- a row's reference follows its maximum where that has come far ahead (in all waves, or in none) ----
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const float m = groups_max(top[nb]);
-        if (lane < 16) S.top[wave][16 * nb + lane] = m;
+      if (scores) {
+        const float m = groups_max(top);
+        if (lane < 16) S.top[part][16 * block + lane] = m;
       }
       lds_sync();
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int row = 16 * nb + rn;
+      if (scores) {
+        const int row = 16 * block + rn;
         float now = S.top[0][row];
 #pragma unroll
         for (int k = 1; k < WK; ++k) now = fmaxf(now, S.top[k][row]);
-        now = now > ref[nb] + kLaSlack ? now : ref[nb];         // (each row by itself: its result has the same bits whatever the others are)
-        const float by = fast_exp2(ref[nb] - now);
-        ref[nb] = now;
-        sum[nb] *= by;
-        if (wave == 0 && lane < 16) S.by[0][row] = by;
+        now = now > ref + kLaSlack ? now : ref;                 // (each row by itself: its result has the same bits whatever the others are)
+        const float by = fast_exp2(ref - now);
+        ref = now;
+        sum *= by;
+        if (part == 0 && lane < 16) S.by[0][row] = by;
+        weigh();
       }
-      weigh();
       lds_sync();
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -980,8 +965,7 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
         for (int cb = 0; cb < CB; ++cb) o[cb][rb] *= by;
       }
     }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) sum[nb] += z[nb];
+    sum += z;
 
     if (special) {
       take_out<K>(tile, tid);
@@ -989,23 +973,19 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     }
 
     // ---- O^T += V^T P^T ----
+    lbf16x8 p[TERMS][RB];
 #pragma unroll
-    for (int m = 0; m < T / 32; ++m) {
-      lbf16x8 p[K::TERMS][RB];
+    for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-      for (int term = 0; term < K::TERMS; ++term)
+      for (int rb = 0; rb < RB; ++rb) p[term][rb] = operand(read_lds16(p_at + (term * RB + rb) * 1024));
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) p[term][rb] = operand(read_lds16(p_at + ((term * (T / 32) + m) * RB + rb) * 1024 + 16 * lane));
+    for (int cb = 0; cb < CB; ++cb) {
+      const unsigned at = ((tile + v_at) ^ (64 * ((cb >> 1) & 1))) + 128 * (cb >> 2) + 8 * (cb & 1);
+      const lbf16x8 v = join(read_columns(at), read_columns(at + 16 * K::kRow));
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        const unsigned at = ((tile + v_at) ^ (64 * ((cb >> 1) & 1))) + 128 * (cb >> 2) + 8 * (cb & 1) + m * 32 * K::kRow;
-        const lbf16x8 v = join(read_columns(at), read_columns(at + 16 * K::kRow));
+      for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-          for (int term = 0; term < K::TERMS; ++term) o[cb][rb] = multiply(v, p[term][rb], o[cb][rb]);
-        }
-        if (cb % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        for (int term = 0; term < TERMS; ++term) o[cb][rb] = multiply(v, p[term][rb], o[cb][rb]);
       }
     }
     bad >>= kPages;
@@ -1181,11 +1161,8 @@ __global__ __launch_bounds__(kLaThreads) void merge_latent_kernel(LatentAttnPara
 LatentAttnPlan make_latent_attn_plan(const LatentArgs& a) {
   LatentAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * a.H;
-  // 128 rows: the least to do for all together, but 30 us for the smallest batch.  Fewer, in as many more groups, where there is little to do, by the number of
-  // groups of 16 rows x 64 tokens if all requests had all their pages (bf16, C = 512; 16, 32, 128 rows): 64: 17, 22, 31 us; 2048: 32, 33, 41 us; 4096: 48, 42, 51 us;
-  // 8192: 73, 60, 62 us; 16384: 127, 102, 87 us.  (Three terms of 32 rows' weights, for tiles of 64 tokens, are too much for LDS: no fp32 there.)
   const int64_t small = static_cast<int64_t>(a.B) * ((rows + 15) / 16) * ((static_cast<int64_t>(a.max_pages) + 3) / 4);
-  p.rows = rows <= 16 || small <= 2048 ? 16 : a.out_dtype == kBF16 && (rows <= 32 || small <= 6144) ? 32 : 128;
+  p.rows = rows <= 16 || small <= 2048 ? 16 : rows <= 32 || small <= 6144 ? 32 : rows <= 64 ? 64 : 128;
   p.groups = static_cast<int>((rows + p.rows - 1) / p.rows);
   const int64_t tiles = static_cast<int64_t>(a.B) * p.groups * static_cast<int64_t>(a.max_pages);
   p.ranges = static_cast<int>(std::min<int64_t>(kLaRanges, (tiles + 7) / 8 * 8));
@@ -1211,10 +1188,13 @@ template <int C, int R>
 static int launch_latent_rows(const LatentAttnParams& P, const LatentAttnPlan& p, hipStream_t stream) {
   if (P.out_f32) {
     if (p.rows == 16) return launch_latent<LatentNarrow<C, R, 1, 3>>(P, p, stream);
+    if (p.rows == 32) return launch_latent<LatentNarrow<C, R, 2, 3>>(P, p, stream);
+    if (p.rows == 64) return launch_latent<LatentNarrow<C, R, 4, 3>>(P, p, stream);
     return launch_latent<LatentWide<C, R, 3>>(P, p, stream);
   }
   if (p.rows == 16) return launch_latent<LatentNarrow<C, R, 1, 1>>(P, p, stream);
   if (p.rows == 32) return launch_latent<LatentNarrow<C, R, 2, 1>>(P, p, stream);
+  if (p.rows == 64) return launch_latent<LatentNarrow<C, R, 4, 1>>(P, p, stream);
   return launch_latent<LatentWide<C, R, 1>>(P, p, stream);
 }
 

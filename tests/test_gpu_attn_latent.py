@@ -30,7 +30,7 @@ def lib():
 
 class Device(U.Device):
     """With the block table widened, by columns that hold no pages, until there is more to be done for every request than `least` groups of 16 rows x 64
-    tokens: the kernels of 16, 32 and 128 rows."""
+    tokens: the kernels of 16, of 32 and of 64 or 128 rows."""
     least = 0
 
     def __init__(self, c, **more):
@@ -75,6 +75,7 @@ CASES = {
     "sixteen_rows": dict(ctx=[5, 31, 64, 100, 0], n=[1, 1, 1, 1, 1], H=16),
     "thirtytwo_rows": dict(ctx=[33, 200, 0, 65], n=[2, 1, 2, 2], H=16),
     "sixtyfour_rows": dict(ctx=[33, 200, 0, 47], n=[3, 5, 1, 4], H=13),
+    "fifty_rows": dict(ctx=[33, 200, 0, 47, 700], n=[3, 5, 1, 4, 2], H=10, tree=True),
     "tree": dict(ctx=[5, 0, 140], n=[9, 64, 33], H=5, tree=True),
     "chain128": dict(ctx=[70], n=[128], H=2),
     "ragged": dict(ctx=[1, 900, 17, 64, 333, 2], n=[3, 1, 10, 2, 5, 7], H=20),
