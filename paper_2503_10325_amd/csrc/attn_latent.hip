@@ -83,7 +83,8 @@ __device__ __forceinline__ int tiles_of(const LatentAttnParams& P, int ctx, int 
 // A number that is the same in all lanes, in scalar registers.
 __device__ __forceinline__ double uniform(double x) { return lane_f64(x, 0); }
 // The groups of all requests end to end, each its kHead (what its start and end cost, in tiles) and its tiles, in `used` ranges of equal length, whole numbers apart,
-// at least kLeast long.  A border that would leave a piece of a group with fewer than kSnap tiles goes to the group's end.
+// at least kLeast long, or twice that where there are more than 64 (one request, 16 heads; 500 tiles: 20.5 us, with kLeast alone 24.5, as there are more to be
+// merged; 9 tiles x 4 groups: 14.8, with twice that 16.6).  A border that would leave a piece of a group with fewer than kSnap tiles goes to the group's end.
 struct LaCut {
   int used;
   double each, total;
@@ -91,7 +92,7 @@ struct LaCut {
 __device__ __forceinline__ LaCut cut_ranges(int most, int least, double total) {
   LaCut c;
   c.total = total;
-  c.used = __builtin_amdgcn_readfirstlane(static_cast<int>(fmin(fmax(total / least, 1.0), static_cast<double>(most))));
+  c.used = __builtin_amdgcn_readfirstlane(static_cast<int>(fmin(fmax(fmax(fmin(total / least, 64.0), total / (2 * least)), 1.0), static_cast<double>(most))));
   c.each = uniform(total / c.used);
   return c;
 }
@@ -115,7 +116,7 @@ struct LatentNarrow {
   static constexpr bool kWide = false;
   static constexpr int C = C_, R = R_, NB = NB_, TERMS = TERMS_;
   static constexpr int W = C + R;
-  static constexpr int kHead = 6, kSnap = 2, kLeast = 4;       // see LaCut
+  static constexpr int kHead = 6, kSnap = 1, kLeast = 2;       // see LaCut
   static constexpr int M = 16 * NB, T = 32, KB = NB == 4 ? 2 : 1, WK = 2 / KB;      // blocks of 16 tokens of a wave; waves that share a row
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;            // 16-byte units of a row in LDS
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
@@ -135,7 +136,7 @@ struct LatentWide {
   static constexpr bool kWide = true;
   static constexpr int C = C_, R = R_, TERMS = TERMS_;
   static constexpr int W = C + R;
-  static constexpr int kHead = 12, kSnap = 4, kLeast = 4;      // see LaCut
+  static constexpr int kHead = TERMS == 1 ? 12 : 5, kSnap = 4, kLeast = 4;      // see LaCut
   static constexpr int M = 128, T = 32, WK = 1;
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
@@ -384,10 +385,19 @@ __device__ __forceinline__ void write_results_wide(const LatentAttnParams& P, La
         }
       }
       lds_sync();
-      for (int u = tid; u < kTogether * 32 * kLanes; u += kLaThreads) {
-        const int r = u / kLanes, c = u % kLanes;
-        if (32 * rb0 + r >= J.rows) break;
-        *reinterpret_cast<raw4*>(to + static_cast<int64_t>(32 * rb0 + r) * kBytes + 16 * c) = read_lds16(ring + r * kApart + 16 * c);
+      // rows r0, r0 + kBy, ..: eight reads of LDS on their way
+      constexpr int kBy = kLaThreads / kLanes, kFly = 8;
+      static_assert(kLaThreads % kLanes == 0 && kTogether * 32 % (kBy * kFly) == 0, "");
+      const int r0 = tid / kLanes, c = tid % kLanes;
+      unsigned char* line = to + static_cast<int64_t>(32 * rb0 + r0) * kBytes + 16 * c;
+      for (int r = 0; r < kTogether * 32 && 32 * rb0 + r < J.rows; r += kBy * kFly) {
+        raw4 x[kFly];
+#pragma unroll
+        for (int i = 0; i < kFly; ++i) x[i] = read_lds16(ring + (r0 + r + i * kBy) * kApart + 16 * c);
+#pragma unroll
+        for (int i = 0; i < kFly; ++i)
+          if (32 * rb0 + r0 + r + i * kBy < J.rows) *reinterpret_cast<raw4*>(line + i * kBy * kBytes) = x[i];
+        line += kBy * kFly * kBytes;
       }
     }
   };
@@ -489,7 +499,8 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
 #pragma unroll
       for (int j = 0; j < K::kLoads; ++j) issue(j);
     }
-    wait_loads<0>();
+    if (J.t0 + NS - 2 <= J.t1) wait_loads<(NS - 2) * K::kLoads>();        // (not for the tiles)
+    else wait_loads<0>();
     take(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (what was there has been read)
     bring(1);
