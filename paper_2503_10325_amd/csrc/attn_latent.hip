@@ -1074,19 +1074,71 @@ __global__ __launch_bounds__(kLaThreads, 1) void attn_latent_kernel(LatentAttnPa
   }
 }
 
-// Merges the partial results of the groups that were cut, piece by piece in their order.  Every workgroup works out which rows there are, and takes its share: four
-// rows at a time, a wave each, or, of many pieces, one, whose pieces the waves share.
+// Merges the partial results of the groups that were cut, pieces in their order.  Every workgroup works out which rows there are, and takes its share: four
+// rows at a time, a wave each; or, of many pieces, a quarter of one, whose pieces the waves share.  Latency bounds it, so that as much as there is of a row is
+// asked for at once (one request, 16 heads, 16000 tokens in 125 pieces: 9 us with whole rows, eight pieces at a time).
 constexpr int kLaMergers = 2048;               // workgroups
 constexpr int kLaFew = 8;                      // pieces
+
+// What is held by reference m, by another one.
+__device__ __forceinline__ float share_at(float m, float now) { return m == -INFINITY ? 0.f : fast_exp2(m - now); }
+// Elements `col` .. + E of a row of pieces first, first + step, ..: their reference, sum of weights and sum of results.
+template <int C, int E, int FLY, typename Part>
+__device__ __forceinline__ void merge_pieces(const LatentAttnParams& P, Part part, int pieces, int first, int step, int col, float& m, float& Z, float (&sum)[E]) {
+  typedef float Words __attribute__((ext_vector_type(E)));
+  for (int i0 = first; i0 < pieces; i0 += FLY * step) {
+    float2 ml[FLY];
+    Words x[FLY];
+#pragma unroll
+    for (int f = 0; f < FLY; ++f) {
+      const int64_t at = part(min(i0 + f * step, pieces - 1));
+      ml[f] = P.ws_ml[at];
+      x[f] = *reinterpret_cast<const Words*>(P.ws_o + at * C + col);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float now = m;
+#pragma unroll
+    for (int f = 0; f < FLY; ++f) {
+      if (i0 + f * step >= pieces) ml[f] = make_float2(-INFINITY, 0.f);
+      now = fmaxf(now, ml[f].x);
+    }
+    const float by = share_at(m, now);
+    m = now;
+    Z *= by;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] *= by;
+#pragma unroll
+    for (int f = 0; f < FLY; ++f) {
+      const float share = ml[f].y * share_at(ml[f].x, now);
+      Z += share;
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] = fmaf(x[f][e], share, sum[e]);
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void write_merged(const LatentAttnParams& P, int64_t row, int C, int col, float m, float Z, const float (&sum)[E]) {
+  typedef float Words __attribute__((ext_vector_type(E)));
+  typedef __bf16 Halves __attribute__((ext_vector_type(E)));
+  const float f = Z == 0.f ? 0.f : 1.f / Z;
+  Words y;
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = sum[e] * f;
+  if (P.out_f32) *reinterpret_cast<Words*>(static_cast<float*>(P.out) + row * C + col) = y;
+  else *reinterpret_cast<Halves*>(static_cast<uint16_t*>(P.out) + row * C + col) = __builtin_convertvector(y, Halves);
+  if (P.lse && col == 0) P.lse[row] = (m + log2f(Z)) * static_cast<float>(kLn2);
+}
+
 template <int C>
-__global__ __launch_bounds__(kLaThreads) void merge_latent_kernel(LatentAttnParams P, int M) {
-  constexpr int E = C / kWave, kFly = 8;
+__global__ __launch_bounds__(kLaThreads, 2) void merge_latent_kernel(LatentAttnParams P, int M) {
+  constexpr int E = C / kWave, kQuarter = E / kLaWaves;         // elements of a lane: of a row, of a quarter
   __shared__ int upto[kLaRanges];
   __shared__ int4 records[kLaRanges];
-  __shared__ float shared_sum[kLaWaves - 1][C], shared_z[kLaWaves - 1];
+  __shared__ float shared_sum[kLaWaves - 1][kQuarter][kWave];
+  __shared__ float2 shared_mz[kLaWaves - 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   static_assert(kLaRanges == kLaThreads, "a thread for each record");
-  auto units_of = [](const int4& r) { const int rows = r.z >> 16, pieces = r.z & 0xffff; return pieces == 0 ? 0 : pieces <= kLaFew ? (rows + kLaWaves - 1) / kLaWaves : rows; };
+  auto units_of = [](const int4& r) { const int rows = r.z >> 16, pieces = r.z & 0xffff; return pieces == 0 ? 0 : pieces <= kLaFew ? (rows + kLaWaves - 1) / kLaWaves : 4 * rows; };
   {
     const int4 r = tid < P.ranges ? P.cut[tid] : make_int4(0, 0, 0, 0);
     records[tid] = r;
@@ -1106,65 +1158,47 @@ __global__ __launch_bounds__(kLaThreads) void merge_latent_kernel(LatentAttnPara
     for (int w = 0; w < kLaRanges / kWave; ++w) k += __popcll(__builtin_amdgcn_ballot_w64(upto[64 * w + lane] <= u));
     const int4 record = records[k];
     const int pieces = record.z & 0xffff, rows = record.z >> 16, unit = u - (k > 0 ? upto[k - 1] : 0);
-    const bool few = pieces <= kLaFew;
-    const int r = few ? unit * kLaWaves + wave : unit;
-    auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
-    float m = -INFINITY, sum[E], Z = 0.f;
+    const int64_t row0 = static_cast<int64_t>(record.y) << 32 | static_cast<unsigned>(record.x);
+    if (pieces <= kLaFew) {
+      const int r = unit * kLaWaves + wave;
+      if (r >= rows) continue;
+      float m = -INFINITY, Z = 0.f, sum[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0.f;
-    if (r < rows) {
-      for (int i = lane; i < pieces; i += kWave) m = fmaxf(m, P.ws_ml[part(i)].x);
-      m = wave_max(m);
-      const int step = few ? 1 : kLaWaves;
-      for (int i0 = few ? 0 : wave; i0 < pieces; i0 += kFly * step) {
-        float2 ml[kFly];
-        float4 x[kFly][E / 4];
+      for (int e = 0; e < E; ++e) sum[e] = 0.f;
+      auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
+      merge_pieces<C, E, kLaFew / 2>(P, part, pieces, 0, 1, E * lane, m, Z, sum);
+      write_merged<E>(P, row0 + r, C, E * lane, m, Z, sum);
+    } else {
+      const int r = unit >> 2, col = (unit & 3) * (C / 4) + kQuarter * lane;
+      float m = -INFINITY, Z = 0.f, sum[kQuarter];
 #pragma unroll
-        for (int f = 0; f < kFly; ++f) {
-          const int64_t at = part(min(i0 + f * step, pieces - 1));
-          ml[f] = P.ws_ml[at];
-#pragma unroll
-          for (int e = 0; e < E / 4; ++e) x[f][e] = *reinterpret_cast<const float4*>(P.ws_o + at * C + e * 4 * kWave + 4 * lane);
-        }
-#pragma unroll
-        for (int f = 0; f < kFly; ++f) {
-          const float share = i0 + f * step >= pieces || ml[f].x == -INFINITY ? 0.f : ml[f].y * fast_exp2(ml[f].x - m);
-          Z += share;
-#pragma unroll
-          for (int e = 0; e < E / 4; ++e) {
-            sum[4 * e] = fmaf(x[f][e].x, share, sum[4 * e]); sum[4 * e + 1] = fmaf(x[f][e].y, share, sum[4 * e + 1]);
-            sum[4 * e + 2] = fmaf(x[f][e].z, share, sum[4 * e + 2]); sum[4 * e + 3] = fmaf(x[f][e].w, share, sum[4 * e + 3]);
-          }
-        }
-      }
-    }
-    if (!few) {
+      for (int e = 0; e < kQuarter; ++e) sum[e] = 0.f;
+      auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
+      merge_pieces<C, kQuarter, 16>(P, part, pieces, wave, kLaWaves, col, m, Z, sum);
       __syncthreads();                                          // (what was there has been read)
       if (wave > 0) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) shared_sum[wave - 1][e * kWave + lane] = sum[e];
-        if (lane == 0) shared_z[wave - 1] = Z;
+        for (int e = 0; e < kQuarter; ++e) shared_sum[wave - 1][e][lane] = sum[e];
+        if (lane == 0) shared_mz[wave - 1] = make_float2(m, Z);
       }
       __syncthreads();
       if (wave > 0) continue;
+      float now = m;
+#pragma unroll
+      for (int w = 0; w < kLaWaves - 1; ++w) now = fmaxf(now, shared_mz[w].x);
+      const float by = share_at(m, now);
+      Z *= by;
+#pragma unroll
+      for (int e = 0; e < kQuarter; ++e) sum[e] *= by;
 #pragma unroll
       for (int w = 0; w < kLaWaves - 1; ++w) {
-        Z += shared_z[w];
+        const float share = share_at(shared_mz[w].x, now);
+        Z = fmaf(shared_mz[w].y, share, Z);
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += shared_sum[w][e * kWave + lane];
+        for (int e = 0; e < kQuarter; ++e) sum[e] = fmaf(shared_sum[w][e][lane], share, sum[e]);
       }
+      write_merged<kQuarter>(P, row0 + r, C, col, now, Z, sum);
     }
-    if (r >= rows) continue;
-    const int64_t row = (static_cast<int64_t>(record.y) << 32 | static_cast<unsigned>(record.x)) + r;
-    const float f = Z == 0.f ? 0.f : 1.f / Z;
-#pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const lf32x4 x = {sum[e] * f, sum[e + 1] * f, sum[e + 2] * f, sum[e + 3] * f};
-      const int64_t to = row * C + e * kWave + 4 * lane;
-      if (P.out_f32) *reinterpret_cast<float4*>(static_cast<float*>(P.out) + to) = make_float4(x[0], x[1], x[2], x[3]);
-      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + to) = pack4(x);
-    }
-    if (P.lse && lane == 0) P.lse[row] = (m + log2f(Z)) * static_cast<float>(kLn2);
   }
 }
 
@@ -1192,7 +1226,7 @@ static int launch_latent(const LatentAttnParams& P, const LatentAttnPlan& p, hip
   static_assert(lds <= 160 * 1024, "");
   if (lds > 65536 && set_lds_once(attn_latent_kernel<K>, lds, lds_set) != 0) return -6;
   hipLaunchKernelGGL(attn_latent_kernel<K>, dim3(p.ranges), dim3(kLaThreads), lds, stream, P);
-  hipLaunchKernelGGL(merge_latent_kernel<K::C>, dim3(static_cast<unsigned>(std::min<int64_t>(kLaMergers, static_cast<int64_t>(p.ranges) * p.rows / 2))), dim3(kLaThreads), 0, stream, P, p.rows);
+  hipLaunchKernelGGL(merge_latent_kernel<K::C>, dim3(static_cast<unsigned>(std::min<int64_t>(kLaMergers, static_cast<int64_t>(p.ranges) * p.rows))), dim3(kLaThreads), 0, stream, P, p.rows);
   return 0;
 }
 template <int C, int R>
