@@ -1206,8 +1206,11 @@ __global__ __launch_bounds__(kLaThreads, 2) void merge_latent_kernel(LatentAttnP
 LatentAttnPlan make_latent_attn_plan(const LatentArgs& a) {
   LatentAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * a.H;
-  const int64_t small = static_cast<int64_t>(a.B) * ((rows + 15) / 16) * ((static_cast<int64_t>(a.max_pages) + 3) / 4);
-  p.rows = rows <= 16 || small <= 2048 ? 16 : rows <= 32 || small <= 6144 ? 32 : rows <= 64 ? 64 : 128;
+  // The more rows the less there is to do for all of them together, but the fewer workgroups share it.  By the number of groups of 16 rows x 64 tokens if all requests
+  // had all their pages (16, 32, 64, 128 rows; us, bf16, C = 512): 36: 15, 17, 21, 27; 1040: 26, 28, 30, 38; 2080: 32, 36, 38, 45; 4160: 47, 37, 52, 55;
+  // 8320: 77, 53, 51, 76; 16640: 127, 88, 78, 67; 33280: 256, 139, 138, 111.  With fp32 results and C = 256 they change places at the same numbers.
+  const int64_t work = static_cast<int64_t>(a.B) * ((rows + 15) / 16) * ((static_cast<int64_t>(a.max_pages) + 3) / 4);
+  p.rows = rows <= 16 || work <= 3000 ? 16 : rows <= 32 || work <= 6000 ? 32 : rows <= 64 || work <= 12000 ? 64 : 128;
   p.groups = static_cast<int>((rows + p.rows - 1) / p.rows);
   const int64_t tiles = static_cast<int64_t>(a.B) * p.groups * static_cast<int64_t>(a.max_pages);
   p.ranges = static_cast<int>(std::min<int64_t>(kLaRanges, (tiles + 7) / 8 * 8));

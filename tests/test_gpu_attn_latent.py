@@ -30,7 +30,7 @@ def lib():
 
 class Device(U.Device):
     """With the block table widened, by columns that hold no pages, until there is more to be done for every request than `least` groups of 16 rows x 64
-    tokens: the kernels of 16, of 32 and of 64 or 128 rows."""
+    tokens: the kernels of 16, 32, 64 and 128 rows."""
     least = 0
 
     def __init__(self, c, **more):
@@ -40,7 +40,7 @@ class Device(U.Device):
         super().__init__(dict(c, table=np.concatenate([c["table"], spare], 1)), **more)
 
 
-@pytest.fixture(params=[0, 2048, 6144], ids=lambda least: f"above{least}", autouse=True)
+@pytest.fixture(params=[0, 3000, 6000, 12000], ids=lambda least: f"above{least}", autouse=True)
 def least(request, monkeypatch):
     monkeypatch.setattr(Device, "least", request.param)
 

@@ -68,7 +68,7 @@ def test_attention():
         assert sv.spec_verify_attn_latent_workspace_size(sv.make_latent_desc(**{**OK, **bad})) == 0
         with pytest.raises(sv.SpecError):
             sv.spec_describe_attn_latent_plan(sv.make_latent_desc(**{**OK, **bad}))
-    for heads, pages, rows in ((4, 10, 16), (8, 10, 16), (8, 4000, 32), (8, 8000, 32), (16, 2000, 32), (16, 4000, 64), (32, 8000, 128)):     # 4 tokens of that many heads
+    for heads, pages, rows in ((4, 10, 16), (8, 10, 16), (8, 4000, 32), (8, 8000, 32), (16, 2000, 32), (16, 4000, 64), (32, 2000, 64), (32, 8000, 128)):     # 4 tokens of that many heads
         plan = sv.spec_describe_attn_latent_plan(sv.make_latent_desc(**{**OK, "num_heads": heads, "max_pages_per_req": pages}))
         assert f" {rows} query rows" in plan, plan
 
