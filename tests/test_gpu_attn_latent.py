@@ -105,11 +105,12 @@ def test_ends_around_tiles(past, n, H):
     check(U.batch(24, ctx=[64 + past, 128 + past - n], n=[n, n], H=H, tree=n > 3))
 
 
-def test_scores_that_grow_and_shrink():
+@pytest.mark.parametrize("H", [16, 48])
+def test_scores_that_grow_and_shrink(H):
     """References that move by more than fp32's range of exponents, upwards again and again."""
     for f32 in (False, True):
         for sign in (1.0, -1.0):
-            c = U.batch(25, ctx=[600], n=[3], H=16, spread=0.0)
+            c = U.batch(25, ctx=[600], n=[3], H=H, spread=0.0)
             for pg in range(c["held"]):
                 place = np.where(c["table"][0] == pg)[0]
                 if len(place):
@@ -124,8 +125,9 @@ def test_other_scales():
     check(c, softmax=1.0, f32=True)
 
 
-def test_pages_that_are_none():
-    c = U.batch(27, ctx=[200, 40, 5, 64], n=[3, 2, 2, 1], H=16)
+@pytest.mark.parametrize("H", [16, 48])
+def test_pages_that_are_none(H):
+    c = U.batch(27, ctx=[200, 40, 5, 64], n=[3, 2, 2, 1], H=H)
     c["table"][0, 1] = -1
     c["table"][0, 12] = c["held"]
     c["table"][1, :] = -1                                        # rows that see nothing at all
@@ -140,8 +142,9 @@ def test_pages_that_are_none():
     check(c)
 
 
-def test_slots_behind_and_pages_that_are_not_the_requests():
-    c = U.batch(30, ctx=[37, 5, 64], n=[3, 2, 1], H=16, tree=True)
+@pytest.mark.parametrize("H", [16, 48])
+def test_slots_behind_and_pages_that_are_not_the_requests(H):
+    c = U.batch(30, ctx=[37, 5, 64], n=[3, 2, 1], H=H, tree=True)
     clean = c["pool"].copy()
     used = np.zeros((c["held"], 16), dtype=bool)
     for b in range(3):
