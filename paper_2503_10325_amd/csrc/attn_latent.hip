@@ -1075,44 +1075,39 @@ __global__ __launch_bounds__(kLaThreads, 1) void attn_latent_kernel(LatentAttnPa
 }
 
 // Merges the partial results of the groups that were cut, pieces in their order.  Every workgroup works out which rows there are, and takes its share: four
-// rows at a time, a wave each; or, of many pieces, a quarter of one, whose pieces the waves share.  Latency bounds it, so that as much as there is of a row is
-// asked for at once (one request, 16 heads, 16000 tokens in 125 pieces: 9 us with whole rows, eight pieces at a time).
+// rows at a time, a wave each; or, of many pieces, a quarter of one, whose pieces the waves share.  Latency bounds it where rows are few: quarters ask for all there is
+// at once (one request, 16 heads, 16000 tokens in 125 pieces: 5 us, whole rows 9).  Where they are not, whole rows have fewer loads to issue (16 requests of 64
+// rows in 16 pieces: 52 us with the attention, in quarters 57).
 constexpr int kLaMergers = 2048;               // workgroups
-constexpr int kLaFew = 8;                      // pieces
+constexpr int kLaFew = 8, kLaFewOfMany = 32, kLaManyRows = 256;      // whole rows: up to 8 pieces, or 32 where there are many rows
 
 // What is held by reference m, by another one.
 __device__ __forceinline__ float share_at(float m, float now) { return m == -INFINITY ? 0.f : fast_exp2(m - now); }
-// Elements `col` .. + E of a row of pieces first, first + step, ..: their reference, sum of weights and sum of results.
+// Elements `col` .. + E of a row of pieces first, first + step, .. (64 at most): their reference, sum of weights and sum of results.
 template <int C, int E, int FLY, typename Part>
-__device__ __forceinline__ void merge_pieces(const LatentAttnParams& P, Part part, int pieces, int first, int step, int col, float& m, float& Z, float (&sum)[E]) {
+__device__ __forceinline__ void merge_pieces(const LatentAttnParams& P, Part part, int pieces, int first, int step, int col, int lane, float& m, float& Z, float (&sum)[E]) {
   typedef float Words __attribute__((ext_vector_type(E)));
-  for (int i0 = first; i0 < pieces; i0 += FLY * step) {
-    float2 ml[FLY];
+  float2 ml = make_float2(-INFINITY, 0.f);                      // a lane for each piece
+  if (first + lane * step < pieces) ml = P.ws_ml[part(first + lane * step)];
+  float share = 0.f;
+  Z = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[e] = 0.f;
+  for (int i0 = 0; first + i0 * step < pieces; i0 += FLY) {
     Words x[FLY];
 #pragma unroll
-    for (int f = 0; f < FLY; ++f) {
-      const int64_t at = part(min(i0 + f * step, pieces - 1));
-      ml[f] = P.ws_ml[at];
-      x[f] = *reinterpret_cast<const Words*>(P.ws_o + at * C + col);
-    }
+    for (int f = 0; f < FLY; ++f) x[f] = *reinterpret_cast<const Words*>(P.ws_o + part(min(first + (i0 + f) * step, pieces - 1)) * C + col);
     __builtin_amdgcn_sched_barrier(0);
-    float now = m;
-#pragma unroll
-    for (int f = 0; f < FLY; ++f) {
-      if (i0 + f * step >= pieces) ml[f] = make_float2(-INFINITY, 0.f);
-      now = fmaxf(now, ml[f].x);
+    if (i0 == 0) {
+      m = wave_max(ml.x);
+      share = ml.y * share_at(ml.x, m);
     }
-    const float by = share_at(m, now);
-    m = now;
-    Z *= by;
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] *= by;
 #pragma unroll
     for (int f = 0; f < FLY; ++f) {
-      const float share = ml[f].y * share_at(ml[f].x, now);
-      Z += share;
+      const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), i0 + f));      // (0 behind the last piece)
+      Z += by;
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] = fmaf(x[f][e], share, sum[e]);
+      for (int e = 0; e < E; ++e) sum[e] = fmaf(x[f][e], by, sum[e]);
     }
   }
 }
@@ -1132,18 +1127,22 @@ __device__ __forceinline__ void write_merged(const LatentAttnParams& P, int64_t 
 template <int C>
 __global__ __launch_bounds__(kLaThreads, 2) void merge_latent_kernel(LatentAttnParams P, int M) {
   constexpr int E = C / kWave, kQuarter = E / kLaWaves;         // elements of a lane: of a row, of a quarter
-  __shared__ int upto[kLaRanges];
+  __shared__ int upto[kLaRanges], rows_of[kLaWaves];
   __shared__ int4 records[kLaRanges];
   __shared__ float shared_sum[kLaWaves - 1][kQuarter][kWave];
   __shared__ float2 shared_mz[kLaWaves - 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   static_assert(kLaRanges == kLaThreads, "a thread for each record");
-  auto units_of = [](const int4& r) { const int rows = r.z >> 16, pieces = r.z & 0xffff; return pieces == 0 ? 0 : pieces <= kLaFew ? (rows + kLaWaves - 1) / kLaWaves : 4 * rows; };
+  int few;                                                      // whole rows up to that many pieces
   {
     const int4 r = tid < P.ranges ? P.cut[tid] : make_int4(0, 0, 0, 0);
     records[tid] = r;
-    const double sum = wave_scan(static_cast<double>(units_of(r)));
-    upto[tid] = static_cast<int>(sum);
+    const int rows = r.z >> 16, pieces = r.z & 0xffff;
+    const double all = wave_scan(static_cast<double>(pieces > 0 ? rows : 0));
+    if (lane == 63) rows_of[wave] = static_cast<int>(all);
+    __syncthreads();
+    few = rows_of[0] + rows_of[1] + rows_of[2] + rows_of[3] >= kLaManyRows ? kLaFewOfMany : kLaFew;
+    upto[tid] = static_cast<int>(wave_scan(static_cast<double>(pieces == 0 ? 0 : pieces <= few ? (rows + kLaWaves - 1) / kLaWaves : 4 * rows)));
     __syncthreads();
     int before = 0;
     for (int w = 0; w < wave; ++w) before += upto[64 * w + 63];
@@ -1159,22 +1158,18 @@ __global__ __launch_bounds__(kLaThreads, 2) void merge_latent_kernel(LatentAttnP
     const int4 record = records[k];
     const int pieces = record.z & 0xffff, rows = record.z >> 16, unit = u - (k > 0 ? upto[k - 1] : 0);
     const int64_t row0 = static_cast<int64_t>(record.y) << 32 | static_cast<unsigned>(record.x);
-    if (pieces <= kLaFew) {
+    if (pieces <= few) {
       const int r = unit * kLaWaves + wave;
       if (r >= rows) continue;
-      float m = -INFINITY, Z = 0.f, sum[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] = 0.f;
+      float m, Z, sum[E];
       auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
-      merge_pieces<C, E, kLaFew / 2>(P, part, pieces, 0, 1, E * lane, m, Z, sum);
+      merge_pieces<C, E, 4>(P, part, pieces, 0, 1, E * lane, lane, m, Z, sum);
       write_merged<E>(P, row0 + r, C, E * lane, m, Z, sum);
     } else {
       const int r = unit >> 2, col = (unit & 3) * (C / 4) + kQuarter * lane;
-      float m = -INFINITY, Z = 0.f, sum[kQuarter];
-#pragma unroll
-      for (int e = 0; e < kQuarter; ++e) sum[e] = 0.f;
+      float m = -INFINITY, Z, sum[kQuarter];
       auto part = [&](int i) { return (static_cast<int64_t>(record.w + i) * 2 + (i == 0 ? 1 : 0)) * M + r; };
-      merge_pieces<C, kQuarter, 16>(P, part, pieces, wave, kLaWaves, col, m, Z, sum);
+      merge_pieces<C, kQuarter, 16>(P, part, pieces, wave, kLaWaves, col, lane, m, Z, sum);
       __syncthreads();                                          // (what was there has been read)
       if (wave > 0) {
 #pragma unroll
