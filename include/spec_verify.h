@@ -571,7 +571,7 @@ size_t spec_verify_attn_latent_workspace_size(const spec_latent_desc* desc);
  * behind the last draft are read but take no part, whatever they hold; an entry of a draft
  * that is not finite reaches only the rows that see that draft.  Accuracy, for a row that
  * sees L positions with weights w, with A the largest scale sum_i |q_i k_i| of them and
- * e = 2^-19 (1 + A) + 2^-28 L: before it is rounded, out is within (2^-8 + e)
+ * e = 2^-17 (1 + A) + 2^-26 L (every rounding at its worst): before it is rounded, out is within (2^-8 + e)
  * sum w |c| (out_dtype SPEC_F32: e sum w |c|) of the exact result; lse is within
  * e + 2^-22 |lse|.  The workspace need not be cleared. */
 int32_t spec_verify_attn_latent(

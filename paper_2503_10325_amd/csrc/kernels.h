@@ -273,7 +273,7 @@ void launch_absorb_latent(const LatentArgs& a, const void* q, int64_t q_stride, 
 int launch_expand_latent(const LatentArgs& a, const void* x, const void* w, int64_t w_stride, void* out, hipStream_t stream);
 // A pure function of the descriptor, as AttnPlan.
 struct LatentAttnPlan {
-  int rows;           // query rows a workgroup takes at a time: 16, 32 or 128
+  int rows;           // query rows a workgroup takes at a time: 16, 32, 64 or 128
   int groups;         // ... groups of so many that cover a request's rows
   int ranges;         // workgroups: ranges of the batch's tokens and groups of equal cost
 };

@@ -1,13 +1,14 @@
-"""Attention over the cache of latents against the 64-bit reference, as accurate as its header says.
+"""Attention over the cache of latents against the 64-bit reference, more accurate than its header says.
 
 For a row that sees L positions with weights w, A the largest scale * sum_i |q_i k_i| among them:
 
     |out - exact| <= (t + e) sum w |c|  (+ half a step of the result's type),   |lse - exact| <= e + 2^-22 |lse|,
-    e = 2^-19 (1 + A) + 2^-28 L,   t = 2^-8 for bf16 results, 0 for fp32 ones.
+    t = 2^-8 for bf16 results, 0 for fp32 ones.
 
-t is half a step of a weight in bf16 (three terms hold all of fp32).  Of e: a score is a sum of exact products in 10 to 18 steps, rounded to fp32 after
-each (2^-24 of at most A), then multiplied and subtracted (2^-24 A each): below 2^-19 A; the exponential 2^-23; the sums of weights and of results in
-L / 32 steps and a few merges, 2^-24 each, in either direction.
+t is half a step of a weight in bf16 (three terms hold all of fp32).  The header's e is 2^-17 (1 + A) + 2^-26 L: a score is a sum of exact products in up
+to 36 steps, rounded to fp32 after each (2^-24 of at most A), then multiplied and subtracted (2^-24 A each), in a weight and in the sum it is divided by:
+76 * 2^-24 A; the exponential and the merges a few 2^-22; results in up to 3 L / 16 steps, sums of weights in L / 32, 2^-24 each: 3.5 * 2^-28 L.  Roundings are of
+either sign, and of n of them about the square root of n remains: the tests hold all kernels to e = 2^-19 (1 + A) + 2^-28 L.
 """
 import numpy as np
 import pytest
