@@ -111,7 +111,8 @@ __device__ __forceinline__ double border(double at, double start, double end) {
 }
 
 // Up to 16 NB rows, NB 1, 2 or 4.  Of the scores a wave takes 16 rows, by half of a tile's tokens (NB 1: two waves have none) or, NB 4, by all.
-// 4096 tokens x 64 requests, 302 MB: 16 rows 60 us, 32 rows 66, 64 rows 80 to 90; with tiles of 64 tokens, two in LDS, 61, 71 and (as 128 rows) 98.
+// 4096 tokens x 64 requests, 302 MB: 16 rows 60 us, 32 rows 65, 64 rows 84 (with another barrier a tile, and no keys read ahead of it, 89); with tiles of 64 tokens,
+// two in LDS, 61, 71 and (as 128 rows) 98.
 template <int C_, int R_, int NB_, int TERMS_>
 struct LatentNarrow {
   static constexpr bool kWide = false;
@@ -126,8 +127,8 @@ struct LatentNarrow {
   static constexpr int kSteps = W / 32;
   static constexpr int kLoads = kTile / kLaWaves / 1024;        // of a wave for a tile
   static constexpr int kOffsets = 8 * kRow / 1024;              // loads that bring 8 rows
-  static constexpr int kWeights = TERMS * RB * 1024, kBuffers = 1;
-  static constexpr int kSmall = kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 + 4 + 80;
+  static constexpr int kWeights = TERMS * RB * 1024, kBuffers = 2;
+  static constexpr int kSmall = kBuffers * kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 + kWave * 4 + 80;
   static constexpr int kStages = std::min(6, (160 * 1024 - kSmall) / kTile);
   static_assert(kStages >= 3 && kRow % 256 == 128 && kLoads == kOffsets, "");
 };
@@ -790,7 +791,8 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
   write_results_wide<K>(P, S, J, o);
 }
 
-// Up to 64 query rows: memory bounds it.  Three tiles or more are on their way while one is worked on, in turn: scores, weights to LDS, results.
+// Up to 64 query rows: memory bounds it, or with 64 the chain of a tile: scores, weights to LDS, a barrier, results.  Two tiles or more are on their way meanwhile; the
+// next tile is there behind the same barrier, so that the first of its keys are read beside the results.
 template <typename K>
 __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J) {
   constexpr int W = K::W, T = K::T, KB = K::KB, WK = K::WK, RB = K::RB, CB = K::CB, kPages = K::kPages, NS = K::kStages, TERMS = K::TERMS;
@@ -864,18 +866,27 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) o[cb][rb] = lf32x4{0.f, 0.f, 0.f, 0.f};
 
+  // All but the last `ahead` tiles (or fewer, of all that there are) have come.
+  auto arrived = [&](int ahead) __attribute__((always_inline)) {
+    if (NS >= 6 && ahead >= 4) wait_loads<4 * K::kLoads>();
+    else if (NS >= 5 && ahead == 3) wait_loads<3 * K::kLoads>();
+    else if (NS >= 4 && ahead == 2) wait_loads<2 * K::kLoads>();
+    else if (ahead == 1) wait_loads<K::kLoads>();
+    else wait_loads<0>();
+  };
+  constexpr int kDeep = 8;                                      // K is read seven steps ahead
+  lbf16x8 k[kDeep][KB];
+  auto read_k = [&](unsigned tile, int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) k[step % kDeep][kb] = operand(read_lds16(((tile + k_at) ^ (64 * (step & 1))) + 128 * (step >> 1) + kb * 16 * K::kRow));
+  };
+  arrived(min(NS - 2, J.t1 - 1 - J.t0));
+  lds_sync();
+#pragma unroll
+  for (int step = 0; step < kDeep - 1; ++step) read_k(ring, step);
+
   int slot = 0;
   for (int t = J.t0; t < J.t1; ++t) {
-    // ---- the tile is here, and all waves are done with the one before ----
-    const int more = J.t1 - 1 - t;
-    if (more >= NS - 2) wait_loads<(NS - 2) * K::kLoads>();
-    else if (NS >= 5 && more == 2) wait_loads<2 * K::kLoads>();
-    else if (NS >= 6 && more == 3) wait_loads<3 * K::kLoads>();
-    else if (NS >= 4 && more == 1) wait_loads<K::kLoads>();
-    else wait_loads<0>();
-    lds_sync();
-    const bool another = t + NS - 1 < J.t1;
-    if (another) aim(t + NS - 1, slot == 0 ? NS - 1 : slot - 1, NS - 1);
     const unsigned tile = ring + slot * K::kTile;
     const bool special = (t + 1) * static_cast<int64_t>(T) > J.ctx || (bad & 3u) != 0u;
 
@@ -902,27 +913,17 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
       // the two blocks of 16 tokens are the halves of a lane's 16 bytes
 #pragma unroll
       for (int term = 0; term < TERMS; ++term) {
-        const unsigned at = p_at + (term * RB + block) * 1024;
+        const unsigned at = p_at + (t & 1) * K::kWeights + (term * RB + block) * 1024;
         if constexpr (KB == 1) *lds_pointer<unsigned long long>(at + 8 * part) = static_cast<unsigned long long>(w[term][0][1]) << 32 | w[term][0][0];
         else *lds_pointer<raw4>(at) = raw4{w[term][0][0], w[term][0][1], w[term][1][0], w[term][1][1]};
       }
     };
     if (scores) {
-      // (K is read ahead, and the loads of a tile lie between the products: all at once they wait for each other)
-      constexpr int kDeep = 8;
-      lbf16x8 k[kDeep][KB];
-      auto read_k = [&](int step) __attribute__((always_inline)) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) k[step % kDeep][kb] = operand(read_lds16(((tile + k_at) ^ (64 * (step & 1))) + 128 * (step >> 1) + kb * 16 * K::kRow));
-      };
-#pragma unroll
-      for (int step = 0; step < kDeep - 1; ++step) read_k(step);
 #pragma unroll
       for (int step = 0; step < K::kSteps; ++step) {
-        if (step + kDeep - 1 < K::kSteps) read_k(step + kDeep - 1);
+        if (step + kDeep - 1 < K::kSteps) read_k(tile, step + kDeep - 1);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) s[kb] = multiply(k[step % kDeep][kb], qf[step], step == 0 ? lf32x4{0.f, 0.f, 0.f, 0.f} : s[kb]);
-        if (another && step % 2 == 0 && step / 2 < K::kLoads) issue(step / 2);
         __builtin_amdgcn_sched_barrier(0);
       }
       // masks: only where the tile reaches the drafts, or a page is none
@@ -943,14 +944,16 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
       for (int kb = 0; kb < KB; ++kb) top = max3(top, max3(s[kb][0], s[kb][1], s[kb][2]), s[kb][3]);
       top *= P.c;
       weigh();
-    } else if (another) {
-#pragma unroll
-      for (int j = 0; j < K::kLoads; ++j) issue(j);
     }
+    // ---- behind the barrier: all weights are there, the next tile is, and all waves are done with the one before ----
     const unsigned flag = any_lane(top > ref + kLaSlack) ? 1u : 0u;
-    if (lane == 0) S.ahead[0][wave] = flag;
+    if (lane == 0) S.ahead[t & 1][wave] = flag;
+    arrived(min(NS - 3, J.t1 - 2 - t));
     lds_sync();
-    const raw4 flags = *reinterpret_cast<const raw4*>(S.ahead[0]);
+    const raw4 flags = *reinterpret_cast<const raw4*>(S.ahead[t & 1]);
+    const bool another = t + NS - 1 < J.t1;
+    if (another) aim(t + NS - 1, slot == 0 ? NS - 1 : slot - 1, NS - 1);
+    slot = slot + 1 == NS ? 0 : slot + 1;
     if (__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3])) {
       // ---- a row's reference follows its maximum where that has come far ahead (in all waves, or in none) ----
       if (scores) {
@@ -990,19 +993,31 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
 #pragma unroll
     for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) p[term][rb] = operand(read_lds16(p_at + (term * RB + rb) * 1024));
+      for (int rb = 0; rb < RB; ++rb) p[term][rb] = operand(read_lds16(p_at + (t & 1) * K::kWeights + (term * RB + rb) * 1024));
+    lbf16x8 v[3];
+    auto read_v = [&](int cb) __attribute__((always_inline)) {
+      const unsigned at = ((tile + v_at) ^ (64 * ((cb >> 1) & 1))) + 128 * (cb >> 2) + 8 * (cb & 1);
+      v[cb % 3] = join(read_columns(at), read_columns(at + 16 * K::kRow));
+    };
+    read_v(0);
+    read_v(1);
+    // (a tile's loads lie between the products: all at once they wait for each other)
+    if (another) issue(0);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-      const unsigned at = ((tile + v_at) ^ (64 * ((cb >> 1) & 1))) + 128 * (cb >> 2) + 8 * (cb & 1);
-      const lbf16x8 v = join(read_columns(at), read_columns(at + 16 * K::kRow));
+      if (cb + 2 < CB) read_v(cb + 2);
+#pragma unroll
+      for (int step = cb * kDeep / CB; step < (cb + 1) * kDeep / CB && step < kDeep - 1; ++step) read_k(ring + slot * K::kTile, step);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-        for (int term = 0; term < TERMS; ++term) o[cb][rb] = multiply(v, p[term][rb], o[cb][rb]);
+        for (int term = 0; term < TERMS; ++term) o[cb][rb] = multiply(v[cb % 3], p[term][rb], o[cb][rb]);
       }
+      if (another && cb + 1 < K::kLoads) issue(cb + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    static_assert(K::kLoads <= CB + 1, "");
     bad >>= kPages;
-    slot = slot + 1 == NS ? 0 : slot + 1;
   }
 
   write_results<K>(P, S, J, o, ref, sum, wave, lane);
