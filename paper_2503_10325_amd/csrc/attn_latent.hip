@@ -662,9 +662,9 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
     const unsigned inside1 = opaque(tile1 + in_tile), outside1 = opaque(apart + ((t + 1) & 1) * K::kWeights);
     lbf16x8 p[2][RB];
     ls16x4 v[3][2];
-    auto read_v = [&](int i, int part) __attribute__((always_inline)) {                     // block i % CB, tokens 16 (i / CB) ..
+    auto read_v = [&](int b, int part) __attribute__((always_inline)) {                     // block b % CB, tokens 16 (b / CB % 2) ..
       const unsigned at = part == 0 ? v_base : v_other;
-      v[i % 3][part] = read_columns((at ^ (64 * (i % CB & 1))) + 128 * (i % CB >> 1) + (i / CB * 16 + part * 8) * K::kRow);
+      v[b % 3][part] = read_columns((at ^ (64 * (b % CB & 1))) + 128 * (b % CB >> 1) + (b / CB % 2 * 16 + part * 8) * K::kRow);
     };
 #pragma unroll
     for (int step = kRead; step < kSteps; ++step) {
@@ -695,18 +695,12 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
     };
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      const int term = b / (2 * CB), i = b % (2 * CB);
-      if (term > 0 && i == 0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) read_v(j >> 1, j & 1);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) p[0][rb] = read_p(inside, outside, 2 * RB * term + rb);
-      }
+      const int next = b / CB + 1;                              // operands: of a term's first or second 16 tokens
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        if (rb < 2 && i + 2 < 2 * CB) read_v(i + 2, rb);
-        if (i == CB - 1) p[1][rb] = read_p(inside, outside, 2 * RB * term + RB + rb);
-        accumulate(o[i % CB][rb], join(v[i % 3][0], v[i % 3][1]), p[i / CB][rb]);
+        if (rb < 2 && b + 2 < kBlocks) read_v(b + 2, rb);
+        if (b % CB == CB - 2 && next < 2 * TERMS) p[next & 1][rb] = read_p(inside, outside, RB * next + rb);
+        accumulate(o[b % CB][rb], join(v[b % 3][0], v[b % 3][1]), p[b / CB & 1][rb]);
         beside(b * RB + rb);
         __builtin_amdgcn_sched_barrier(0);
       }
