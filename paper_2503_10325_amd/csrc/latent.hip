@@ -42,6 +42,11 @@ struct LatentParams {
 };
 
 // ---- append -----------------------------------------------------------------------------------------------------
+// 1 / sqrt(x), off by a few steps of fp64: the instruction's estimate (2^-24) and a step of Newton's method, which squares its error.
+__device__ __forceinline__ double inverse_root(double x) {
+  const double y = __builtin_amdgcn_rsq(x), next = fma(0.5 * y, fma(-x * y, y, 1.0), y);
+  return x > 0.0 && x < INFINITY ? next : y;
+}
 // A workgroup takes the new tokens of one page, a wave four of them at a time, their latents asked for before anything else.  Sums of squares are held in
 // fp64 (so that no bf16 latent overflows them), a result is rounded to fp32 and then once to bf16.  Few tokens: a chain of trips to memory, 3 us;
 // 22000 tokens: 16 us, 3.1 TB/s read + written (a copy: 5.2), as all workgroups are resident and load, compute and store at the same time.
@@ -90,7 +95,7 @@ __global__ __launch_bounds__(kLatentThreads) void append_latent_kernel(LatentPar
         sum = fma(a, a, sum);
         sum = fma(b, b, sum);
       }
-      const double by = 1.0 / sqrt(wave_sum(sum) * (1.0 / C) + static_cast<double>(P.eps));
+      const double by = inverse_root(wave_sum(sum) * (1.0 / C) + static_cast<double>(P.eps));
 #pragma unroll
       for (int i = 0; i < E / 2; ++i) {
         const abf16x2 y = {static_cast<__bf16>(static_cast<float>(bf16_lo(x[j][i]) * by * bf16_lo(g[i]))),
