@@ -49,7 +49,7 @@ __device__ __forceinline__ double inverse_root(double x) {
 }
 // A workgroup takes the new tokens of one page, a wave four of them at a time, their latents asked for before anything else.  Sums of squares are held in
 // fp64 (so that no bf16 latent overflows them), a result is rounded to fp32 and then once to bf16.  Few tokens: a chain of trips to memory, 3 us;
-// 22000 tokens: 16 us, 3.1 TB/s read + written (a copy: 5.2), as all workgroups are resident and load, compute and store at the same time.
+// 22000 tokens: 15 us, 3.3 TB/s read + written (a copy: 5.2), as all workgroups are resident and load, compute and store at the same time.
 template <int C>
 __global__ __launch_bounds__(kLatentThreads) void append_latent_kernel(LatentParams P) {
   constexpr int E = C / kWave;                                  // elements of a lane
