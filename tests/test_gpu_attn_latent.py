@@ -81,6 +81,7 @@ CASES = {
     "chain128": dict(ctx=[70], n=[128], H=2),
     "ragged": dict(ctx=[1, 900, 17, 64, 333, 2], n=[3, 1, 10, 2, 5, 7], H=20),
     "many": dict(ctx=[(37 * i) % 200 for i in range(150)], n=[i % 4 for i in range(150)], H=8),
+    "many_of_many_rows": dict(ctx=[(53 * i) % 150 for i in range(140)], n=[(i % 7) // 2 for i in range(140)], H=50),
     "long": dict(ctx=[20000, 777], n=[2, 1], H=4),
 }
 
