@@ -7,8 +7,8 @@
 // Query rows of a request (node x head, consecutive in memory) are taken in groups of 16, 32 or 128, the tokens in tiles, which four waves bring to LDS and
 // share: LatentNarrow and LatentWide below.  Of the second product every wave takes C / 4 columns for all rows; the weights go through LDS.
 //
-// Bound: up to 32 rows by memory (64 tokens' rows in one, 2048 x 64 of 16 heads: 39 us, 5.6 TB/s, and 6 for the merge), with 128 by the matrix instructions
-// (batch 64, 8192 tokens, 4 x 128 rows: 1160 TFLOP/s of the 1520 that a large matrix product reaches).
+// Bound: up to 32 rows by memory (64 requests of 2048 tokens at the median, 16 heads, from cold caches: 48 us, 4.6 TB/s with the start, and 6 for the merge), with 128
+// by the matrix instructions (64 requests of 8192 tokens, 4 x 128 rows: 1160 to 1190 TFLOP/s of the 1520 that a large matrix product reaches).
 //
 // Work: the tiles of all requests and groups lie end to end and are cut into ranges of equal cost, one per workgroup, whatever the lengths; every
 // workgroup works out from ctx_len and q_offsets which pieces its range holds.  Groups that are cut leave partial results, which a second launch
