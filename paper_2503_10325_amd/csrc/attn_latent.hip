@@ -4,7 +4,7 @@
 //   S^T = K Q^T     matrix instructions leave a lane with consecutive tokens of one query row, 4 (16x16x32) or 8 (32x32x16: 4 and 4) at a time
 //   O^T = V^T P^T   so its weights, in bf16, are operands as they are; V^T, the same bytes as K, is read from LDS by columns
 // fp32 results take the weights in three terms of bf16, which hold all of fp32.
-// Query rows of a request (node x head, consecutive in memory) are taken in groups of 16, 32 or 128, the tokens in tiles, which four waves bring to LDS and
+// Query rows of a request (node x head, consecutive in memory) are taken in groups of 16, 32, 64 or 128, the tokens in tiles, which four waves bring to LDS and
 // share: LatentNarrow and LatentWide below.  Of the second product every wave takes C / 4 columns for all rows; the weights go through LDS.
 //
 // Bound: up to 32 rows by memory (64 requests of 2048 tokens at the median, 16 heads, from cold caches: 48 us, 4.6 TB/s with the start, and 6 for the merge), with 128
