@@ -139,6 +139,7 @@ struct LatentWide {
   static constexpr int C = C_, R = R_, TERMS = TERMS_;
   static constexpr int W = C + R;
   static constexpr int kHead = TERMS == 1 ? 12 : 5, kSnap = 4, kLeast = 4;      // see LaCut
+  static constexpr bool kMoved = C == 256 && TERMS == 3;        // see accumulate()
   static constexpr int M = 128, T = 32, WK = 1;
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
@@ -309,9 +310,13 @@ __device__ __forceinline__ void write_results(const LatentAttnParams& P, LatentS
 }
 
 // An accumulation in registers of their own kind (the compiler, left to choose, keeps results in vector registers and copies the queries' operands for
-// every product).  Nothing that the compiler knows of may read or write x within a few instructions: see settle().
+// every product).  Nothing that the compiler knows of may read or write x within a few instructions: see settle().  MOVED: where it keeps results in other
+// registers for one of the loops, and moves them right in front of their products: a product reads what a vector instruction writes two wait states later.
+// (tests/test_kernel_waits.py reads the built code for which kernels that is so.)
+template <bool MOVED>
 __device__ __forceinline__ void accumulate(lf32x16& x, lbf16x8 a, lbf16x8 b) {
-  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(a), "v"(b));
+  if constexpr (MOVED) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(a), "v"(b));
+  else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void clear(lf32x16& x) {
 #pragma unroll
@@ -700,7 +705,7 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
       for (int rb = 0; rb < RB; ++rb) {
         if (rb < 2 && b + 2 < kBlocks) read_v(b + 2, rb);
         if (b % CB == CB - 2 && next < 2 * TERMS) p[next & 1][rb] = read_p(inside, outside, RB * next + rb);
-        accumulate(o[b % CB][rb], join(v[b % 3][0], v[b % 3][1]), p[b / CB & 1][rb]);
+        accumulate<K::kMoved>(o[b % CB][rb], join(v[b % 3][0], v[b % 3][1]), p[b / CB & 1][rb]);
         beside(b * RB + rb);
         __builtin_amdgcn_sched_barrier(0);
       }
