@@ -573,7 +573,9 @@ size_t spec_verify_attn_latent_workspace_size(const spec_latent_desc* desc);
  * sees L positions with weights w, with A the largest scale sum_i |q_i k_i| of them and
  * e = 2^-17 (1 + A) + 2^-26 L (every rounding at its worst): before it is rounded, out is within (2^-8 + e)
  * sum w |c| (out_dtype SPEC_F32: e sum w |c|) of the exact result; lse is within
- * e + 2^-22 |lse|.  The workspace need not be cleared. */
+ * e + 2^-22 |lse|.  That holds while L times the largest |c| is at most 2^111 (beyond, sums may
+ * become infinite before they are divided), and but for weights and products below 2^-126,
+ * which may count as zero.  The workspace need not be cleared. */
 int32_t spec_verify_attn_latent(
     const spec_latent_desc* desc,
     const void* q,               /* [total_q, H, C + R] bf16                           */
