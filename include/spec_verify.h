@@ -569,7 +569,8 @@ size_t spec_verify_attn_latent_workspace_size(const spec_latent_desc* desc);
  * Positions whose page is outside [0, num_pages), or behind max_pages_per_req pages, count as
  * not there; a row that sees no position at all gives zeros and lse = -infinity.  Slots
  * behind the last draft are read but take no part, whatever they hold; an entry of a draft
- * that is not finite reaches only the rows that see that draft.  Accuracy, for a row that
+ * that is not finite reaches only the rows that see that draft, and makes their results NaN
+ * if it is the latent's, whatever its weight.  Accuracy, for a row that
  * sees L positions with weights w, with A the largest scale sum_i |q_i k_i| of them and
  * e = 2^-17 (1 + A) + 2^-26 L (every rounding at its worst): before it is rounded, out is within (2^-8 + e)
  * sum w |c| (out_dtype SPEC_F32: e sum w |c|) of the exact result; lse is within

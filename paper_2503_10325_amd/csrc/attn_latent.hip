@@ -130,7 +130,7 @@ struct LatentNarrow {
   static constexpr int kLoads = kTile / kLaWaves / 1024;        // of a wave for a tile
   static constexpr int kOffsets = 8 * kRow / 1024;              // loads that bring 8 rows
   static constexpr int kWeights = TERMS * RB * 1024, kBuffers = 2;
-  static constexpr int kSmall = kBuffers * kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 + kWave * 4 + 80;
+  static constexpr int kSmall = kBuffers * kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 + kWave * 4 + 96;
   static constexpr int kStages = std::min(6, (160 * 1024 - kSmall) / kTile);
   static_assert(kStages >= 3 && kRow % 256 == 128 && kLoads == kOffsets, "");
 };
@@ -153,7 +153,7 @@ struct LatentWide {
   static constexpr int kInTile = T * 128 / 1024;                // of a tile's 8 TERMS operands of 1 KB: those that lie in the tile itself, where
   static constexpr int kWeights = (TERMS * 2 * RB - kInTile) * 1024, kBuffers = 2;      // the shared part of the keys was; the others' bytes
   static constexpr int kSmall = kBuffers * kWeights + kLaMaxNodes * 16 + 4 * M * (3 + WK) + std::max(4 * M * WK, 4 * kLaMaxNodes) + 32 + kWave * 20 +
-                                2 * kOffsets * kWave * 4 + 80;
+                                2 * kOffsets * kWave * 4 + 96;
   static constexpr int kStages = std::min(4, (160 * 1024 - kSmall) / kTile);
   static_assert(kStages >= 3 && kRow % 256 == 128 && kLoads == kOffsets, "");
 };
@@ -162,7 +162,7 @@ template <typename K>
 struct LatentShared {
   __align__(1024) unsigned char ring[K::kStages][K::kTile];
   __align__(16) unsigned char p[K::kBuffers][K::kWeights];
-  unsigned long long anc[kLaMaxNodes][2];
+  unsigned long long anc[kLaMaxNodes + 1][2];                   // of the nodes; the last: nodes with latents that are not finite, see take_out()
   int node[K::M];
   union {
     int parent[kLaMaxNodes];                                    // (until the ancestors are known)
@@ -226,7 +226,7 @@ __device__ __forceinline__ void find_lineage(const LatentAttnParams& P, LatentSh
   asm volatile("" : "+s"(heads));                               // (or its reciprocal is kept across pieces)
   if (tid < K::M) S.node[tid] = (J.row_base + min(tid, J.rows - 1)) / heads;
   lds_sync();
-  if (tid < kLaMaxNodes) {
+  if (tid <= kLaMaxNodes) {                                     // (the last: none yet)
     unsigned long long w[2] = {0ull, 0ull};
     if (tid < J.n) {
       if (P.parent) {
@@ -246,23 +246,45 @@ __device__ __forceinline__ void find_lineage(const LatentAttnParams& P, LatentSh
   }
 }
 
-// A weight of zero times what is not finite would be NaN: where rows differ in what they see, such values are taken out of V.  (A row that sees one has met it in
-// its scores.)  By all threads, of a tile that all have read for the scores.
+// A weight of zero times what is not finite is NaN, also where the zero is that of a row that does not see the token: where rows differ in what they see, such
+// values are taken out of V, and the drafts that had them noted (a row that sees one need not have met it in its scores: one of -infinity is a weight of zero).
+// What all rows see stays.  By all threads, of tile t, that all have read for the scores; `none`: its pages that are none, a bit each.
 template <typename K>
-__device__ __forceinline__ void take_out(unsigned tile, int tid) {
-  constexpr int kUnits = K::C / 8;
-  for (int u = tid; u < K::T * kUnits; u += kLaThreads) {
-    const unsigned at = tile + u / kUnits * K::kRow + u % kUnits * 16;
-    raw4 w = read_lds16(at);
-    bool any = false;
+__device__ __forceinline__ void take_out(LatentShared<K>& S, unsigned tile, int tid, int t, int ctx, unsigned none) {
+  constexpr int kUnits = K::C / 8, kBy = kLaThreads / kUnits, kFly = K::kWide ? 4 : K::T / kBy;
+  const int shared = static_cast<int>(min(ctx - static_cast<int64_t>(t) * K::T, static_cast<int64_t>(K::T)));      // tokens of the context
+  const unsigned mine = tile + tid / kUnits * K::kRow + tid % kUnits * 16;
+#pragma unroll 1
+  for (int from = 0; from < K::T; from += kBy * kFly) {
+    raw4 w[kFly];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool l = (w[i] & 0x7f80u) == 0x7f80u, h = (w[i] & 0x7f800000u) == 0x7f800000u;
-      any |= l | h;
-      w[i] = (l ? 0u : w[i] & 0xffffu) | (h ? 0u : w[i] & 0xffff0000u);
+    for (int f = 0; f < kFly; ++f) w[f] = read_lds16(mine + (from + f * kBy) * K::kRow);
+#pragma unroll
+    for (int f = 0; f < kFly; ++f) {
+      const int token = from + f * kBy + tid / kUnits, node = token - shared;
+      const bool there = ((none >> (token / kLaPage)) & 1u) == 0u;
+      raw4 x;
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool l = (w[f][i] & 0x7f80u) == 0x7f80u, h = (w[f][i] & 0x7f800000u) == 0x7f800000u;
+        any |= l | h;
+        x[i] = (l ? 0u : w[f][i] & 0xffffu) | (h ? 0u : w[f][i] & 0xffff0000u);
+      }
+      if (!any || (there && node < 0)) continue;
+      *lds_pointer<raw4>(mine + (from + f * kBy) * K::kRow) = x;
+      if (there && node < kLaMaxNodes) atomicOr(&S.anc[kLaMaxNodes][node >> 6], 1ull << (node & 63));
     }
-    if (any) *lds_pointer<raw4>(at) = w;
   }
+}
+// What a row's results are multiplied by, with z its sum of weights: NaN where it sees a draft that take_out has noted.
+template <typename K>
+__device__ __forceinline__ float result_factor(const LatentShared<K>& S, const LatentPiece& J, int row, float z) {
+  if (J.t1 * static_cast<int64_t>(K::T) > J.ctx) {              // (else there are no nodes)
+    const unsigned long long lo = S.anc[kLaMaxNodes][0], hi = S.anc[kLaMaxNodes][1];
+    if ((lo | hi) != 0ull && ((S.anc[S.node[row]][0] & lo) | (S.anc[S.node[row]][1] & hi)) != 0ull) return __builtin_nanf("");
+  }
+  return z == 0.f ? 0.f : 1.f / z;
 }
 
 template <typename K>
@@ -294,7 +316,7 @@ __device__ __forceinline__ void write_results(const LatentAttnParams& P, LatentS
   for (int rb = 0; rb < RB; ++rb) {
     const int row = 16 * rb + rn;
     if (row >= J.rows) continue;
-    const float z = row_sum(row), f = z == 0.f ? 0.f : 1.f / z;
+    const float f = result_factor<K>(S, J, row, row_sum(row));
 #pragma unroll
     for (int cb = 0; cb < CB; cb += 2) {
       const lf32x4 a = o[cb][rb] * f, b = o[cb + 1][rb] * f;
@@ -364,7 +386,9 @@ __device__ __forceinline__ void write_results_wide(const LatentAttnParams& P, La
     const float l = S.sum[0][tid], m = l == 0.f ? -INFINITY : S.by[0][tid];
     if (!J.whole) P.ws_ml[J.part + tid] = make_float2(m, l);
     else if (P.lse) P.lse[row0 + tid] = (m + log2f(l)) * static_cast<float>(kLn2);
+    S.top[0][tid] = result_factor<K>(S, J, tid, l);
   }
+  lds_sync();
   // Through LDS, so that a store takes consecutive bytes of rows (straight from the registers: 16 bytes of 64 rows, and 40000 cycles for a piece of fp32 results).
   auto put = [&](auto f32, auto row_blocks) __attribute__((always_inline)) {
     constexpr bool kF32 = decltype(f32)::value;
@@ -378,7 +402,7 @@ __device__ __forceinline__ void write_results_wide(const LatentAttnParams& P, La
 #pragma unroll
       for (int j = 0; j < kTogether; ++j) {
         const int rb = rb0 + j;
-        const float l = S.sum[0][32 * rb + rn], f = l == 0.f ? 0.f : 1.f / l;
+        const float f = S.top[0][32 * rb + rn];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
           const unsigned at = ring + (32 * j + rn) * kApart + (wave * (K::C / 4) + 32 * cb + 16 * h) * (kF32 ? 4 : 2);
@@ -764,7 +788,7 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
       }
       settle();
       if (t >= drafts_from || (bad & 3u) != 0u) {
-        take_out<K>(ring + slot * K::kTile, tid);
+        take_out<K>(S, ring + slot * K::kTile, tid, t, J.ctx, bad & 3u);
         lds_sync();
       }
     }
@@ -985,7 +1009,7 @@ __device__ __forceinline__ void latent_piece(const LatentAttnParams& P, LatentSh
     sum += z;
 
     if (special) {
-      take_out<K>(tile, tid);
+      take_out<K>(S, tile, tid, t, J.ctx, bad & 3u);
       lds_sync();
     }
 
