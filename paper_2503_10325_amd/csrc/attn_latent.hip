@@ -141,7 +141,7 @@ struct LatentWide {
   static constexpr int C = C_, R = R_, TERMS = TERMS_;
   static constexpr int W = C + R;
   static constexpr int kHead = TERMS == 1 ? 12 : 5, kSnap = 4, kLeast = 4;      // see LaCut
-  static constexpr bool kMoved = C == 256 && TERMS == 3;        // see accumulate()
+  static constexpr bool kMoved = C == 256 && TERMS == 3;        // in the outer loop, see accumulate()
   static constexpr int M = 128, T = 32, WK = 1;
   static constexpr int kUnits = (W / 8 + 7) / 8 * 8;
   static constexpr int kRow = 16 * kUnits, kTile = T * kRow;
@@ -679,7 +679,7 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
     return special;
   };
   // The rest of the scores; O^T += V^T P^T of tile t, and the weights of the tile behind it.
-  auto second_half = [&](int t, int slot) __attribute__((always_inline)) {
+  auto second_half = [&](auto moved, int t, int slot) __attribute__((always_inline)) {
     const int slot1 = slot + 1 == NS ? 0 : slot + 1;
     const unsigned tile = ring + slot * K::kTile, tile1 = ring + slot1 * K::kTile, tile2 = ring + (slot1 + 1 == NS ? 0 : slot1 + 1) * K::kTile;
 #pragma unroll
@@ -731,7 +731,7 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
       for (int rb = 0; rb < RB; ++rb) {
         if (rb < 2 && b + 2 < kBlocks) read_v(b + 2, rb);
         if (b % CB == CB - 2 && next < 2 * TERMS) p[next & 1][rb] = read_p(inside, outside, RB * next + rb);
-        accumulate<K::kMoved>(o[b % CB][rb], join(v[b % 3][0], v[b % 3][1]), p[b / CB & 1][rb]);
+        accumulate<decltype(moved)::value>(o[b % CB][rb], join(v[b % 3][0], v[b % 3][1]), p[b / CB & 1][rb]);
         beside(b * RB + rb);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -793,8 +793,15 @@ __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, Lat
       }
     }
     bool more;
+    if constexpr (K::kMoved) {                                  // (a copy of its own for the outer loop, where the moves are)
+      second_half(std::true_type(), t, slot);
+      slot = slot + 1 == NS ? 0 : slot + 1;
+      if (++t >= J.t1) break;
+      special = first_half(t, slot);
+      if (special != 0u) continue;
+    }
     do {
-      second_half(t, slot);
+      second_half(std::false_type(), t, slot);
       slot = slot + 1 == NS ? 0 : slot + 1;
       more = ++t < J.t1;
       if (!more) break;
