@@ -502,8 +502,10 @@ int32_t spec_compact_kv_quant(
  * latent_dim elements per token, k_h = [W_k,h c | r] and v_h = W_v,h c, with R = rope_dim
  * more elements r, rotated by position, that the keys of all heads share.  The cache holds
  * [c | r] of a token as a row of W = C + R elements: pool [num_pages, page_size, W] bf16.
- * The weights go to the other side of the attention (the absorbed form: for at most
- * 128 drafts the cheaper one),
+ * The weights go to the other side of the attention (the absorbed form, with fewer
+ * operations than keys and values of every head for up to C (N + V) / (2 C - N - V) new
+ * tokens of a request, N = nope_dim, V = value_dim: 171 with C = 512, N = V = 128, and
+ * 73 to 256 with the other sizes),
  *   <q_h, k_h> = <[q_nope W_k,h | q_rope], [c | r]>,
  *   sum_t p_t v_h,t = W_v,h sum_t p_t c_t,
  * so that a step is: append, absorb, attention over the rows (the first C elements are
@@ -526,7 +528,8 @@ typedef struct {
   int32_t page_size;         /* tokens per cache page: 16                           */
   int32_t total_q;           /* rows of the step's tensors; q_offsets[B] at most    */
   int32_t max_q_per_req;     /* upper bound of the new tokens of a request          */
-  int32_t max_pages_per_req; /* row stride of block_table                           */
+  int32_t max_pages_per_req; /* row stride of block_table; the attention's kernel is chosen as
+                                if all requests had so many pages (results are right for any) */
   int32_t num_pages;         /* pages of the pool                                   */
   int32_t interleaved;       /* rotated pairs: 0 = (i, i + R / 2), 1 = (2 i, 2 i + 1) */
   int32_t out_dtype;         /* spec_dtype of the attention's `out`                 */
@@ -538,7 +541,7 @@ typedef struct {
 /* New tokens into the cache: row q_offsets[b] + i to slot ctx_len[b] + i, prompts (any
  * length, parent == NULL) and drafts alike.  With norm_weight g the latent x is normalised
  * on the way, c = x g / sqrt(mean(x^2) + norm_eps), else copied; the shared key is rotated.
- * Results are rounded once.  What spec_append_kv says of slots without a page holds here. */
+ * Results are worked out in fp64 (c) or fp32 and rounded from fp32.  What spec_append_kv says of slots without a page holds here. */
 int32_t spec_append_latent(
     const spec_latent_desc* desc, /* host                                             */
     const void* latent, int64_t latent_stride, /* [total_q] rows of C bf16            */

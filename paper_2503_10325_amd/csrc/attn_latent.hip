@@ -3,7 +3,8 @@
 //
 //   S^T = K Q^T     matrix instructions leave a lane with consecutive tokens of one query row, 4 (16x16x32) or 8 (32x32x16: 4 and 4) at a time
 //   O^T = V^T P^T   so its weights, in bf16, are operands as they are; V^T, the same bytes as K, is read from LDS by columns
-// fp32 results take the weights in three terms of bf16, which hold all of fp32.
+// fp32 results take the weights in three terms of bf16, which hold all of fp32; bf16 results take one, whose rounding weighs as much as the result's own: together
+// 0.0020 to 0.0023 of a result (root mean square; the result's alone 0.0017), where two terms would double the products of the second kind.
 // Query rows of a request (node x head, consecutive in memory) are taken in groups of 16, 32, 64 or 128, the tokens in tiles, which four waves bring to LDS and
 // share: LatentNarrow and LatentWide below.  Of the second product every wave takes C / 4 columns for all rows; the weights go through LDS.
 //
@@ -28,7 +29,8 @@ constexpr int kLaMaxNodes = 128;
 constexpr int kLaRanges = 256;                 // workgroups: one per compute unit
 constexpr float kLaNoScore = -3.0e38f;         // the reference before the first position: finite, so that -infinity stays ahead of nothing
 // A row's reference follows its maximum when that is 2^16 ahead: weights are at most 2^16, and sums of L of them times latents of up to c stay finite while
-// L c < 2^112.  (Sooner costs time: 2^8 ahead, 5 requests of 61 nodes, 40 heads 145 us, 138 as it is and with 2^40; the serving batch 356, 348 and 350.)
+// L c < 2^112.  (Sooner costs time: 2^8 ahead, from cold caches, 5 requests of 61 nodes, 40 heads 145 us, 138 with 2^16
+// and with 2^40; 64 requests of 2 to 10 tokens, 128 heads 356, 348 and 350.)
 constexpr float kLaSlack = 16.f;
 
 struct LatentAttnParams {
@@ -442,8 +444,11 @@ __device__ __forceinline__ void write_results_wide(const LatentAttnParams& P, La
 // Up to 128 query rows: matrix instructions bound it, and one wave per SIMD has to keep them busy by itself, at one instruction in 5 cycles.  32x32x16
 // products: a lane has 16 of a tile's 32 scores of one query row (lane % 32; score i: token 8 (i / 4) + 4 (lane / 32) + i % 4), so that a wave works out the
 // weights and the references of its 32 rows by itself.  In turn:
-//   scores of tile t + 1 (36 products, a read of LDS each), at whose middle lies the barrier behind which all waves' weights of tile t are there, then
+//   scores of tile t + 1 (36 products, a read of LDS each), at whose middle lies the barrier behind which all waves' weights of tile t are there, with the loads of
+//   tile t + kStages - 1, then
 //   O^T += V^T P^T of tile t (32 products), between which the weights of tile t + 1 are worked out.
+// With four stages (C = 256) a tile's loads have the time of a whole tile and are waited for at the next one's barrier; with three, all that LDS holds at
+// C = 512, they are waited for behind the results, with a second barrier.
 // A tile of C = 512 takes 3250 cycles, 2176 of them in the products; 64 requests x 8192 tokens x 4 x 128 rows 490 to 505 us, 1160 to 1190 TFLOP/s.
 template <typename K>
 __device__ __forceinline__ void latent_piece_wide(const LatentAttnParams& P, LatentShared<K>& S, const LatentPiece& J) {
@@ -1251,7 +1256,8 @@ LatentAttnPlan make_latent_attn_plan(const LatentArgs& a) {
   LatentAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(a.max_q) * a.H;
   // The more rows, the less there is to do for all of them together, but the fewer workgroups share it.  By the number of groups of 16 rows x 64 tokens if all requests
-  // had all their pages (16, 32, 64, 128 rows; us, bf16, C = 512): 36: 15, 17, 21, 27; 1040: 26, 28, 30, 38; 2080: 32, 36, 38, 45; 4160: 47, 37, 52, 55;
+  // had all their pages (lengths are on the device; a table far wider than they need costs up to twice the time: 4 requests of 512 tokens, 128 heads, 18 us with
+  // 33 pages a row, 30 with 2048), 16, 32, 64, 128 rows; us, bf16, C = 512: 36: 15, 17, 21, 27; 1040: 26, 28, 30, 38; 2080: 32, 36, 38, 45; 4160: 47, 37, 52, 55;
   // 8320: 77, 53, 51, 76; 16640: 127, 88, 78, 67; 33280: 256, 139, 138, 111.  With fp32 results and C = 256 they change places at the same numbers.
   const int64_t work = static_cast<int64_t>(a.B) * ((rows + 15) / 16) * ((static_cast<int64_t>(a.max_pages) + 3) / 4);
   p.rows = rows <= 16 || work <= 3000 ? 16 : rows <= 32 || work <= 6000 ? 32 : rows <= 64 || work <= 12000 ? 64 : 128;

@@ -42,7 +42,7 @@ struct LatentParams {
 };
 
 // ---- append -----------------------------------------------------------------------------------------------------
-// 1 / sqrt(x), off by a few steps of fp64: the instruction's estimate (2^-24) and a step of Newton's method, which squares its error.
+// 1 / sqrt(x), to about 2^-47: the instruction's estimate (2^-24) and a step of Newton's method, which takes an error of e to 1.5 e^2.
 __device__ __forceinline__ double inverse_root(double x) {
   const double y = __builtin_amdgcn_rsq(x), next = fma(0.5 * y, fma(-x * y, y, 1.0), y);
   return x > 0.0 && x < INFINITY ? next : y;
